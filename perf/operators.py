@@ -199,14 +199,14 @@ def _plan(s):
     shape = hs.make_attn_shape(case["batch"], case["heads"], case["kv_heads"], case["d"], case["page"],
                                s["blocks"], s["table"].shape[1],
                                hs.HS_FP16 if case["dtype"] == "fp16" else hs.HS_BF16)
-    size = 0
+    size, bound = 0, s["table"].shape[1] * case["page"]     # the most keys that the table can list
     if case["op"] == "prefill":
         size = hs.hs_attn_prefill_workspace_bytes(shape, s["kv"], s["n"])
     elif case["op"] == "decode":
-        size = hs.hs_attn_decode_workspace_bytes(shape, case["kv_hi"])
+        size = hs.hs_attn_decode_workspace_bytes(shape, bound)
     elif case["op"] == "shared":
-        size = hs.hs_attn_decode_shared_workspace_bytes(shape, case["prefix"], case["kv_hi"])
-    s["plan"] = (hs, shape, torch.empty(max(size, 16), dtype=torch.uint8, device=DEV), size)
+        size = hs.hs_attn_decode_shared_workspace_bytes(shape, case["prefix"], bound)
+    s["plan"] = (hs, shape, torch.empty(max(size, 16), dtype=torch.uint8, device=DEV), size, bound)
     return s["plan"]
 
 
@@ -218,7 +218,7 @@ def run(s):
     case = s["case"]
     op = case["op"]
     if own:
-        hs, shape, ws, size = s.get("plan") or _plan(s)
+        hs, shape, ws, size, bound = s.get("plan") or _plan(s)
         if op == "append":
             hs.hs_kv_append(shape, s["k"], s["v"], 0, s["slots"], s["cu"][-1], s["cache"])
             return {"cache": s["cache"]}
@@ -226,11 +226,11 @@ def run(s):
             hs.hs_attn_prefill(shape, s["q"], s["cache"], s["table"], s["o"], s["lse"], s["kv"], s["n"],
                                s["cu"], ws, size)
         elif op == "decode":
-            hs.hs_attn_decode(shape, s["q"], s["cache"], s["table"], s["kv_len"], case["kv_hi"], s["o"],
-                              s["lse"], ws, size)
+            hs.hs_attn_decode(shape, s["q"], s["cache"], s["table"], s["kv_len"], bound, s["o"], s["lse"],
+                              ws, size)
         else:
             hs.hs_attn_decode_shared(shape, s["q"], s["cache"], s["prefix_table"], case["prefix"],
-                                     s["table"], s["kv_len"], case["kv_hi"], s["o"], s["lse"], ws, size)
+                                     s["table"], s["kv_len"], bound, s["o"], s["lse"], ws, size)
         return _answers(s)
     if op == "append":
         P = case["page"]
