@@ -32,6 +32,7 @@ HS_DEVERR_BLOCK_OOB = 1
 HS_DEVERR_MISALIGNED = 2
 HS_DEVERR_NULL = 3
 HS_DEVERR_TIMEOUT = 4
+HS_DEVERR_LENGTH = 5
 
 HS_MAX_BATCH = 384
 HS_CHUNK = 64
@@ -43,12 +44,17 @@ HS_LINATTN_RECURRENT = 1
 HS_LINATTN_CHUNKED_TC = 2
 HS_LINATTN_SINGLE_TOKEN = 3
 
+HS_BF16 = 0
+HS_FP16 = 1
+
 EXPORTED = ("hs_status_string", "hs_version", "hs_align_prefix", "hs_restore_kv_pages",
             "hs_save_kv_pages", "hs_restore_kv_page_slices", "hs_save_kv_page_slices",
             "hs_restore_state", "hs_checkpoint_states", "hs_linattn_prefill_from_state",
             "hs_linattn_num_checkpoints", "hs_linattn_prefill_packed", "hs_restore_request",
             "hs_test_prefill_stalled", "hs_linattn_prefill_scan", "hs_linattn_scan_workspace_bytes",
-            "hs_linattn_prefill_scan_noalloc")
+            "hs_linattn_prefill_scan_noalloc", "hs_kv_append", "hs_attn_prefill",
+            "hs_attn_prefill_workspace_bytes", "hs_attn_decode", "hs_attn_decode_workspace_bytes",
+            "hs_attn_decode_shared", "hs_attn_decode_shared_workspace_bytes")
 
 
 class HsError(RuntimeError):
@@ -61,6 +67,13 @@ class hs_linattn_shape(C.Structure):
     _fields_ = [("batch", C.c_int32), ("n_heads", C.c_int32), ("d_k", C.c_int32),
                 ("d_v", C.c_int32), ("max_tokens", C.c_int64), ("kernel", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class hs_attn_shape(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("dtype", C.c_int32),
+                ("num_blocks", C.c_int64), ("max_pages", C.c_int64), ("q_stride", C.c_int64),
+                ("o_stride", C.c_int64), ("scale", C.c_float), ("unsplit", C.c_int32)]
 
 
 _lock = threading.Lock()
@@ -100,6 +113,15 @@ def load() -> C.CDLL:
             L.hs_linattn_scan_workspace_bytes.argtypes = [C.POINTER(hs_linattn_shape), vp, vp, vp]
             L.hs_linattn_prefill_scan_noalloc.argtypes = [C.POINTER(hs_linattn_shape), vp, vp, vp,
                                                           vp, vp, vp, vp, vp, i32, vp, vp, vp]
+            ash = C.POINTER(hs_attn_shape)
+            L.hs_kv_append.argtypes = [ash, vp, vp, i64, vp, i64, vp, vp, vp]
+            L.hs_attn_prefill.argtypes = [ash, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+            L.hs_attn_prefill_workspace_bytes.argtypes = [ash, vp, vp, vp]
+            L.hs_attn_decode.argtypes = [ash, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp]
+            L.hs_attn_decode_workspace_bytes.argtypes = [ash, i64, vp]
+            L.hs_attn_decode_shared.argtypes = [ash, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, i64,
+                                                vp, vp]
+            L.hs_attn_decode_shared_workspace_bytes.argtypes = [ash, i64, i64, vp]
             for name in EXPORTED[2:]:
                 getattr(L, name).restype = C.c_int
             _lib = L
@@ -364,3 +386,82 @@ def hs_linattn_num_checkpoints(pos0, n_tokens, ckpt_interval: int) -> int:
         B, p0, nt, int(ckpt_interval), C.addressof(tot))
     _check(rc, "hs_linattn_num_checkpoints")
     return tot.value
+
+
+def make_attn_shape(batch, n_heads, n_kv_heads, head_dim, page_size, num_blocks, max_pages,
+                    dtype=HS_BF16, scale=None, q_stride=0, o_stride=0, unsplit=False):
+    """scale=None: head_dim ** -0.5."""
+    return hs_attn_shape(int(batch), int(n_heads), int(n_kv_heads), int(head_dim), int(page_size),
+                         int(dtype), int(num_blocks), int(max_pages), int(q_stride), int(o_stride),
+                         float(head_dim) ** -0.5 if scale is None else float(scale), int(unsplit))
+
+
+def hs_kv_append(shape: hs_attn_shape, k, v, kv_stride: int, slots, n_rows: int, cache, d_err=None,
+                 stream=None):
+    """slots: device int64, block * page_size + row in the page; negative: the row is skipped."""
+    rc = (_lib or load()).hs_kv_append(
+        C.byref(shape), _ptr(k), _ptr(v), int(kv_stride), _ptr(slots), int(n_rows), _ptr(cache),
+        _ptr(d_err), _stream(stream))
+    _check(rc, "hs_kv_append")
+
+
+def hs_attn_prefill_workspace_bytes(shape: hs_attn_shape, pos0, n_tokens) -> int:
+    B = int(shape.batch)
+    p0, keep_p0 = _i64(pos0, B)
+    nt, keep_nt = _i32(n_tokens, B)
+    out = C.c_int64()
+    rc = (_lib or load()).hs_attn_prefill_workspace_bytes(C.byref(shape), p0, nt, C.addressof(out))
+    _check(rc, "hs_attn_prefill_workspace_bytes")
+    return out.value
+
+
+def hs_attn_prefill(shape: hs_attn_shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows,
+                    workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """Causal attention of packed tails over the paged cache.  pos0 / n_tokens / cu_rows: host
+    sequences of length batch, batch, batch + 1; lse may be None."""
+    B = int(shape.batch)
+    p0, keep_p0 = _i64(pos0, B)
+    nt, keep_nt = _i32(n_tokens, B)
+    cu, keep_cu = _i64(cu_rows, B + 1)
+    rc = (_lib or load()).hs_attn_prefill(
+        C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(o), _ptr(lse), p0, nt, cu,
+        _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
+    _check(rc, "hs_attn_prefill")
+
+
+def hs_attn_decode_workspace_bytes(shape: hs_attn_shape, max_kv_len: int) -> int:
+    out = C.c_int64()
+    rc = (_lib or load()).hs_attn_decode_workspace_bytes(C.byref(shape), int(max_kv_len),
+                                                         C.addressof(out))
+    _check(rc, "hs_attn_decode_workspace_bytes")
+    return out.value
+
+
+def hs_attn_decode(shape: hs_attn_shape, q, cache, block_table, kv_len, max_kv_len: int, o, lse=None,
+                   workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """One decode step; kv_len: device int32 [batch], the token of the step counted in."""
+    rc = (_lib or load()).hs_attn_decode(
+        C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(kv_len), int(max_kv_len),
+        _ptr(o), _ptr(lse), _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
+    _check(rc, "hs_attn_decode")
+
+
+def hs_attn_decode_shared_workspace_bytes(shape: hs_attn_shape, prefix_len: int,
+                                          max_kv_len: int) -> int:
+    out = C.c_int64()
+    rc = (_lib or load()).hs_attn_decode_shared_workspace_bytes(
+        C.byref(shape), int(prefix_len), int(max_kv_len), C.addressof(out))
+    _check(rc, "hs_attn_decode_shared_workspace_bytes")
+    return out.value
+
+
+def hs_attn_decode_shared(shape: hs_attn_shape, q, cache, prefix_table, prefix_len: int, block_table,
+                          kv_len, max_kv_len: int, o, lse=None, workspace=None,
+                          workspace_bytes: int = 0, d_err=None, stream=None):
+    """One decode step of requests behind one cached prefix; kv_len and block_table: of the keys
+    behind it."""
+    rc = (_lib or load()).hs_attn_decode_shared(
+        C.byref(shape), _ptr(q), _ptr(cache), _ptr(prefix_table), int(prefix_len),
+        _ptr(block_table), _ptr(kv_len), int(max_kv_len), _ptr(o), _ptr(lse), _ptr(workspace),
+        int(workspace_bytes), _ptr(d_err), _stream(stream))
+    _check(rc, "hs_attn_decode_shared")

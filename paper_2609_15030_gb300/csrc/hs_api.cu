@@ -20,10 +20,11 @@ inline hs_status cuda_status(cudaError_t e)
     return e == cudaSuccess ? HS_OK : HS_ERR_CUDA;
 }
 
-// the current device's SM count, queried once per device
 std::atomic<int> g_sm_count[64];
 
-hs_status sm_count(int *out)
+}  // namespace
+
+hs_status hs::device_sm_count(int *out)
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess)
@@ -35,6 +36,13 @@ hs_status sm_count(int *out)
     if (dev >= 0 && dev < 64)
         g_sm_count[dev].store(*out, std::memory_order_relaxed);
     return HS_OK;
+}
+
+namespace {
+
+inline hs_status sm_count(int *out)
+{
+    return hs::device_sm_count(out);
 }
 
 hs_status copy_slots(const float *const *src, float *const *dst, int32_t n, int64_t floats_each,

@@ -117,6 +117,9 @@ struct GlaParams {
     int32_t row0[HS_MAX_BATCH];     // token row of the problem's first token in q/k/v/log_g/o
 };
 
+// the current device's SM count, queried once per device (hs_api.cu)
+hs_status device_sm_count(int *out);
+
 // launchers (return the launch's cudaError_t)
 cudaError_t launch_kv_scatter(const void *const *staging, void *const *cache, int32_t n_layers,
                               const int32_t *bt, int32_t n_pages, int64_t page_bytes,
