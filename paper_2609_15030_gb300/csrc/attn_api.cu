@@ -72,8 +72,32 @@ hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
     p.n_kv = s.n_kv_heads;
     p.group = s.n_heads / s.n_kv_heads;
     p.page_shift = page_shift(s.page_size);
+    p.unsplit = s.unsplit;
     p.scale_log2 = s.scale * 1.4426950408889634f;
     return HS_OK;
+}
+
+// the plan of a valid call, and whether the caller's workspace holds it
+hs_status plan(hs::AttnParams &p, int d, int64_t *bytes)
+{
+    int sms = 0;
+    const hs_status st = hs::device_sm_count(&sms);
+    if (st == HS_OK)
+        *bytes = hs::plan_attn(p, d, sms);
+    return st;
+}
+
+hs_status run(hs::AttnParams &p, const hs_attn_shape &s, void *workspace, int64_t workspace_bytes,
+              cudaStream_t stream)
+{
+    int64_t need = 0;
+    const hs_status st = plan(p, s.head_dim, &need);
+    if (st != HS_OK)
+        return st;
+    if (need > workspace_bytes || (need > 0 && workspace == nullptr))
+        return HS_ERR_INVALID_ARG;
+    p.part = static_cast<float *>(workspace);
+    return cuda_status(hs::launch_attn(p, s.head_dim, s.dtype, stream));
 }
 
 // the requests' lengths into p; *any: whether there is a token
@@ -99,8 +123,8 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
         if (n_tokens[b] == 0)
             continue;
         *any = true;
-        if (pos0[b] + n_tokens[b] > INT32_MAX - 256 ||
-            (int64_t)n_tokens[b] * p.group > INT32_MAX - 512 ||
+        if (pos0[b] + n_tokens[b] > INT32_MAX - 8192 ||
+            (int64_t)n_tokens[b] * p.group > INT32_MAX - 8192 ||
             (rows && cu_rows[b] + n_tokens[b] > INT32_MAX / p.n_heads))
             return HS_ERR_UNSUPPORTED;
         p.pos0[b] = (int32_t)pos0[b];
@@ -113,7 +137,7 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
 hs_status check_pointers(const hs::AttnParams &p, const void *workspace, int64_t workspace_bytes)
 {
     if (p.q == nullptr || p.cache == nullptr || p.table == nullptr || p.o == nullptr ||
-        workspace_bytes < 0)
+        workspace_bytes < 0 || p.num_blocks < 1)
         return HS_ERR_INVALID_ARG;
     if (misaligned16(p.q) || misaligned16(p.cache) || misaligned16(p.o) || misaligned16(workspace) ||
         (reinterpret_cast<uintptr_t>(p.table) & 3u) != 0 ||
@@ -131,7 +155,7 @@ hs_status check_decode(const hs_attn_shape *shp, int64_t prefix_len, int64_t max
     const int64_t room = shp->max_pages > INT32_MAX ? INT64_MAX : shp->max_pages * shp->page_size;
     if (prefix_len < 0 || max_kv_len < 0 || max_kv_len > room)
         return HS_ERR_INVALID_ARG;
-    if (prefix_len > INT32_MAX - 256 || max_kv_len > INT32_MAX - 256 - prefix_len)
+    if (prefix_len > INT32_MAX - 8192 || max_kv_len > INT32_MAX - 8192 - prefix_len)
         return HS_ERR_UNSUPPORTED;
     p.max_kv = (int32_t)max_kv_len;
     p.prefix_len = (int32_t)prefix_len;
@@ -162,7 +186,7 @@ hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache,
     st = check_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
-    return cuda_status(hs::launch_attn(p, shp->head_dim, shp->dtype, stream));
+    return run(p, *shp, workspace, workspace_bytes, stream);
 }
 
 }  // namespace
@@ -220,7 +244,7 @@ hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *c
     st = check_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
-    return cuda_status(hs::launch_attn(p, shp->head_dim, shp->dtype, stream));
+    return run(p, *shp, workspace, workspace_bytes, stream);
 }
 
 hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_t *pos0,
@@ -236,7 +260,7 @@ hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_
     if (st != HS_OK)
         return st;
     *bytes_out = 0;
-    return HS_OK;
+    return any ? plan(p, shp->head_dim, bytes_out) : HS_OK;
 }
 
 hs_status hs_attn_decode(const hs_attn_shape *shp, const void *q, const void *cache,
@@ -274,7 +298,10 @@ hs_status hs_attn_decode_shared_workspace_bytes(const hs_attn_shape *shp, int64_
     if (st != HS_OK)
         return st;
     *bytes_out = 0;
-    return HS_OK;
+    if (p.batch == 0)
+        return HS_OK;
+    p.kv_len = bytes_out != nullptr ? reinterpret_cast<const int32_t *>(bytes_out) : nullptr;
+    return plan(p, shp->head_dim, bytes_out);
 }
 
 }  // extern "C"

@@ -73,6 +73,19 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
     }
 }
 
+// registers per thread of this warpgroup (all four of its warps), out of those the block was launched with
+template <int N>
+__device__ __forceinline__ void more_registers()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+template <int N>
+__device__ __forceinline__ void fewer_registers()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 // ---------------------------------------------------------------- TMA
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, int32_t x, int32_t y,
@@ -92,6 +105,29 @@ __device__ __forceinline__ void tma_prefetch_2d(const void *tmap, int32_t x, int
                      reinterpret_cast<uint64_t>(tmap)),
                  "r"(x), "r"(y)
                  : "memory");
+}
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t y,
+                                            int32_t z, int32_t w, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+        : "memory");
+}
+
+// 16 bytes of global memory to shared memory, zeros where `ok` is false (nothing is read then)
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool ok)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+                 "r"(ok ? 16 : 0)
+                 : "memory");
+}
+
+__device__ __forceinline__ void cp_async_wait_all()
+{
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 __device__ __forceinline__ void fence_proxy_async_smem()
@@ -294,6 +330,12 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int b_mn = 0)
 {
     return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// the same with bf16 A and B (format 1)
+__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn = 0)
+{
+    return idesc_f16(M, N, b_mn) | (1u << 7) | (1u << 10);
 }
 
 __device__ __forceinline__ void tmem_wait_ld()
