@@ -17,7 +17,7 @@
 // them.  With `unsplit` a CTA takes the whole items that begin in its run.
 //
 // Warps.  Per tile of rows one group of four softmax warps (thread = row = TMEM lane), then one
-// warp that issues the MMAs, one that loads keys and values by TMA, one that looks after values at
+// warp that issues the MMAs, one that loads keys and values by TMA, two that look after values at
 // masked places.  Per key tile and group: S = Q K^T into TMEM; the group reads it, writes the
 // weights over it as 16-bit pairs; O += P V with P as the TMEM operand.  With two groups the
 // tensor core works on one while the other is in its softmax.
@@ -58,7 +58,7 @@ struct Cfg {
     // groups had left the segment before the one before it
     static constexpr int kMarks = kStages <= 5 ? 4 : 8;
     static constexpr int kSoftmax = NG * 4;                // warps
-    static constexpr int kThreads = (kSoftmax + 4) * 32;   // the last warp only lends its registers
+    static constexpr int kThreads = (kSoftmax + 4) * 32;
     // registers of a softmax thread and of another one, out of those of the launch (65,536 over the
     // resident threads, a multiple of 8): 256 x 224 + 128 x 56 = 384 x 168 and
     // 128 x 200 + 128 x 56 = 256 x 128
@@ -482,6 +482,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     if (warp == C::kSoftmax)
         tmem_alloc(smem_u32(&sm.tmem), C::kTmemCols);
     pdl_wait();
+    if (p.joined)
+        pdl_release();     // the join takes its place as CTAs end
     if (warp == C::kSoftmax + 1) {
         int before = 0;
         const int own = p.kv_len != nullptr ? read_lengths(p, sm.len, lane, cta == 0, 0, &before) : 0;
@@ -664,9 +666,22 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             }
             __syncwarp();
         }
-    } else if (warp == C::kSoftmax + 2) {
-        // ---- values at masked places
+    } else {
+        // ---- values at masked places, two warps
         uint32_t n = 0, seg = 0, ph_raw = 0;
+        const int who = tid - (C::kSoftmax + 2) * 32;
+        auto pair_and = [](bool x) {
+            int r;
+            asm volatile("{\n\t.reg .pred p, q;\n\t"
+                         "setp.ne.s32 p, %1, 0;\n\t"
+                         "bar.red.and.pred q, 1, 64, p;\n\t"
+                         "selp.s32 %0, 1, 0, q;\n\t}"
+                         : "=r"(r)
+                         : "r"((int)x)
+                         : "memory");
+            return r != 0;
+        };
+        auto pair_sync = [] { asm volatile("bar.sync 1, 64;" ::: "memory"); };
         bool go = true;
         for (; go && walk.next(s); ++seg) {
             int all = group_keys<NG>(p, sm.len, s, NG - 1);
@@ -681,16 +696,18 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 if (k0 + kKeys <= common)
                     continue;
                 if (!clean) {
-                    for (int i = lane; i < D; i += 32)
+                    for (int i = who; i < D; i += 64)
                         from[i] = INT_MAX;
-                    if (lane == 0)
+                    if (who == 0)
                         *any = 0;
                     clean = true;
-                    __syncwarp();
+                    pair_sync();
                 }
                 const uint32_t st = (2 * n + 1) % kSt;
                 go = wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1);
                 ph_raw ^= 1u << st;
+                // both warps go on or neither: they meet in a plain barrier below
+                go = pair_and(go);
                 if (!go)
                     break;
                 uint8_t *const v = smem_raw + (NG + st) * C::kTile;
@@ -699,30 +716,41 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 const int hi = all - k0 < kKeys ? all - k0 : kKeys;
                 const int end = (hi + 15) / 16 * 16;
                 // 16 bytes at a time: chunk x of row r is chunk x & 7 of half x >> 3, swizzled
-                for (int i = lo * (D / 8) + lane; i < end * (D / 8); i += 32) {
+                constexpr int kAhead = 8;
+                auto chunk = [&](int i) {
                     const int r = i / (D / 8), x = i % (D / 8);
-                    uint4 *const at = reinterpret_cast<uint4 *>(
-                        v + ((r >> 3) * kHalf + (x >> 3)) * 1024 + (r & 7) * 128 +
-                        (((x & 7) ^ (r & 7)) << 4));
-                    if (r >= hi) {
-                        *at = make_uint4(0, 0, 0, 0);
-                        continue;
+                    return reinterpret_cast<uint4 *>(v + ((r >> 3) * kHalf + (x >> 3)) * 1024 +
+                                                     (r & 7) * 128 + (((x & 7) ^ (r & 7)) << 4));
+                };
+                for (int i0 = lo * (D / 8) + who; i0 < hi * (D / 8); i0 += 64 * kAhead) {
+                    uint32_t bad = 0;
+                    uint4 y[kAhead];
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k) {
+                        const int i = i0 + k * 64;
+                        y[k] = i < hi * (D / 8) ? *chunk(i) : make_uint4(0, 0, 0, 0);
                     }
-                    const uint4 y = *at;
-                    if ((not_finite<T>(y.x) | not_finite<T>(y.y) | not_finite<T>(y.z) |
-                         not_finite<T>(y.w)) == 0)
+#pragma unroll
+                    for (int k = 0; k < kAhead; ++k)
+                        bad |= not_finite<T>(y[k].x) | not_finite<T>(y[k].y) | not_finite<T>(y[k].z) |
+                               not_finite<T>(y[k].w);
+                    if (bad == 0)
                         continue;
-                    uint16_t *const e = reinterpret_cast<uint16_t *>(at);
-                    for (int w = 0; w < 8; ++w)
-                        if ((not_finite<T>(e[w]) & 0x8000u) != 0) {
-                            atomicMin(&from[x * 8 + w], k0 + r);
-                            e[w] = 0;
-                            *any = 1;
-                        }
+                    for (int i = i0; i < hi * (D / 8) && i < i0 + 64 * kAhead; i += 64) {
+                        uint16_t *const e = reinterpret_cast<uint16_t *>(chunk(i));
+                        for (int w = 0; w < 8; ++w)
+                            if ((not_finite<T>(e[w]) & 0x8000u) != 0) {
+                                atomicMin(&from[i % (D / 8) * 8 + w], k0 + i / (D / 8));
+                                e[w] = 0;
+                                *any = 1;
+                            }
+                    }
                 }
+                for (int i = hi * (D / 8) + who; i < end * (D / 8); i += 64)
+                    *chunk(i) = make_uint4(0, 0, 0, 0);
                 fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0)
+                pair_sync();
+                if (who == 0)
                     mbar_arrive(full(st));
             }
         }
@@ -759,12 +787,21 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 keys = p.pos0[x.b] + t + 1;
             }
         };
+        // a warp copies its 32 rows, a row's 16-byte chunks by neighbouring lanes
         auto load_q = [&]() {
-            const T *const src = static_cast<const T *>(p.q) + (ok ? row * p.q_stride + head * D : 0);
-            const uint32_t dst = q_at + g * C::kTile + (uint32_t)r * 128;
+            constexpr int kChunks = D / 8, kRows = 32 / kChunks;
+            const int64_t from = ok ? row * p.q_stride + head * D : 0;
+            const unsigned real = __ballot_sync(0xffffffffu, ok);
+            const int c = lane % kChunks;
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c)
-                cp_async_16(dst + (c >> 3) * 16384 + (((c & 7) ^ (r & 7)) << 4), src + c * 8, ok);
+            for (int i = 0; i < 32; i += kRows) {
+                const int rr = i + lane / kChunks;
+                const int64_t at = __shfl_sync(0xffffffffu, from, rr);
+                const int r8 = rr & 7;
+                cp_async_16(q_at + g * C::kTile + (c >> 3) * 16384 + ((warp & 3) * 32 + rr) * 128 +
+                                (((c & 7) ^ r8) << 4),
+                            static_cast<const T *>(p.q) + at + c * 8, (real >> rr) & 1);
+            }
         };
         auto q_done = [&]() {
             cp_async_wait_all();
@@ -829,26 +866,26 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                     }
                 }
                 const float shift = m == -INFINITY ? 0.f : -m;
-                float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+                const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
+                uint64_t l01 = 0, l23 = 0;
 #pragma unroll
                 for (int c = 0; c < kKeys; c += 32) {
                     uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) {
-                        const float a0 = ex2(fmaf(x[c + 2 * i], p.scale_log2, shift));
-                        const float a1 = ex2(fmaf(x[c + 2 * i + 1], p.scale_log2, shift));
-                        const float a2 = ex2(fmaf(x[c + 2 * i + 2], p.scale_log2, shift));
-                        const float a3 = ex2(fmaf(x[c + 2 * i + 3], p.scale_log2, shift));
-                        l0 += a0;
-                        l1 += a1;
-                        l2 += a2;
-                        l3 += a3;
+                        const float2 y0 = unpair(fma2(pair(x[c + 2 * i], x[c + 2 * i + 1]), scale2, shift2));
+                        const float2 y1 =
+                            unpair(fma2(pair(x[c + 2 * i + 2], x[c + 2 * i + 3]), scale2, shift2));
+                        const float a0 = ex2(y0.x), a1 = ex2(y0.y), a2 = ex2(y1.x), a3 = ex2(y1.y);
+                        l01 = add2(l01, pair(a0, a1));
+                        l23 = add2(l23, pair(a2, a3));
                         w[i] = Elem<T>::pack(a0, a1);
                         w[i + 1] = Elem<T>::pack(a2, a3);
                     }
                     tmem_st16(s_at + c / 2, w);
                 }
-                l += (l0 + l1) + (l2 + l3);
+                const float2 ls = unpair(add2(l01, l23));
+                l += ls.x + ls.y;
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(bar_p);
@@ -957,107 +994,190 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
 // ---- joining partial results ---------------------------------------------------------------
 //
 // With M = max m_i over the parts of a row: o = sum 2^(m_i - M) a_i / L, L = sum 2^(m_i - M) l_i,
-// lse = ln 2 (M + log2 L).  A warp takes a row, D / 32 columns a lane; parts in the order of their
-// keys, so that the same split gives the same bits.
+// lse = ln 2 (M + log2 L).  One to eight warps take a row, D / 32 columns a lane; warp y of w has
+// the parts y, y + w, ..., and their sums are added in the order of the warps, so that the same split
+// gives the same bits.  A lane looks up one part's pair and address, so that neither these loads nor
+// those of the parts' rows wait for one another: what bounds the join of a few rows is latency.
+
+constexpr int kMergeWarps = 8;
 
 template <int D>
 struct Joined {
     float a[D / 32];
-    float m = -INFINITY, l = 0.f;
-    __device__ Joined()
-    {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-            a[i] = 0.f;
-    }
-    __device__ void add(const float *slot, int rows, int r, int lane)
-    {
-        const float2 ml = reinterpret_cast<const float2 *>(slot)[r];
-        if (ml.x == -INFINITY && ml.y == 0.f)
-            return;                                  // no key of this part: a is not written
-        const float top = fmaxf(m, ml.x);
-        const float f = ex2(m - top), h = ex2(ml.x - top);
-        m = top;
-        l = l * f + ml.y * h;
-        const float *src = slot + pairs_floats(rows) + (int64_t)r * D + lane * (D / 32);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i)
-            a[i] = a[i] * f + src[i] * h;
-    }
-    template <typename T>
-    __device__ void write(const AttnParams &p, int64_t row, int head, int lane) const
-    {
-        const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-        uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<T *>(p.o) + row * p.o_stride + head * D +
-                                                   lane * (D / 32));
-#pragma unroll
-        for (int i = 0; i < D / 32; i += 2)
-            o[i / 2] = Elem<T>::pack(a[i] * inv, a[i + 1] * inv);
-        if (p.lse != nullptr && lane == 0)
-            p.lse[row * p.n_heads + head] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
-    }
+    float m, l;
 };
 
-constexpr int kMergeWarps = 8;
-
-// items split between CTAs: block (c, y) takes the item inside which CTA c's run begins, if it is the
-// first one to begin there
-template <typename T, int D, int NG>
-__global__ void __launch_bounds__(kMergeWarps * 32)
-attn_merge_kernel(const __grid_constant__ AttnParams p)
+// `part(i, pair, a)`: where part i has the row's pair and its a, false if it has none (its CTA has no
+// units)
+template <int D, typename F>
+__device__ __forceinline__ Joined<D> join_parts(const float *base, int count, int first, int step,
+                                                int lane, F part)
 {
-    __shared__ int32_t len[HS_MAX_BATCH];
-    __shared__ Start start;
-    __shared__ int own;
-    pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = blockIdx.x + 1;
-    if (warp == 0) {
-        int before = 0;
-        const int n = p.kv_len != nullptr ? read_lengths(p, len, lane, false, 0, &before) : 0;
-        const Start st = find_start<NG>(p, len, n, c, lane);
-        if (lane == 0) {
-            start = st;
-            own = n;
+    constexpr int E = D / 32;
+    Joined<D> x;
+    x.m = -INFINITY;
+    x.l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        x.a[e] = 0.f;
+    for (int i0 = first; i0 < count; i0 += 32 * step) {
+        const int i = i0 + lane * step;
+        int64_t at_pair = 0, at_a = 0;
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (i < count && part(i, at_pair, at_a))
+            ml = *reinterpret_cast<const float2 *>(base + at_pair);
+        const bool live = !(ml.x == -INFINITY && ml.y == 0.f);   // else no key: its a is not written
+        float top = ml.x;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1)
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        top = fmaxf(top, x.m);
+        const float f = x.m == -INFINITY && x.l == 0.f ? 0.f : ex2(x.m - top);
+        const float h = live ? ex2(ml.x - top) : 0.f;
+        float l = ml.y * h;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1)
+            l += __shfl_xor_sync(0xffffffffu, l, w);
+        x.m = top;
+        x.l = x.l * f + l;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            x.a[e] *= f;
+        const unsigned any = __ballot_sync(0xffffffffu, live);
+        const int last = 32 - __clz(any);
+        for (int j0 = 0; j0 < last; j0 += 8) {
+            float v[8][E], hj[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t at = __shfl_sync(0xffffffffu, at_a, j0 + j);
+                hj[j] = __shfl_sync(0xffffffffu, h, j0 + j);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    v[j][e] = 0.f;
+                if ((any >> (j0 + j)) & 1) {
+                    if constexpr (E == 4) {
+                        const float4 y = *reinterpret_cast<const float4 *>(base + at + lane * 4);
+                        v[j][0] = y.x, v[j][1] = y.y, v[j][2] = y.z, v[j][3] = y.w;
+                    } else {
+                        const float2 y = *reinterpret_cast<const float2 *>(base + at + lane * 2);
+                        v[j][0] = y.x, v[j][1] = y.y;
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    x.a[e] = fmaf(v[j][e], hj[j], x.a[e]);
         }
     }
-    __syncthreads();
-    const Walk<NG> w(p, len, start);
-    if (w.kt == 0 || w.u >= w.u1)
-        return;
-    const int64_t units = p.kv_len != nullptr ? (int64_t)own : p.units;
+    return x;
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void write_row(const AttnParams &p, const Joined<D> &x, int64_t row, int head,
+                                          int lane)
+{
+    const float inv = x.l > 0.f ? 1.f / x.l : (x.l == 0.f ? 0.f : x.l);
+    uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<T *>(p.o) + row * p.o_stride + head * D +
+                                               lane * (D / 32));
+#pragma unroll
+    for (int i = 0; i < D / 32; i += 2)
+        o[i / 2] = Elem<T>::pack(x.a[i] * inv, x.a[i + 1] * inv);
+    if (p.lse != nullptr && lane == 0)
+        p.lse[row * p.n_heads + head] = x.l == 0.f ? -INFINITY : kLn2 * (x.m + log2f(x.l));
+}
+
+// the warps of a row join their sums and the first of them writes the row (all threads of the block
+// call this; `on`: the row exists)
+template <typename T, int D>
+__device__ __forceinline__ void finish_row(const AttnParams &p, Joined<D> x, int per_row, int warp,
+                                           int lane, bool on, int64_t row, int head)
+{
+    __shared__ float sums[kMergeWarps][D + 2];
+    constexpr int E = D / 32;
+    if (per_row > 1) {
+        float *const own = sums[warp];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            own[lane * E + e] = x.a[e];
+        if (lane == 0) {
+            own[D] = x.m;
+            own[D + 1] = x.l;
+        }
+        __syncthreads();
+        if (warp % per_row == 0) {
+            float top = x.m;
+            for (int w = 1; w < per_row; ++w)
+                top = fmaxf(top, sums[warp + w][D]);
+            float l = 0.f, a[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                a[e] = 0.f;
+            for (int w = 0; w < per_row; ++w) {
+                const float *const from = sums[warp + w];
+                if (from[D] == -INFINITY && from[D + 1] == 0.f)
+                    continue;
+                const float h = ex2(from[D] - top);
+                l += from[D + 1] * h;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    a[e] = fmaf(from[lane * E + e], h, a[e]);
+            }
+            x.m = top;
+            x.l = l;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                x.a[e] = a[e];
+        }
+        __syncthreads();
+    }
+    if (on && warp % per_row == 0)
+        write_row<T, D>(p, x, row, head, lane);
+}
+
+// prefill: block (x, y) takes the x-th item that is split between CTAs
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, int per_row)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Walk<NG> w(p, nullptr, find_start<NG>(p, nullptr, 0, p.split_at[blockIdx.x], lane));
     const int64_t u0 = w.u - w.kt, u1 = u0 + w.tiles();    // the item's units
-    const int c0 = cta_of(units, p.ctas, u0), c1 = cta_of(units, p.ctas, u1 - 1);
-    if (c0 != cta_of(units, p.ctas, w.u - 1))
-        return;
-    const int rows = slot_rows<NG>(p);
-    const int64_t size = slot_floats<D>(rows);
-    const int all = w.rows();
-    for (int r = blockIdx.y * kMergeWarps + warp; r < rows; r += gridDim.y * kMergeWarps) {
-        const int rr = w.rt * 128 * NG + r;
-        if (rr >= all)
-            break;
-        Joined<D> x;
-        x.add(p.part + (2 * c0 + 1) * size, rows, r, lane);
-        for (int i = c; i <= c1; ++i)
-            if (has_units(units, p.ctas, i))
-                x.add(p.part + 2 * i * size, rows, r, lane);
-        const int t = rr / p.group;
-        x.template write<T>(p, p.kv_len != nullptr ? w.b : (int64_t)p.row0[w.b] + t,
-                            w.kvh * p.group + rr - t * p.group, lane);
+    const int c0 = cta_of(p.units, p.ctas, u0), c1 = cta_of(p.units, p.ctas, u1 - 1);
+    const int64_t size = slot_floats<D>(128 * NG);
+    const int all = w.rows() - w.rt * 128 * NG;
+    const int rows = all < 128 * NG ? all : 128 * NG;
+    const int some = kMergeWarps / per_row;                // rows at a time
+    pdl_wait_and_release();
+    for (int r0 = blockIdx.y * some; r0 < rows; r0 += gridDim.y * some) {
+        const int r = r0 + warp / per_row;
+        const bool on = r < rows;
+        const Joined<D> x =
+            join_parts<D>(p.part, on ? c1 - c0 + 1 : 0, warp % per_row, per_row, lane,
+                          [&](int i, int64_t &at_pair, int64_t &at_a) {
+                              const int64_t slot = (i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * size;
+                              at_pair = slot + 2 * r;
+                              at_a = slot + pairs_floats(128 * NG) + (int64_t)r * D;
+                              return true;
+                          });
+        const int rr = w.rt * 128 * NG + (on ? r : 0), t = rr / p.group;
+        finish_row<T, D>(p, x, per_row, warp, lane, on, (int64_t)p.row0[w.b] + t,
+                         w.kvh * p.group + rr - t * p.group);
     }
 }
 
-// behind a shared prefix: block (request, KV head), a warp per head
+// decode: block (request and KV head, y); with a shared prefix its parts first
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-attn_merge_shared_kernel(const __grid_constant__ AttnParams p)
+attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
 {
     __shared__ int32_t len[HS_MAX_BATCH];
     __shared__ int sums[2];
-    pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int b = blockIdx.x / p.n_kv, kvh = blockIdx.x - b * p.n_kv;
+    // the lengths may be read before the wait: the kernel in front, which has waited itself, only
+    // reads them
     if (warp == 0) {
         int before = 0;
         const int n = read_lengths(p, len, lane, false, b, &before);
@@ -1067,30 +1187,47 @@ attn_merge_shared_kernel(const __grid_constant__ AttnParams p)
         }
     }
     __syncthreads();
-    if (len[b] < 0)
-        return;
     const int per = tiles_of(p.prefix_len), own = len[b] > 0 ? tiles_of(len[b]) : 1;
     const int64_t pre = (int64_t)per * p.n_kv * row_tiles<NG>(p.batch * p.group);
     const int64_t units = pre + sums[1];
     const int64_t u0 = pre + sums[0] + (int64_t)kvh * own;
     const int item = b * p.n_kv + kvh;
+    const bool skip = len[b] < 0;
     // an unsplit item belongs to the CTA in whose run it begins
-    const int c0 = cta_of(units, p.ctas, u0);
-    const int c1 = p.unsplit ? c0 : cta_of(units, p.ctas, u0 + own - 1);
-    const float *const own_at = p.part + prefix_part_floats<D, NG>(p);
-    for (int h = warp; h < p.group; h += kMergeWarps) {
+    const int c0 = skip ? 0 : cta_of(units, p.ctas, u0);
+    const int c1 = skip || p.unsplit ? c0 : cta_of(units, p.ctas, u0 + own - 1);
+    pdl_wait_and_release();
+    if (skip || (per == 0 && c0 == c1))
+        return;
+    const int64_t own_at = per > 0 ? prefix_part_floats<D, NG>(p) : 0, size = slot_floats<D>(p.group);
+    const int64_t pre_size = slot_floats<D>(128 * NG);
+    const int some = kMergeWarps / per_row;
+    for (int h0 = blockIdx.y * some; h0 < p.group; h0 += gridDim.y * some) {
+        const int h = h0 + warp / per_row;
+        const bool on = h < p.group;
         const int rr = b * p.group + h, rt = rr / (128 * NG), r = rr - rt * 128 * NG;
         const int pitem = rt * p.n_kv + kvh;
-        const int p0 = cta_of(units, p.ctas, (int64_t)pitem * per);
-        const int p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (int64_t)(pitem + 1) * per - 1);
-        Joined<D> x;
-        for (int c = p0; c <= p1; ++c)
-            if (has_units(units, p.ctas, c))
-                x.add(p.part + (pitem + c) * slot_floats<D>(128 * NG), 128 * NG, r, lane);
-        for (int c = c0; c <= c1; ++c)
-            if (has_units(units, p.ctas, c))
-                x.add(own_at + (item + c) * slot_floats<D>(p.group), p.group, h, lane);
-        x.template write<T>(p, b, kvh * p.group + h, lane);
+        int p0 = 0, p1 = -1;
+        if (on && per > 0) {
+            p0 = cta_of(units, p.ctas, (int64_t)pitem * per);
+            p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (int64_t)(pitem + 1) * per - 1);
+        }
+        const int n = p1 - p0 + 1;
+        const Joined<D> x = join_parts<D>(
+            p.part, on ? n + c1 - c0 + 1 : 0, warp % per_row, per_row, lane,
+            [&](int i, int64_t &at_pair, int64_t &at_a) {
+                const bool pre_part = i < n;
+                const int c = pre_part ? p0 + i : c0 + i - n;
+                const int64_t slot =
+                    pre_part ? (pitem + c) * pre_size
+                    : per > 0 ? own_at + (item + c) * size
+                              : (int64_t)(c == c0 ? 2 * c + 1 : 2 * c) * size;
+                const int row = pre_part ? r : h;
+                at_pair = slot + 2 * row;
+                at_a = slot + pairs_floats(pre_part ? 128 * NG : p.group) + (int64_t)row * D;
+                return has_units(units, p.ctas, c);
+            });
+        finish_row<T, D>(p, x, per_row, warp, lane, on, b, kvh * p.group + h);
     }
 }
 
@@ -1150,17 +1287,29 @@ int groups_of(const AttnParams &p)
     return p.prefix_len > 0 && p.batch * p.group > 128 ? 2 : 1;
 }
 
+// most parts of an item of `tiles` key tiles
+int parts_of(int64_t tiles, int64_t units, int ctas)
+{
+    return (int)(tiles / (units / ctas > 0 ? units / ctas : 1)) + 2;
+}
+
 template <int NG>
 void plan_prefill(AttnParams &p, int most)
 {
     int64_t units = 0;
+    int longest = 0;
     for (int b = 0; b < p.batch; ++b)
-        for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group); ++rt)
-            units += (int64_t)p.n_kv * prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
+        for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group); ++rt) {
+            const int n = prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
+            units += (int64_t)p.n_kv * n;
+            longest = n > longest ? n : longest;
+        }
     p.units = units;
     p.ctas = (int)(units < most ? units : most);
+    p.parts = parts_of(longest, units, p.ctas);
     int c = 0;
-    int64_t u = 0;
+    int64_t u = 0, split = -1;
+    p.n_split = 0;
     for (int b = 0; b < p.batch && c < p.ctas; ++b)
         for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group) && c < p.ctas; ++rt) {
             const int n = prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
@@ -1169,6 +1318,11 @@ void plan_prefill(AttnParams &p, int most)
                 p.start_b[c] = (int16_t)b;
                 p.start_item[c] = rt * p.n_kv + (int)(v / n);
                 p.start_kt[c] = (int)(v % n);
+                // the first run that begins inside an item names it for the join
+                if (p.start_kt[c] != 0 && v / n * n + u != split) {
+                    split = v / n * n + u;
+                    p.split_at[p.n_split++] = (int16_t)c;
+                }
             }
             u += (int64_t)n * p.n_kv;
         }
@@ -1184,17 +1338,19 @@ cudaError_t launch(const AttnParams &p, cudaStream_t s)
     cudaError_t e = launch_pdl_big_smem(attn_kernel<T, D, NG>, dim3((unsigned)p.ctas),
                                         dim3(Cfg<D, NG>::kThreads), smem_bytes<D, NG>(), s, smem_set, p,
                                         map);
-    if (e != cudaSuccess)
+    if (e != cudaSuccess || !p.joined)
         return e;
-    if (p.prefix_len > 0)
-        return launch_pdl(attn_merge_shared_kernel<T, D, NG>, dim3((unsigned)(p.batch * p.n_kv)),
-                          dim3(kMergeWarps * 32), 0, s, p);
-    if (p.unsplit || p.ctas == 1)
-        return cudaSuccess;
+    // warps to a row: about eight parts each
+    int per_row = 1;
+    while (per_row < kMergeWarps && per_row * 8 < p.parts)
+        per_row *= 2;
     const int rows = slot_rows<NG>(p);
-    const int blocks = (rows + kMergeWarps - 1) / kMergeWarps;
-    return launch_pdl(attn_merge_kernel<T, D, NG>, dim3((unsigned)(p.ctas - 1), (unsigned)(blocks < 8 ? blocks : 8)),
-                      dim3(kMergeWarps * 32), 0, s, p);
+    const unsigned y = (unsigned)((rows * per_row + kMergeWarps - 1) / kMergeWarps);
+    if (p.kv_len != nullptr)
+        return launch_pdl(attn_merge_decode_kernel<T, D, NG>, dim3((unsigned)(p.batch * p.n_kv), y),
+                          dim3(kMergeWarps * 32), 0, s, p, per_row);
+    return launch_pdl(attn_merge_prefill_kernel<T, D, NG>, dim3((unsigned)p.n_split, y),
+                      dim3(kMergeWarps * 32), 0, s, p, per_row);
 }
 
 template <typename T>
@@ -1221,16 +1377,20 @@ int64_t plan_attn(AttnParams &p, int d, int sm_count)
             plan_prefill<2>(p, most);
         else
             plan_prefill<1>(p, most);
-        return p.unsplit || p.ctas == 1 ? 0 : 2 * p.ctas * slot(128 * ng);
+        p.joined = !p.unsplit && p.n_split > 0;
+        return p.joined ? 2 * p.ctas * slot(128 * ng) : 0;
     }
     const int64_t own = (int64_t)p.batch * p.n_kv * (p.max_kv > 0 ? tiles_of(p.max_kv) : 1);
     const int64_t items = (ng == 2 ? row_tiles<2>(p.batch * p.group) : row_tiles<1>(p.batch * p.group)) *
                           (int64_t)p.n_kv;
     const int64_t units = own + items * tiles_of(p.prefix_len);
     p.ctas = (int)(units < most ? units : most);
+    const int longest = p.max_kv > p.prefix_len ? p.max_kv : p.prefix_len;
+    p.parts = parts_of(tiles_of(longest), units, p.ctas);
+    p.joined = p.prefix_len > 0 || (!p.unsplit && p.ctas > 1 && tiles_of(p.max_kv) > 1);
     if (p.prefix_len > 0)
         return (items + p.ctas) * slot(128 * ng) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
-    return p.unsplit || p.ctas == 1 ? 0 : 2 * p.ctas * slot(p.group);
+    return p.joined ? 2 * p.ctas * slot(p.group) : 0;
 }
 
 cudaError_t launch_attn(const AttnParams &p, int d, int dtype, cudaStream_t s)

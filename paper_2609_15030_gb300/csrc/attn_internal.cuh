@@ -34,6 +34,8 @@ struct AttnParams {
     int32_t prefix_len;
     int32_t unsplit;
     int32_t ctas;
+    int32_t parts;                // about the most CTAs that share an item
+    int32_t joined;               // partial results are left and joined
     float scale_log2;             // scale * log2(e)
     // prefill only: the requests, and where each CTA's share of the tiles begins
     int32_t pos0[HS_MAX_BATCH];
@@ -42,6 +44,8 @@ struct AttnParams {
     int32_t start_item[kAttnMaxCtas];   // row tile * n_kv + KV head of the request
     int32_t start_kt[kAttnMaxCtas];
     int16_t start_b[kAttnMaxCtas];
+    int16_t split_at[kAttnMaxCtas];     // CTAs whose run is the first to begin inside an item
+    int32_t n_split;
 };
 
 // Fills in the schedule (units, ctas, start_*) and says how many bytes of workspace it takes.
