@@ -16,11 +16,11 @@
 // keys fall to several CTAs leaves (m, l, a) of each in the workspace and attn_merge_kernel joins
 // them.  With `unsplit` a CTA takes the whole items that begin in its run.
 //
-// Warps.  Per tile of rows one group of four softmax warps (thread = row = TMEM lane), then one
-// warp that issues the MMAs, one that loads keys and values by TMA, two that look after values at
+// Warps.  Per tile of rows one group of four softmax warps (thread = row = TMEM lane) and a warp that
+// issues its MMAs; one warp that loads keys and values by TMA; the others look after values at
 // masked places.  Per key tile and group: S = Q K^T into TMEM; the group reads it, writes the
-// weights over it as 16-bit pairs; O += P V with P as the TMEM operand.  With two groups the
-// tensor core works on one while the other is in its softmax.
+// weights over it as 16-bit pairs, half of them at a time; O += P V with P as the TMEM operand.  With
+// two groups the tensor core works on one while the other is in its softmax.
 //
 // Values at masked places.  A weight of zero times a NaN or an infinity is NaN, so v must be finite
 // wherever some row of the tile does not attend: rows behind the last key are zeroed in shared
@@ -57,20 +57,20 @@ struct Cfg {
     // is free of the tile kStages / 2 before; the MMAs of that tile's segment began after both
     // groups had left the segment before the one before it
     static constexpr int kMarks = kStages <= 5 ? 4 : 8;
-    static constexpr int kSoftmax = NG * 4;                // warps
+    static constexpr int kSoftmax = NG * 4;               // warps
     static constexpr int kThreads = (kSoftmax + 4) * 32;
     // registers of a softmax thread and of another one, out of those of the launch (65,536 over the
-    // resident threads, a multiple of 8): 256 x 224 + 128 x 56 = 384 x 168 and
-    // 128 x 200 + 128 x 56 = 256 x 128
+    // resident threads, a multiple of 8): 256 x 216 + 128 x 72 = 384 x 168 and
+    // 128 x 184 + 128 x 72 = 256 x 128
     static constexpr int kRegs = NG == 2 ? 168 : 128;
-    static constexpr int kMoreRegs = NG == 2 ? 224 : 200, kLessRegs = 56;
+    static constexpr int kMoreRegs = NG == 2 ? 216 : 184, kLessRegs = 72;
     static_assert(kSoftmax * 32 * kMoreRegs + 128 * kLessRegs <= kThreads * kRegs, "");
     static constexpr int kTmemCols = NG == 2 ? 512 : 256;  // S and O of each group, 128 columns each
 };
 
 // where a CTA's run of units begins and ends
 struct Start {
-    int64_t u, u1;
+    int32_t u, left;                     // its first unit and how many
     int32_t b, rt, kvh, kt;
 };
 
@@ -79,8 +79,9 @@ template <int D, int NG>
 struct Smem {
     uint64_t full[8], empty[8];          // a stage may be read / its MMAs are done
     uint64_t raw[8];                     // a value tile with masked places has landed
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
-    uint64_t drain;
+    uint64_t q_full[2], s_full[2], o_full[2];
+    uint64_t p_full[2][2];               // of each half of the weights
+    uint64_t drain[2];
     uint32_t tmem;
     int32_t abort;
     Start start;
@@ -109,18 +110,23 @@ __host__ __device__ __forceinline__ int tiles_of(int keys)
     return (keys + kKeys - 1) / kKeys;
 }
 
-__host__ __device__ __forceinline__ int64_t first_unit(int64_t units, int ctas, int c)
+// the first unit of CTA c's run (c <= 320; small numbers without the slow division)
+__host__ __device__ __forceinline__ int first_unit(int units, int ctas, int c)
 {
-    return units * c / ctas;
+    if (units < 1 << 22)
+        return (int)((uint32_t)units * (uint32_t)c / (uint32_t)ctas);
+    return (int)((int64_t)units * c / ctas);
 }
 
 // the CTA that has unit u: the largest c with first_unit(c) <= u
-__device__ __forceinline__ int cta_of(int64_t units, int ctas, int64_t u)
+__device__ __forceinline__ int cta_of(int units, int ctas, int u)
 {
-    return (int)(((u + 1) * ctas - 1) / units);
+    if (units < 1 << 22)
+        return (int)(((uint32_t)(u + 1) * (uint32_t)ctas - 1) / (uint32_t)units);
+    return (int)((((int64_t)u + 1) * ctas - 1) / units);
 }
 
-__device__ __forceinline__ bool has_units(int64_t units, int ctas, int c)
+__device__ __forceinline__ bool has_units(int units, int ctas, int c)
 {
     return first_unit(units, ctas, c) < first_unit(units, ctas, c + 1);
 }
@@ -152,7 +158,7 @@ template <int NG>
 struct Walk {
     const AttnParams &p;
     const int32_t *len;
-    int64_t u, u1;
+    int left;                            // units of the run not yet given out
     int b, rt, kvh, kt;
 
     __device__ int rows() const
@@ -185,21 +191,21 @@ struct Walk {
         while (b < p.batch && skip());
     }
     __device__ Walk(const AttnParams &params, const int32_t *lens, const Start &s)
-        : p(params), len(lens), u(s.u), u1(s.u1), b(s.b), rt(s.rt), kvh(s.kvh), kt(s.kt)
+        : p(params), len(lens), left(s.left), b(s.b), rt(s.rt), kvh(s.kvh), kt(s.kt)
     {
-        if (p.unsplit && u < u1 && kt != 0) {         // begins with the next whole item
-            u += tiles() - kt;
+        if (p.unsplit && left > 0 && kt != 0) {       // begins with the next whole item
+            left -= tiles() - kt;
             next_item();
         }
     }
     __device__ bool next(Segment &s)
     {
-        if (u >= u1)
+        if (left <= 0)
             return false;
         const int n = tiles();
         int take = n - kt;
-        if (!p.unsplit && take > u1 - u)
-            take = (int)(u1 - u);
+        if (!p.unsplit && take > left)
+            take = left;
         s.b = b;
         s.rt = rt;
         s.kvh = kvh;
@@ -208,7 +214,7 @@ struct Walk {
         s.rows = rows();
         s.whole = kt == 0 && take == n;
         s.item = (b < 0 ? rt : b) * p.n_kv + kvh;
-        u += take;
+        left -= take;
         kt += take;
         if (kt == n)
             next_item();
@@ -303,7 +309,7 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *
     Start s;
     if (p.kv_len == nullptr) {
         s.u = first_unit(p.units, p.ctas, c);
-        s.u1 = first_unit(p.units, p.ctas, c + 1);
+        s.left = first_unit(p.units, p.ctas, c + 1) - s.u;
         s.b = p.start_b[c];
         s.rt = p.start_item[c] / p.n_kv;
         s.kvh = p.start_item[c] - s.rt * p.n_kv;
@@ -312,19 +318,19 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *
     }
     const int per = tiles_of(p.prefix_len);
     const int pre = per * p.n_kv * row_tiles<NG>(p.batch * p.group);
-    const int64_t units = (int64_t)pre + own;
+    const int units = pre + own;
     s.u = first_unit(units, p.ctas, c);
-    s.u1 = first_unit(units, p.ctas, c + 1);
+    s.left = first_unit(units, p.ctas, c + 1) - s.u;
     s.b = -1;
     s.rt = s.kvh = s.kt = 0;
     if (s.u < pre) {
-        const int item = (int)s.u / per;
-        s.kt = (int)s.u - item * per;
+        const int item = s.u / per;
+        s.kt = s.u - item * per;
         s.rt = item / p.n_kv;
         s.kvh = item - s.rt * p.n_kv;
         return s;
     }
-    int v = (int)(s.u - pre);                 // the request with unit v of all requests'
+    int v = s.u - pre;                 // the request with unit v of all requests'
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
         const int b = b0 + lane;
         const int x = own_units(p, b < p.batch ? len[b] : -1);
@@ -342,12 +348,13 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *
         }
         v -= last;
     }
-    return s;                                 // no unit is left: s.u == s.u1
+    return s;                                 // no unit is left
 }
 
 // ---- partial results -----------------------------------------------------------------------
 //
-// A slot holds R rows: R pairs (m, l), padded to 16 bytes, then R rows of D floats a.  Without a shared prefix an item
+// A slot holds R rows: R pairs (m, l), padded to 16 bytes, then the sums a: of decode R rows of D
+// floats, of prefill D columns of R (a warp stores 32 rows of a column, and the join reads them so).  Without a shared prefix an item
 // leaves a partial result in at most two places of a CTA's run: at its beginning, where it does not
 // start the item (slot 2 cta), and at its end, where it does (slot 2 cta + 1).  Behind a shared
 // prefix every segment is partial; its slot is item + cta, which no other segment of its part
@@ -424,6 +431,13 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t x)
     return ((x & Elem<T>::kExp) + Elem<T>::kOne) & 0x80008000u;
 }
 
+__device__ __forceinline__ float max3(float x, float y, float z)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
+}
+
 __device__ __forceinline__ float ex2(float x)
 {
     float r;
@@ -466,25 +480,28 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     if (tid == 0) {
         for (int i = 0; i < kSt; ++i) {
             mbar_init(full(i), 1);
-            mbar_init(empty(i), 1);
+            mbar_init(empty(i), NG);
             mbar_init(smem_u32(&sm.raw[i]), 1);
         }
         for (int g = 0; g < NG; ++g) {
             mbar_init(smem_u32(&sm.q_full[g]), 128);
             mbar_init(smem_u32(&sm.s_full[g]), 1);
-            mbar_init(smem_u32(&sm.p_full[g]), 128);
+            mbar_init(smem_u32(&sm.p_full[g][0]), 128);
+            mbar_init(smem_u32(&sm.p_full[g][1]), 128);
             mbar_init(smem_u32(&sm.o_full[g]), 1);
+            mbar_init(smem_u32(&sm.drain[g]), 1);
         }
-        mbar_init(smem_u32(&sm.drain), 1);
-        fence_mbar_init();
+                fence_mbar_init();
         sm.abort = 0;
     }
+    if (warp == C::kSoftmax + 3 && lane == 0)
+        prefetch_tensormap(&map);
     if (warp == C::kSoftmax)
         tmem_alloc(smem_u32(&sm.tmem), C::kTmemCols);
     pdl_wait();
     if (p.joined)
         pdl_release();     // the join takes its place as CTAs end
-    if (warp == C::kSoftmax + 1) {
+    if (warp == C::kSoftmax + 3) {
         int before = 0;
         const int own = p.kv_len != nullptr ? read_lengths(p, sm.len, lane, cta == 0, 0, &before) : 0;
         const Start st = find_start<NG>(p, sm.len, own, cta, lane);
@@ -500,7 +517,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
 
     if (warp >= C::kSoftmax) {
     fewer_registers<C::kLessRegs>();
-    if (warp == C::kSoftmax + 1) {
+    if (warp == C::kSoftmax + 3) {
         // ---- loads: key and value tiles in turn through the stages
         const int per = p.page_shift >= 7 ? 1 : kKeys >> p.page_shift;      // pages of a tile
         const int box = p.page_shift >= 7 ? kKeys : 1 << p.page_shift;      // keys of a copy
@@ -567,121 +584,136 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                     mbar_wait_bounded(full(st), (i / kSt) & 1, kTimeoutNs);
             }
         }
-    } else if (warp == C::kSoftmax) {
-        // ---- MMAs.  Per group the order QK(0), PV(0), QK(1), PV(1), ...: the scores of the next
-        // tile overwrite the weights of the last one behind the product that reads them
-        uint32_t n = 0;                  // key tiles done: tile i is in stages 2 i and 2 i + 1
-        uint32_t ph_q = 0, ph_p[2] = {0, 0};
+    } else if (warp < C::kSoftmax + NG) {
+        // ---- MMAs, a warp to a group, in the order QK(0), PV(0), QK(1), PV(1), ...: the scores of the
+        // next tile overwrite the weights of the last one behind the product that reads them.  A stage
+        // is free once both groups are done with it
+        const int g = warp - C::kSoftmax;
+        const uint32_t s_at = tmem + g * 256, o_at = s_at + 128;
+        const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
+        const uint32_t bar_p = smem_u32(&sm.p_full[g][0]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint64_t q_desc = sdesc_sw128(q_at + g * C::kTile, 16, 1024);
+        const uint64_t k_desc = sdesc_sw128(st_at, 16, kHalf * 1024);
+        const uint64_t v_desc = sdesc_sw128(st_at, 1024, kHalf * 1024);
+        uint32_t st = 0, ph = 0;         // the stage at hand and the phase of its use
+        auto next_stage = [&]() {
+            if (++st == kSt) {
+                st = 0;
+                ph ^= 1;
+            }
+        };
+        auto qk = [&]() {                // the scores of the tile at hand; its stage is free behind them
+            if (elect_one()) {
+                const uint64_t b = k_desc + st * (C::kTile / 16);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_f16_ss(s_at, q_desc + ((k >> 2) * 16384 + (k & 3) * 32) / 16,
+                               b + ((k >> 2) * 1024 + (k & 3) * 32) / 16, Elem<T>::idesc(kKeys, 0), k > 0);
+                tc_commit(bar_s);
+                tc_commit(empty(st));
+            }
+            __syncwarp();
+        };
+        auto pass = [&]() -> bool {      // a stage that this group has no use for
+            if (!wait(full(st), ph))
+                return false;
+            if (lane == 0)
+                mbar_arrive(empty(st));
+            __syncwarp();
+            next_stage();
+            return true;
+        };
+        uint32_t ph_q = 0, ph_p = 0;
         bool go = true;
         while (go && walk.next(s)) {
-            int keys[2] = {0, 0}, cnt[2] = {0, 0};
-            for (int g = 0; g < NG; ++g) {
-                keys[g] = group_keys<NG>(p, sm.len, s, g);
-                cnt[g] = group_tiles(s, keys[g]);
+            const int keys = group_keys<NG>(p, sm.len, s, g);
+            const int mine = group_tiles(s, keys);
+            int most = mine;
+            if (NG == 2) {
+                const int other = group_tiles(s, group_keys<NG>(p, sm.len, s, 1 - g));
+                most = other > most ? other : most;
             }
-            const int most = cnt[1] > cnt[0] ? cnt[1] : cnt[0];
-            auto qk = [&](int g, uint32_t tile) {
-                const uint32_t k_at = st_at + (2 * tile % kSt) * C::kTile;
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        mma_f16_ss(tmem + g * 256,
-                                   sdesc_sw128(q_at + g * C::kTile + (k >> 2) * 16384 + (k & 3) * 32, 16,
-                                               1024),
-                                   sdesc_sw128(k_at + (k >> 2) * 1024 + (k & 3) * 32, 16, kHalf * 1024),
-                                   Elem<T>::idesc(kKeys, 0), k > 0);
-                    tc_commit(smem_u32(&sm.s_full[g]));
+            if (mine > 0) {
+                go = wait(bar_q, ph_q) && wait(full(st), ph);
+                ph_q ^= 1;
+                if (!go)
+                    break;
+                tc_fence_after();
+                qk();
+                next_stage();
+            } else if (most > 0) {
+                go = pass();
+            }
+            int left = keys - s.kt0 * kKeys;
+            for (int j = 0; j < most && go; ++j, left -= kKeys) {
+                if (j >= mine) {
+                    go = pass() && (j + 1 == most || pass());
+                    continue;
                 }
-                __syncwarp();
-            };
-            for (int j = 0; j < most && go; ++j, ++n) {
-                if (j == 0) {
-                    for (int g = 0; g < NG && go; ++g) {
-                        if (cnt[g] == 0)
-                            continue;
-                        go = wait(smem_u32(&sm.q_full[g]), (ph_q >> g) & 1);
-                        ph_q ^= 1u << g;
-                    }
-                    go = go && wait(full(2 * n % kSt), (2 * n / kSt) & 1);
+                const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
+                const uint32_t v_st = st, v_ph = ph;
+                next_stage();
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    go = go && wait(bar_p + 8 * h, ph_p) && (h == 1 || wait(full(v_st), v_ph));
                     if (!go)
                         break;
                     tc_fence_after();
-                    for (int g = 0; g < NG; ++g)
-                        if (cnt[g] > 0)
-                            qk(g, n);
-                    if (elect_one())
-                        tc_commit(empty(2 * n % kSt));
+                    if (elect_one()) {
+                        const uint64_t b = v_desc + v_st * (C::kTile / 16);
+#pragma unroll
+                        for (int k = h * 4; k < h * 4 + 4; ++k)
+                            if (k < steps)
+                                mma_f16_ts(o_at, s_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
+                                           Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
+                        if (h == 1) {
+                            if (j + 1 == mine)
+                                tc_commit(bar_o);
+                            tc_commit(empty(v_st));
+                        }
+                    }
                     __syncwarp();
                 }
-                const uint32_t v_st = (2 * n + 1) % kSt;
-                const uint32_t v_at = st_at + v_st * C::kTile;
-                bool v_here = false, k_here = false;
-                for (int g = 0; g < NG && go; ++g) {
-                    if (j < cnt[g]) {
-                        go = wait(smem_u32(&sm.p_full[g]), ph_p[g]);
-                        ph_p[g] ^= 1;
-                        if (go && !v_here) {
-                            go = wait(full(v_st), ((2 * n + 1) / kSt) & 1);
-                            v_here = true;
-                        }
-                        if (!go)
-                            break;
-                        tc_fence_after();
-                        const int left = keys[g] - (s.kt0 + j) * kKeys;
-                        const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
-                        if (elect_one()) {
-                            for (int k = 0; k < steps; ++k)
-                                mma_f16_ts(tmem + g * 256 + 128, tmem + g * 256 + k * 8,
-                                           sdesc_sw128(v_at + k * 2 * kHalf * 1024, 1024, kHalf * 1024),
-                                           Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
-                            if (j + 1 == cnt[g])
-                                tc_commit(smem_u32(&sm.o_full[g]));
-                        }
-                        __syncwarp();
-                    }
-                    if (j + 1 < cnt[g]) {
-                        if (!k_here) {
-                            go = wait(full((2 * n + 2) % kSt), ((2 * n + 2) / kSt) & 1);
-                            k_here = true;
-                        }
-                        if (!go)
-                            break;
-                        tc_fence_after();
-                        qk(g, n + 1);
-                    }
+                ph_p ^= 1;
+                if (!go)
+                    break;
+                if (j + 1 < mine) {
+                    go = wait(full(st), ph);
+                    if (!go)
+                        break;
+                    tc_fence_after();
+                    qk();
+                    next_stage();
+                } else if (j + 1 < most) {
+                    go = pass();
                 }
-                if (go && elect_one()) {
-                    tc_commit(empty(v_st));
-                    if (k_here)
-                        tc_commit(empty((2 * n + 2) % kSt));
-                }
-                __syncwarp();
             }
         }
         if (*abort != 0) {
             // the MMAs in flight end (bounded) before their memory goes away
             if (elect_one()) {
-                tc_commit(smem_u32(&sm.drain));
-                mbar_wait_bounded(smem_u32(&sm.drain), 0, kTimeoutNs);
+                tc_commit(smem_u32(&sm.drain[g]));
+                mbar_wait_bounded(smem_u32(&sm.drain[g]), 0, kTimeoutNs);
             }
             __syncwarp();
         }
     } else {
-        // ---- values at masked places, two warps
+        // ---- values at masked places: the warps that are left
+        constexpr int kWho = (3 - NG) * 32;
         uint32_t n = 0, seg = 0, ph_raw = 0;
-        const int who = tid - (C::kSoftmax + 2) * 32;
+        const int who = tid - (C::kSoftmax + NG) * 32;
         auto pair_and = [](bool x) {
             int r;
             asm volatile("{\n\t.reg .pred p, q;\n\t"
                          "setp.ne.s32 p, %1, 0;\n\t"
-                         "bar.red.and.pred q, 1, 64, p;\n\t"
+                         "bar.red.and.pred q, 1, %2, p;\n\t"
                          "selp.s32 %0, 1, 0, q;\n\t}"
                          : "=r"(r)
-                         : "r"((int)x)
+                         : "r"((int)x), "n"(kWho)
                          : "memory");
             return r != 0;
         };
-        auto pair_sync = [] { asm volatile("bar.sync 1, 64;" ::: "memory"); };
+        auto pair_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWho) : "memory"); };
         bool go = true;
         for (; go && walk.next(s); ++seg) {
             int all = group_keys<NG>(p, sm.len, s, NG - 1);
@@ -696,7 +728,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 if (k0 + kKeys <= common)
                     continue;
                 if (!clean) {
-                    for (int i = who; i < D; i += 64)
+                    for (int i = who; i < D; i += kWho)
                         from[i] = INT_MAX;
                     if (who == 0)
                         *any = 0;
@@ -706,7 +738,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 const uint32_t st = (2 * n + 1) % kSt;
                 go = wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1);
                 ph_raw ^= 1u << st;
-                // both warps go on or neither: they meet in a plain barrier below
+                // these warps go on or none: they meet in a plain barrier below
                 go = pair_and(go);
                 if (!go)
                     break;
@@ -722,12 +754,12 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                     return reinterpret_cast<uint4 *>(v + ((r >> 3) * kHalf + (x >> 3)) * 1024 +
                                                      (r & 7) * 128 + (((x & 7) ^ (r & 7)) << 4));
                 };
-                for (int i0 = lo * (D / 8) + who; i0 < hi * (D / 8); i0 += 64 * kAhead) {
+                for (int i0 = lo * (D / 8) + who; i0 < hi * (D / 8); i0 += kWho * kAhead) {
                     uint32_t bad = 0;
                     uint4 y[kAhead];
 #pragma unroll
                     for (int k = 0; k < kAhead; ++k) {
-                        const int i = i0 + k * 64;
+                        const int i = i0 + k * kWho;
                         y[k] = i < hi * (D / 8) ? *chunk(i) : make_uint4(0, 0, 0, 0);
                     }
 #pragma unroll
@@ -736,7 +768,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                                not_finite<T>(y[k].w);
                     if (bad == 0)
                         continue;
-                    for (int i = i0; i < hi * (D / 8) && i < i0 + 64 * kAhead; i += 64) {
+                    for (int i = i0; i < hi * (D / 8) && i < i0 + kWho * kAhead; i += kWho) {
                         uint16_t *const e = reinterpret_cast<uint16_t *>(chunk(i));
                         for (int w = 0; w < 8; ++w)
                             if ((not_finite<T>(e[w]) & 0x8000u) != 0) {
@@ -746,7 +778,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                             }
                     }
                 }
-                for (int i = hi * (D / 8) + who; i < end * (D / 8); i += 64)
+                for (int i = hi * (D / 8) + who; i < end * (D / 8); i += kWho)
                     *chunk(i) = make_uint4(0, 0, 0, 0);
                 fence_proxy_async_smem();
                 pair_sync();
@@ -763,7 +795,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + g * 256 + lanes, o_at = s_at + 128;
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
-        const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint32_t bar_p = smem_u32(&sm.p_full[g][0]), bar_o = smem_u32(&sm.o_full[g]);
         uint32_t ph_s = 0, ph_o = 0;
         // this thread's row of a segment: its token row, head and keys
         int64_t row = 0;
@@ -776,7 +808,6 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             head = x.kvh * p.group + (ok ? rr - t * p.group : 0);
             gkeys = group_keys<NG>(p, sm.len, x, g);
             if (x.b < 0) {
-                // prefix: the row of a request whose length is out of bounds is not written
                 row = t;
                 keys = p.prefix_len;
             } else if (p.kv_len != nullptr) {
@@ -797,9 +828,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             for (int i = 0; i < 32; i += kRows) {
                 const int rr = i + lane / kChunks;
                 const int64_t at = __shfl_sync(0xffffffffu, from, rr);
-                const int r8 = rr & 7;
                 cp_async_16(q_at + g * C::kTile + (c >> 3) * 16384 + ((warp & 3) * 32 + rr) * 128 +
-                                (((c & 7) ^ r8) << 4),
+                                (((c & 7) ^ (rr & 7)) << 4),
                             static_cast<const T *>(p.q) + at + c * 8, (real >> rr) & 1);
             }
         };
@@ -819,7 +849,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         for (uint32_t seg = 0; have && go; ++seg) {
             const int tiles = group_tiles(s, gkeys);
             float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
-            for (int j = 0; j < tiles; ++j) {
+            int valid = keys - s.kt0 * kKeys;   // keys of the row from this tile on
+            for (int j = 0; j < tiles; ++j, valid -= kKeys) {
                 go = wait(bar_s, ph_s);
                 ph_s ^= 1;
                 if (!go)
@@ -827,24 +858,26 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 tc_fence_after();
                 float x[kKeys];
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    tmem_ld32(s_at + c * 32, *reinterpret_cast<float(*)[32]>(&x[c * 32]));
+                for (int c = 0; c < kKeys; c += 32)
+                    tmem_ld32(s_at + c, *reinterpret_cast<float(*)[32]>(&x[c]));
                 tmem_wait_ld();
-                const int valid = keys - (s.kt0 + j) * kKeys;
                 if (__any_sync(0xffffffffu, valid < kKeys)) {
 #pragma unroll
                     for (int c = 0; c < kKeys; ++c)
                         x[c] = c < valid ? x[c] : -INFINITY;
                 }
-                float t0 = x[0], t1 = x[1], t2 = x[2], t3 = x[3];
+                float t0 = max3(x[0], x[1], x[2]), t1 = max3(x[3], x[4], x[5]);
+                float t2 = max3(x[6], x[7], x[8]), t3 = max3(x[9], x[10], x[11]);
 #pragma unroll
-                for (int c = 4; c < kKeys; c += 4) {
-                    t0 = fmaxf(t0, x[c]);
-                    t1 = fmaxf(t1, x[c + 1]);
-                    t2 = fmaxf(t2, x[c + 2]);
-                    t3 = fmaxf(t3, x[c + 3]);
+                for (int c = 12; c + 7 < kKeys; c += 8) {
+                    t0 = max3(t0, x[c], x[c + 1]);
+                    t1 = max3(t1, x[c + 2], x[c + 3]);
+                    t2 = max3(t2, x[c + 4], x[c + 5]);
+                    t3 = max3(t3, x[c + 6], x[c + 7]);
                 }
-                const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * p.scale_log2;
+                t0 = max3(t0, x[124], x[125]);
+                t1 = max3(t1, x[126], x[127]);
+                const float top = max3(t0, t1, fmaxf(t2, t3)) * p.scale_log2;
                 const bool up = top > m + kLazy;
                 if (__any_sync(0xffffffffu, up)) {
                     const float f = up ? ex2(m - top) : 1.f;
@@ -854,41 +887,45 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                         // the previous product is done: the scores came after it
                         l *= f;
 #pragma unroll
-                        for (int c = 0; c < D; c += 32) {
-                            float a[32];
-                            tmem_ld32(o_at + c, a);
+                        for (int c = 0; c < D; c += 16) {      // few registers: the scores hold theirs
+                            uint32_t a[16];
+                            tmem_ld16(o_at + c, a);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                a[i] *= f;
-                            tmem_st32(o_at + c, a);
+                            for (int i = 0; i < 16; ++i)
+                                a[i] = __float_as_uint(__uint_as_float(a[i]) * f);
+                            tmem_st16(o_at + c, a);
                         }
                     }
                 }
                 const float shift = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
                 uint64_t l01 = 0, l23 = 0;
+                // the product with the first half of the values runs during the second half here
 #pragma unroll
-                for (int c = 0; c < kKeys; c += 32) {
-                    uint32_t w[16];
+                for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float2 y0 = unpair(fma2(pair(x[c + 2 * i], x[c + 2 * i + 1]), scale2, shift2));
-                        const float2 y1 =
-                            unpair(fma2(pair(x[c + 2 * i + 2], x[c + 2 * i + 3]), scale2, shift2));
-                        const float a0 = ex2(y0.x), a1 = ex2(y0.y), a2 = ex2(y1.x), a3 = ex2(y1.y);
-                        l01 = add2(l01, pair(a0, a1));
-                        l23 = add2(l23, pair(a2, a3));
-                        w[i] = Elem<T>::pack(a0, a1);
-                        w[i + 1] = Elem<T>::pack(a2, a3);
+                    for (int c = h * 64; c < h * 64 + 64; c += 32) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const int e = c + 2 * i;
+                            const float2 y0 = unpair(fma2(pair(x[e], x[e + 1]), scale2, shift2));
+                            const float2 y1 = unpair(fma2(pair(x[e + 2], x[e + 3]), scale2, shift2));
+                            const float a0 = ex2(y0.x), a1 = ex2(y0.y), a2 = ex2(y1.x), a3 = ex2(y1.y);
+                            l01 = add2(l01, pair(a0, a1));
+                            l23 = add2(l23, pair(a2, a3));
+                            w[i] = Elem<T>::pack(a0, a1);
+                            w[i + 1] = Elem<T>::pack(a2, a3);
+                        }
+                        tmem_st16(s_at + c / 2, w);
                     }
-                    tmem_st16(s_at + c / 2, w);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bar_p + 8 * h);
                 }
                 const float2 ls = unpair(add2(l01, l23));
                 l += ls.x + ls.y;
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(bar_p);
             }
             if (!go)
                 break;
@@ -955,9 +992,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 int rows = 0;
                 float *const slot = slot_of<D, NG>(p, was, cta, &rows);
                 const int at = g * 128 + r;
-                if (at < rows && was_ok)
+                const bool put = at < rows && was_ok;
+                if (put)
                     reinterpret_cast<float2 *>(slot)[at] = make_float2(m, l);
-                float *const a_at = slot + pairs_floats(rows) + (int64_t)at * D;
                 if (tiles > 0) {
 #pragma unroll
                     for (int c = 0; c < D; c += 32) {
@@ -969,10 +1006,17 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                             for (int i = 0; i < 32; ++i)
                                 a[i] = was_keys > from[c + i] ? NAN : a[i];
                         }
-                        if (at < rows && was_ok) {
+                        if (put && p.kv_len == nullptr) {
+                            float *const to = slot + pairs_floats(rows) + c * rows + at;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                to[i * rows] = a[i];
+                        } else if (put) {
+                            float *const to =
+                                slot + pairs_floats(rows) + (int64_t)at * D + c;
 #pragma unroll
                             for (int i = 0; i < 32; i += 4)
-                                *reinterpret_cast<float4 *>(a_at + c + i) =
+                                *reinterpret_cast<float4 *>(to + i) =
                                     make_float4(a[i], a[i + 1], a[i + 2], a[i + 3]);
                         }
                     }
@@ -1136,35 +1180,74 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, Joined<D> x, int
         write_row<T, D>(p, x, row, head, lane);
 }
 
-// prefill: block (x, y) takes the x-th item that is split between CTAs
+// prefill: block (x, y, z) takes 32 rows and 32 columns of the x-th item that is split between CTAs,
+// a lane a row and a warp four columns
 template <typename T, int D, int NG>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, int per_row)
+attn_merge_prefill_kernel(const __grid_constant__ AttnParams p)
 {
+    constexpr int R = 128 * NG, kAhead = 8;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Walk<NG> w(p, nullptr, find_start<NG>(p, nullptr, 0, p.split_at[blockIdx.x], lane));
-    const int64_t u0 = w.u - w.kt, u1 = u0 + w.tiles();    // the item's units
+    const Start st = find_start<NG>(p, nullptr, 0, p.split_at[blockIdx.x], lane);
+    const Walk<NG> w(p, nullptr, st);
+    const int u0 = st.u - st.kt, u1 = u0 + w.tiles();      // the item's units
     const int c0 = cta_of(p.units, p.ctas, u0), c1 = cta_of(p.units, p.ctas, u1 - 1);
-    const int64_t size = slot_floats<D>(128 * NG);
-    const int all = w.rows() - w.rt * 128 * NG;
-    const int rows = all < 128 * NG ? all : 128 * NG;
-    const int some = kMergeWarps / per_row;                // rows at a time
+    const int64_t size = slot_floats<D>(R);
+    const int r = blockIdx.y * 32 + lane, rr = w.rt * R + r, col = blockIdx.z * 32 + warp * 4;
+    const bool on = rr < w.rows();
     pdl_wait_and_release();
-    for (int r0 = blockIdx.y * some; r0 < rows; r0 += gridDim.y * some) {
-        const int r = r0 + warp / per_row;
-        const bool on = r < rows;
-        const Joined<D> x =
-            join_parts<D>(p.part, on ? c1 - c0 + 1 : 0, warp % per_row, per_row, lane,
-                          [&](int i, int64_t &at_pair, int64_t &at_a) {
-                              const int64_t slot = (i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * size;
-                              at_pair = slot + 2 * r;
-                              at_a = slot + pairs_floats(128 * NG) + (int64_t)r * D;
-                              return true;
-                          });
-        const int rr = w.rt * 128 * NG + (on ? r : 0), t = rr / p.group;
-        finish_row<T, D>(p, x, per_row, warp, lane, on, (int64_t)p.row0[w.b] + t,
-                         w.kvh * p.group + rr - t * p.group);
+    if (!on)
+        return;
+    // part i of the item: CTA c0's last segment, then the first ones of the CTAs behind it
+    const float *const first = p.part + (2 * c0 + 1) * size, *const rest = p.part + 2 * c0 * size;
+    const int parts = c1 - c0 + 1;
+    float m = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < parts; i0 += kAhead) {
+        float2 ml[kAhead];
+        float v[kAhead][4];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[i][e] = 0.f;
+            if (i0 + i < parts) {
+                const float *const slot = i0 + i == 0 ? first : rest + 2 * (i0 + i) * size;
+                ml[i] = reinterpret_cast<const float2 *>(slot)[r];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[i][e] = slot[pairs_floats(R) + (col + e) * R + r];
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            top = fmaxf(top, ml[i].x);
+        const float f = m == -INFINITY && l == 0.f ? 0.f : ex2(m - top);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            a[e] *= f;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            // a part without a key of this row: what it holds of a means nothing
+            if (ml[i].x == -INFINITY && ml[i].y == 0.f)
+                continue;
+            const float h = ex2(ml[i].x - top);
+            l = fmaf(ml[i].y, h, l);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                a[e] = fmaf(v[i][e], h, a[e]);
+        }
     }
+    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+    const int t = rr / p.group, head = w.kvh * p.group + rr - t * p.group;
+    const int64_t row = (int64_t)p.row0[w.b] + t;
+    *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + row * p.o_stride + head * D + col) =
+        make_uint2(Elem<T>::pack(a[0] * inv, a[1] * inv), Elem<T>::pack(a[2] * inv, a[3] * inv));
+    if (p.lse != nullptr && col == 0)
+        p.lse[row * p.n_heads + head] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
 
 // decode: block (request and KV head, y); with a shared prefix its parts first
@@ -1188,9 +1271,9 @@ attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
     }
     __syncthreads();
     const int per = tiles_of(p.prefix_len), own = len[b] > 0 ? tiles_of(len[b]) : 1;
-    const int64_t pre = (int64_t)per * p.n_kv * row_tiles<NG>(p.batch * p.group);
-    const int64_t units = pre + sums[1];
-    const int64_t u0 = pre + sums[0] + (int64_t)kvh * own;
+    const int pre = per * p.n_kv * row_tiles<NG>(p.batch * p.group);
+    const int units = pre + sums[1];
+    const int u0 = pre + sums[0] + kvh * own;
     const int item = b * p.n_kv + kvh;
     const bool skip = len[b] < 0;
     // an unsplit item belongs to the CTA in whose run it begins
@@ -1209,8 +1292,8 @@ attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
         const int pitem = rt * p.n_kv + kvh;
         int p0 = 0, p1 = -1;
         if (on && per > 0) {
-            p0 = cta_of(units, p.ctas, (int64_t)pitem * per);
-            p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (int64_t)(pitem + 1) * per - 1);
+            p0 = cta_of(units, p.ctas, pitem * per);
+            p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (pitem + 1) * per - 1);
         }
         const int n = p1 - p0 + 1;
         const Joined<D> x = join_parts<D>(
@@ -1294,7 +1377,7 @@ int parts_of(int64_t tiles, int64_t units, int ctas)
 }
 
 template <int NG>
-void plan_prefill(AttnParams &p, int most)
+bool plan_prefill(AttnParams &p, int most)
 {
     int64_t units = 0;
     int longest = 0;
@@ -1304,7 +1387,9 @@ void plan_prefill(AttnParams &p, int most)
             units += (int64_t)p.n_kv * n;
             longest = n > longest ? n : longest;
         }
-    p.units = units;
+    if (units > INT_MAX)
+        return false;
+    p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
     p.parts = parts_of(longest, units, p.ctas);
     int c = 0;
@@ -1313,8 +1398,8 @@ void plan_prefill(AttnParams &p, int most)
     for (int b = 0; b < p.batch && c < p.ctas; ++b)
         for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group) && c < p.ctas; ++rt) {
             const int n = prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
-            for (; c < p.ctas && first_unit(units, p.ctas, c) < u + (int64_t)n * p.n_kv; ++c) {
-                const int64_t v = first_unit(units, p.ctas, c) - u;
+            for (; c < p.ctas && first_unit(p.units, p.ctas, c) < u + (int64_t)n * p.n_kv; ++c) {
+                const int64_t v = first_unit(p.units, p.ctas, c) - u;
                 p.start_b[c] = (int16_t)b;
                 p.start_item[c] = rt * p.n_kv + (int)(v / n);
                 p.start_kt[c] = (int)(v % n);
@@ -1326,6 +1411,7 @@ void plan_prefill(AttnParams &p, int most)
             }
             u += (int64_t)n * p.n_kv;
         }
+    return true;
 }
 
 template <typename T, int D, int NG>
@@ -1340,16 +1426,15 @@ cudaError_t launch(const AttnParams &p, cudaStream_t s)
                                         map);
     if (e != cudaSuccess || !p.joined)
         return e;
+    if (p.kv_len == nullptr)
+        return launch_pdl(attn_merge_prefill_kernel<T, D, NG>,
+                          dim3((unsigned)p.n_split, 128 * NG / 32, D / 32), dim3(kMergeWarps * 32), 0, s, p);
     // warps to a row: about eight parts each
     int per_row = 1;
     while (per_row < kMergeWarps && per_row * 8 < p.parts)
         per_row *= 2;
-    const int rows = slot_rows<NG>(p);
-    const unsigned y = (unsigned)((rows * per_row + kMergeWarps - 1) / kMergeWarps);
-    if (p.kv_len != nullptr)
-        return launch_pdl(attn_merge_decode_kernel<T, D, NG>, dim3((unsigned)(p.batch * p.n_kv), y),
-                          dim3(kMergeWarps * 32), 0, s, p, per_row);
-    return launch_pdl(attn_merge_prefill_kernel<T, D, NG>, dim3((unsigned)p.n_split, y),
+    const unsigned y = (unsigned)((p.group * per_row + kMergeWarps - 1) / kMergeWarps);
+    return launch_pdl(attn_merge_decode_kernel<T, D, NG>, dim3((unsigned)(p.batch * p.n_kv), y),
                       dim3(kMergeWarps * 32), 0, s, p, per_row);
 }
 
@@ -1373,10 +1458,8 @@ int64_t plan_attn(AttnParams &p, int d, int sm_count)
         return (int64_t)sizeof(float) * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows));
     };
     if (p.kv_len == nullptr) {
-        if (ng == 2)
-            plan_prefill<2>(p, most);
-        else
-            plan_prefill<1>(p, most);
+        if (!(ng == 2 ? plan_prefill<2>(p, most) : plan_prefill<1>(p, most)))
+            return -1;
         p.joined = !p.unsplit && p.n_split > 0;
         return p.joined ? 2 * p.ctas * slot(128 * ng) : 0;
     }
@@ -1384,6 +1467,8 @@ int64_t plan_attn(AttnParams &p, int d, int sm_count)
     const int64_t items = (ng == 2 ? row_tiles<2>(p.batch * p.group) : row_tiles<1>(p.batch * p.group)) *
                           (int64_t)p.n_kv;
     const int64_t units = own + items * tiles_of(p.prefix_len);
+    if (units > INT_MAX)
+        return -1;
     p.ctas = (int)(units < most ? units : most);
     const int longest = p.max_kv > p.prefix_len ? p.max_kv : p.prefix_len;
     p.parts = parts_of(tiles_of(longest), units, p.ctas);

@@ -82,9 +82,10 @@ hs_status plan(hs::AttnParams &p, int d, int64_t *bytes)
 {
     int sms = 0;
     const hs_status st = hs::device_sm_count(&sms);
-    if (st == HS_OK)
-        *bytes = hs::plan_attn(p, d, sms);
-    return st;
+    if (st != HS_OK)
+        return st;
+    *bytes = hs::plan_attn(p, d, sms);
+    return *bytes < 0 ? HS_ERR_UNSUPPORTED : HS_OK;
 }
 
 hs_status run(hs::AttnParams &p, const hs_attn_shape &s, void *workspace, int64_t workspace_bytes,

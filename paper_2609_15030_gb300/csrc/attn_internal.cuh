@@ -24,7 +24,6 @@ struct AttnParams {
     int64_t max_pages;
     int64_t q_stride;
     int64_t o_stride;
-    int64_t units;                // prefill: tiles of keys of all items
     int32_t batch;
     int32_t n_heads;
     int32_t n_kv;
@@ -33,6 +32,7 @@ struct AttnParams {
     int32_t max_kv;               // decode: bound of kv_len
     int32_t prefix_len;
     int32_t unsplit;
+    int32_t units;                // prefill: key tiles of all items
     int32_t ctas;
     int32_t parts;                // about the most CTAs that share an item
     int32_t joined;               // partial results are left and joined
@@ -48,7 +48,8 @@ struct AttnParams {
     int32_t n_split;
 };
 
-// Fills in the schedule (units, ctas, start_*) and says how many bytes of workspace it takes.
+// Fills in the schedule (units, ctas, start_*) and says how many bytes of workspace it takes; -1: more
+// units than 31 bits count.
 int64_t plan_attn(AttnParams &p, int d, int sm_count);
 cudaError_t launch_attn(const AttnParams &p, int d, int dtype, cudaStream_t s);
 cudaError_t launch_kv_append(const void *k, const void *v, int64_t kv_stride, const int64_t *slots,
