@@ -77,35 +77,23 @@ hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
     return HS_OK;
 }
 
-// the plan of a valid call, and whether the caller's workspace holds it
-hs_status plan(hs::AttnParams &p, int d, int64_t *bytes)
+hs_status room(int64_t need, void *workspace, int64_t workspace_bytes, hs::AttnParams &p)
 {
-    int sms = 0;
-    const hs_status st = hs::device_sm_count(&sms);
-    if (st != HS_OK)
-        return st;
-    *bytes = hs::plan_attn(p, d, sms);
-    return *bytes < 0 ? HS_ERR_UNSUPPORTED : HS_OK;
-}
-
-hs_status run(hs::AttnParams &p, const hs_attn_shape &s, void *workspace, int64_t workspace_bytes,
-              cudaStream_t stream)
-{
-    int64_t need = 0;
-    const hs_status st = plan(p, s.head_dim, &need);
-    if (st != HS_OK)
-        return st;
+    if (need < 0)
+        return HS_ERR_UNSUPPORTED;
     if (need > workspace_bytes || (need > 0 && workspace == nullptr))
         return HS_ERR_INVALID_ARG;
     p.part = static_cast<float *>(workspace);
-    return cuda_status(hs::launch_attn(p, s.head_dim, s.dtype, stream));
+    return HS_OK;
 }
 
-// the requests' lengths into p; *any: whether there is a token
+// the requests' lengths into the plan; *any: whether there is a token
 hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32_t *n_tokens,
-                        const int64_t *cu_rows, bool rows, hs::AttnParams &p, bool *any)
+                        const int64_t *cu_rows, bool rows, const hs::AttnParams &p,
+                        hs::PrefillPlan &plan, bool *any)
 {
     *any = false;
+    std::memset(&plan, 0, sizeof plan);
     if (s.batch == 0)
         return HS_OK;
     if (pos0 == nullptr || n_tokens == nullptr || (rows && cu_rows == nullptr))
@@ -128,9 +116,9 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
             (int64_t)n_tokens[b] * p.group > INT32_MAX - 8192 ||
             (rows && cu_rows[b] + n_tokens[b] > INT32_MAX / p.n_heads))
             return HS_ERR_UNSUPPORTED;
-        p.pos0[b] = (int32_t)pos0[b];
-        p.n_tokens[b] = n_tokens[b];
-        p.row0[b] = rows ? (int32_t)cu_rows[b] : 0;
+        plan.req[b].pos0 = (int32_t)pos0[b];
+        plan.req[b].n = n_tokens[b];
+        plan.req[b].row0 = rows ? (int32_t)cu_rows[b] : 0;
     }
     return HS_OK;
 }
@@ -187,7 +175,13 @@ hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache,
     st = check_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
-    return run(p, *shp, workspace, workspace_bytes, stream);
+    int sms = 0;
+    st = hs::device_sm_count(&sms);
+    if (st == HS_OK)
+        st = room(hs::plan_attn_decode(p, shp->head_dim, sms), workspace, workspace_bytes, p);
+    if (st != HS_OK)
+        return st;
+    return cuda_status(hs::launch_attn_decode(p, shp->head_dim, shp->dtype, stream));
 }
 
 }  // namespace
@@ -230,10 +224,11 @@ hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *c
                           int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream)
 {
     hs::AttnParams p;
+    hs::PrefillPlan plan;
     hs_status st = check_shape(shp, p);
     bool any = false;
     if (st == HS_OK)
-        st = check_lengths(*shp, pos0, n_tokens, cu_rows, true, p, &any);
+        st = check_lengths(*shp, pos0, n_tokens, cu_rows, true, p, plan, &any);
     if (st != HS_OK || !any)
         return st;
     p.q = q;
@@ -245,7 +240,13 @@ hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *c
     st = check_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
-    return run(p, *shp, workspace, workspace_bytes, stream);
+    int sms = 0;
+    st = hs::device_sm_count(&sms);
+    if (st == HS_OK)
+        st = room(hs::plan_attn_prefill(p, plan, shp->head_dim, sms), workspace, workspace_bytes, p);
+    if (st != HS_OK)
+        return st;
+    return cuda_status(hs::launch_attn_prefill(p, plan, shp->head_dim, shp->dtype, stream));
 }
 
 hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_t *pos0,
@@ -254,14 +255,25 @@ hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_
     if (bytes_out == nullptr)
         return HS_ERR_INVALID_ARG;
     hs::AttnParams p;
+    hs::PrefillPlan plan;
     hs_status st = check_shape(shp, p);
     bool any = false;
     if (st == HS_OK)
-        st = check_lengths(*shp, pos0, n_tokens, nullptr, false, p, &any);
+        st = check_lengths(*shp, pos0, n_tokens, nullptr, false, p, plan, &any);
     if (st != HS_OK)
         return st;
     *bytes_out = 0;
-    return any ? plan(p, shp->head_dim, bytes_out) : HS_OK;
+    if (!any)
+        return HS_OK;
+    int sms = 0;
+    st = hs::device_sm_count(&sms);
+    if (st != HS_OK)
+        return st;
+    const int64_t need = hs::plan_attn_prefill(p, plan, shp->head_dim, sms);
+    if (need < 0)
+        return HS_ERR_UNSUPPORTED;
+    *bytes_out = need;
+    return HS_OK;
 }
 
 hs_status hs_attn_decode(const hs_attn_shape *shp, const void *q, const void *cache,
@@ -295,14 +307,21 @@ hs_status hs_attn_decode_shared_workspace_bytes(const hs_attn_shape *shp, int64_
     if (bytes_out == nullptr)
         return HS_ERR_INVALID_ARG;
     hs::AttnParams p;
-    const hs_status st = check_decode(shp, prefix_len, max_kv_len, p);
+    hs_status st = check_decode(shp, prefix_len, max_kv_len, p);
     if (st != HS_OK)
         return st;
     *bytes_out = 0;
     if (p.batch == 0)
         return HS_OK;
-    p.kv_len = bytes_out != nullptr ? reinterpret_cast<const int32_t *>(bytes_out) : nullptr;
-    return plan(p, shp->head_dim, bytes_out);
+    int sms = 0;
+    st = hs::device_sm_count(&sms);
+    if (st != HS_OK)
+        return st;
+    const int64_t need = hs::plan_attn_decode(p, shp->head_dim, sms);
+    if (need < 0)
+        return HS_ERR_UNSUPPORTED;
+    *bytes_out = need;
+    return HS_OK;
 }
 
 }  // extern "C"

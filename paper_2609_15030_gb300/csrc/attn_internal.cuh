@@ -9,7 +9,8 @@ namespace hs {
 constexpr int kAttnMaxCtas = 320;
 
 // One attention call, passed by value to the kernels.  A decode step is the call in which every
-// request has one token, row b, and the lengths lie on the device.
+// request has one token, row b, and the lengths lie on the device.  (What only a prefill needs is a
+// parameter of its own: a launch moves all of them.)
 struct AttnParams {
     const void *q;
     const void *cache;
@@ -34,24 +35,36 @@ struct AttnParams {
     int32_t unsplit;
     int32_t units;                // prefill: key tiles of all items
     int32_t ctas;
-    int32_t parts;                // about the most CTAs that share an item
+    int32_t groups;               // tiles of 128 rows to an item
+    int32_t n_split;              // prefill: items that fall to several CTAs
+    int32_t parts;                // decode: about the most CTAs that share an item
     int32_t joined;               // partial results are left and joined
     float scale_log2;             // scale * log2(e)
-    // prefill only: the requests, and where each CTA's share of the tiles begins
-    int32_t pos0[HS_MAX_BATCH];
-    int32_t n_tokens[HS_MAX_BATCH];
-    int32_t row0[HS_MAX_BATCH];
-    int32_t start_item[kAttnMaxCtas];   // row tile * n_kv + KV head of the request
-    int32_t start_kt[kAttnMaxCtas];
-    int16_t start_b[kAttnMaxCtas];
-    int16_t split_at[kAttnMaxCtas];     // CTAs whose run is the first to begin inside an item
-    int32_t n_split;
 };
 
-// Fills in the schedule (units, ctas, start_*) and says how many bytes of workspace it takes; -1: more
-// units than 31 bits count.
-int64_t plan_attn(AttnParams &p, int d, int sm_count);
-cudaError_t launch_attn(const AttnParams &p, int d, int dtype, cudaStream_t s);
+// The requests of a prefill, and its schedule.
+struct PrefillPlan {
+    static constexpr bool kDecode = false;
+    struct Request {
+        int32_t pos0, n, row0, unused;
+    } req[HS_MAX_BATCH];
+    struct Cta {                  // where its run of units begins
+        int32_t b, item, unit, unused;   // item: row tile * n_kv + KV head; the unit of the item
+    } cta[kAttnMaxCtas];
+    int16_t split_at[kAttnMaxCtas];      // CTAs whose run is the first to begin between an item's tiles
+};
+
+// a decode step has all of it on the device
+struct DecodePlan {
+    static constexpr bool kDecode = true;
+};
+
+// Fill in the schedule and say how many bytes of workspace it takes; -1: more units than 31 bits count.
+int64_t plan_attn_prefill(AttnParams &p, PrefillPlan &plan, int d, int sm_count);
+int64_t plan_attn_decode(AttnParams &p, int d, int sm_count);
+cudaError_t launch_attn_prefill(const AttnParams &p, const PrefillPlan &plan, int d, int dtype,
+                                cudaStream_t s);
+cudaError_t launch_attn_decode(const AttnParams &p, int d, int dtype, cudaStream_t s);
 cudaError_t launch_kv_append(const void *k, const void *v, int64_t kv_stride, const int64_t *slots,
                              int64_t n_rows, void *cache, int32_t row_vecs, int32_t page_shift,
                              int64_t num_blocks, int32_t *d_err, int sm_count, cudaStream_t s);

@@ -13,35 +13,34 @@
 //
 // Schedule.  The units of all items in order are shared out evenly over the CTAs, each a
 // contiguous run, so that one long request or many ragged ones fill the SMs alike.  An item whose
-// keys fall to several CTAs leaves (m, l, a) of each in the workspace and attn_merge_kernel joins
+// keys fall to several CTAs leaves (m, l, a) of each in the workspace and a second kernel joins
 // them.  With `unsplit` a CTA takes the whole items that begin in its run.
 //
 // Warps.  Per tile of rows one group of four softmax warps (thread = row = TMEM lane) and a warp that
 // issues its MMAs; one warp that loads keys and values by TMA; the others look after values at
 // masked places.  Per key tile and group: S = Q K^T into TMEM; the group reads it, writes the
-// weights over it as 16-bit pairs, half of them at a time; O += P V with P as the TMEM operand.  With
+// weights over it as 16-bit pairs; O += P V with P as the TMEM operand.  With
 // two groups the tensor core works on one while the other is in its softmax.
 //
 // Values at masked places.  A weight of zero times a NaN or an infinity is NaN, so v must be finite
 // wherever some row of the tile does not attend: rows behind the last key are zeroed in shared
 // memory, and keys that only some rows see (the causal diagonal) are searched; a value there that
 // is not finite is zeroed and noted, and the rows that do see it get NaN in its column at the end.
+#pragma once
+
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <climits>
-
-#include "attn_internal.cuh"
+#include "attn_walk.cuh"
 #include "sm100_ptx.cuh"
 
 namespace hs {
-namespace {
+namespace attn {
 
 using namespace ptx;
 
-constexpr int kKeys = 128;               // keys per tile
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;            // log2 of the largest weight
 constexpr uint64_t kTimeoutNs = 1000000000ull;
@@ -68,19 +67,12 @@ struct Cfg {
     static constexpr int kTmemCols = NG == 2 ? 512 : 256;  // S and O of each group, 128 columns each
 };
 
-// where a CTA's run of units begins and ends
-struct Start {
-    int32_t u, left;                     // its first unit and how many
-    int32_t b, rt, kvh, kt;
-};
-
 // shared memory behind the tiles
 template <int D, int NG>
 struct Smem {
     uint64_t full[8], empty[8];          // a stage may be read / its MMAs are done
     uint64_t raw[8];                     // a value tile with masked places has landed
-    uint64_t q_full[2], s_full[2], o_full[2];
-    uint64_t p_full[2][2];               // of each half of the weights
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
     uint64_t drain[2];
     uint32_t tmem;
     int32_t abort;
@@ -102,300 +94,6 @@ constexpr int smem_bytes()
 static_assert(smem_bytes<128, 2>() <= 227 * 1024 && smem_bytes<64, 2>() <= 227 * 1024, "");
 static_assert(2 * (smem_bytes<128, 1>() + 1024) <= 228 * 1024 &&
               2 * (smem_bytes<64, 1>() + 1024) <= 228 * 1024, "two CTAs per SM");
-
-// ---- the walk over items -------------------------------------------------------------------
-
-__host__ __device__ __forceinline__ int tiles_of(int keys)
-{
-    return (keys + kKeys - 1) / kKeys;
-}
-
-// the first unit of CTA c's run (c <= 320; small numbers without the slow division)
-__host__ __device__ __forceinline__ int first_unit(int units, int ctas, int c)
-{
-    if (units < 1 << 22)
-        return (int)((uint32_t)units * (uint32_t)c / (uint32_t)ctas);
-    return (int)((int64_t)units * c / ctas);
-}
-
-// the CTA that has unit u: the largest c with first_unit(c) <= u
-__device__ __forceinline__ int cta_of(int units, int ctas, int u)
-{
-    if (units < 1 << 22)
-        return (int)(((uint32_t)(u + 1) * (uint32_t)ctas - 1) / (uint32_t)units);
-    return (int)((((int64_t)u + 1) * ctas - 1) / units);
-}
-
-__device__ __forceinline__ bool has_units(int units, int ctas, int c)
-{
-    return first_unit(units, ctas, c) < first_unit(units, ctas, c + 1);
-}
-
-// b = -1 stands for the shared prefix, whose rows are those of all requests
-template <int NG>
-__host__ __device__ __forceinline__ int row_tiles(int rows)
-{
-    return (rows + 128 * NG - 1) / (128 * NG);
-}
-
-// prefill: key tiles of a request's row tile
-template <int NG>
-__host__ __device__ __forceinline__ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
-{
-    const int64_t last = ((int64_t)(rt + 1) * 128 * NG - 1) / group;
-    return tiles_of(pos0 + (int)(last < n_tokens - 1 ? last : n_tokens - 1) + 1);
-}
-
-// one item's key tiles [kt0, kt1) as one CTA has them
-struct Segment {
-    int b, rt, kvh, kt0, kt1;
-    int rows;        // of the whole request (or of all, for the prefix)
-    bool whole;      // all of the item's key tiles
-    int item;        // running number of the item within its part (prefix or requests), decode only
-};
-
-template <int NG>
-struct Walk {
-    const AttnParams &p;
-    const int32_t *len;
-    int left;                            // units of the run not yet given out
-    int b, rt, kvh, kt;
-
-    __device__ int rows() const
-    {
-        return b < 0 ? p.batch * p.group : p.kv_len != nullptr ? p.group : p.n_tokens[b] * p.group;
-    }
-    __device__ int tiles() const
-    {
-        if (b < 0)
-            return tiles_of(p.prefix_len);
-        if (p.kv_len != nullptr)
-            return len[b] > 0 ? tiles_of(len[b]) : 1;   // an empty row is written by someone
-        return prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
-    }
-    __device__ bool skip() const
-    {
-        return p.kv_len != nullptr ? len[b] < 0 : p.n_tokens[b] == 0;
-    }
-    __device__ void next_item()
-    {
-        kt = 0;
-        if (++kvh < p.n_kv)
-            return;
-        kvh = 0;
-        if (++rt < row_tiles<NG>(rows()))
-            return;
-        rt = 0;
-        do
-            ++b;
-        while (b < p.batch && skip());
-    }
-    __device__ Walk(const AttnParams &params, const int32_t *lens, const Start &s)
-        : p(params), len(lens), left(s.left), b(s.b), rt(s.rt), kvh(s.kvh), kt(s.kt)
-    {
-        if (p.unsplit && left > 0 && kt != 0) {       // begins with the next whole item
-            left -= tiles() - kt;
-            next_item();
-        }
-    }
-    __device__ bool next(Segment &s)
-    {
-        if (left <= 0)
-            return false;
-        const int n = tiles();
-        int take = n - kt;
-        if (!p.unsplit && take > left)
-            take = left;
-        s.b = b;
-        s.rt = rt;
-        s.kvh = kvh;
-        s.kt0 = kt;
-        s.kt1 = kt + take;
-        s.rows = rows();
-        s.whole = kt == 0 && take == n;
-        s.item = (b < 0 ? rt : b) * p.n_kv + kvh;
-        left -= take;
-        kt += take;
-        if (kt == n)
-            next_item();
-        return true;
-    }
-};
-
-// keys that the last row of group g of a segment's row tile attends to (0: the group has no row)
-template <int NG>
-__device__ __forceinline__ int group_keys(const AttnParams &p, const int32_t *len, const Segment &s,
-                                          int g)
-{
-    const int r0 = (s.rt * NG + g) * 128;
-    if (r0 >= s.rows)
-        return 0;
-    if (s.b < 0)
-        return p.prefix_len;
-    if (p.kv_len != nullptr)
-        return len[s.b];
-    const int last = (s.rows - r0 < 128 ? s.rows : r0 + 128) - 1;
-    return p.pos0[s.b] + last / p.group + 1;
-}
-
-// keys that every row of the segment's item attends to
-template <int NG>
-__device__ __forceinline__ int common_keys(const AttnParams &p, const int32_t *len, const Segment &s)
-{
-    if (s.b < 0)
-        return p.prefix_len;
-    if (p.kv_len != nullptr)
-        return len[s.b];
-    return p.pos0[s.b] + s.rt * 128 * NG / p.group + 1;
-}
-
-// tiles of the segment that a group with `keys` keys takes part in
-__device__ __forceinline__ int group_tiles(const Segment &s, int keys)
-{
-    const int n = tiles_of(keys);
-    const int end = n < s.kt1 ? n : s.kt1;
-    return end > s.kt0 ? end - s.kt0 : 0;
-}
-
-// decode: units of request b (0: its length is out of bounds and it is skipped)
-__device__ __forceinline__ int own_units(const AttnParams &p, int len)
-{
-    return len < 0 ? 0 : (len > 0 ? tiles_of(len) : 1) * p.n_kv;
-}
-
-__device__ __forceinline__ int warp_scan(int x, int lane)
-{
-#pragma unroll
-    for (int w = 1; w < 32; w <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, w);
-        if (lane >= w)
-            x += y;
-    }
-    return x;
-}
-
-// decode, one warp: the lengths into shared memory; returns the units of all requests, and in
-// *before those of the requests in front of `upto`
-__device__ __forceinline__ int read_lengths(const AttnParams &p, int32_t *len, int lane, bool complain,
-                                            int upto, int *before)
-{
-    int sum = 0, part = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const int b = b0 + lane;
-        int n = -1;
-        if (b < p.batch) {
-            n = p.kv_len[b];
-            if (n < 0 || n > p.max_kv) {
-                if (complain)
-                    report(p.d_err, HS_DEVERR_LENGTH);
-                n = -1;
-            }
-            len[b] = n;
-        }
-        const int x = own_units(p, n);
-        sum += x;
-        part += b < upto ? x : 0;
-    }
-    __syncwarp();
-    *before = __reduce_add_sync(0xffffffffu, part);
-    return __reduce_add_sync(0xffffffffu, sum);
-}
-
-// where CTA c's run begins (one warp; decode: with the lengths in shared memory, `own` their units)
-template <int NG>
-__device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *len, int own, int c,
-                                            int lane)
-{
-    Start s;
-    if (p.kv_len == nullptr) {
-        s.u = first_unit(p.units, p.ctas, c);
-        s.left = first_unit(p.units, p.ctas, c + 1) - s.u;
-        s.b = p.start_b[c];
-        s.rt = p.start_item[c] / p.n_kv;
-        s.kvh = p.start_item[c] - s.rt * p.n_kv;
-        s.kt = p.start_kt[c];
-        return s;
-    }
-    const int per = tiles_of(p.prefix_len);
-    const int pre = per * p.n_kv * row_tiles<NG>(p.batch * p.group);
-    const int units = pre + own;
-    s.u = first_unit(units, p.ctas, c);
-    s.left = first_unit(units, p.ctas, c + 1) - s.u;
-    s.b = -1;
-    s.rt = s.kvh = s.kt = 0;
-    if (s.u < pre) {
-        const int item = s.u / per;
-        s.kt = s.u - item * per;
-        s.rt = item / p.n_kv;
-        s.kvh = item - s.rt * p.n_kv;
-        return s;
-    }
-    int v = s.u - pre;                 // the request with unit v of all requests'
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const int b = b0 + lane;
-        const int x = own_units(p, b < p.batch ? len[b] : -1);
-        const int incl = warp_scan(x, lane);
-        const unsigned hit = __ballot_sync(0xffffffffu, v < incl);
-        const int last = __shfl_sync(0xffffffffu, incl, 31);
-        if (hit != 0) {
-            const int at = __ffs(hit) - 1;
-            v -= __shfl_sync(0xffffffffu, incl - x, at);
-            s.b = b0 + at;
-            const int n = len[s.b] > 0 ? tiles_of(len[s.b]) : 1;
-            s.kvh = v / n;
-            s.kt = v - s.kvh * n;
-            return s;
-        }
-        v -= last;
-    }
-    return s;                                 // no unit is left
-}
-
-// ---- partial results -----------------------------------------------------------------------
-//
-// A slot holds R rows: R pairs (m, l), padded to 16 bytes, then the sums a: of decode R rows of D
-// floats, of prefill D columns of R (a warp stores 32 rows of a column, and the join reads them so).  Without a shared prefix an item
-// leaves a partial result in at most two places of a CTA's run: at its beginning, where it does not
-// start the item (slot 2 cta), and at its end, where it does (slot 2 cta + 1).  Behind a shared
-// prefix every segment is partial; its slot is item + cta, which no other segment of its part
-// (prefix, requests) has, since both only grow along the run.
-
-__host__ __device__ __forceinline__ int pairs_floats(int rows)
-{
-    return (2 * rows + 3) / 4 * 4;
-}
-
-template <int D>
-__host__ __device__ __forceinline__ int64_t slot_floats(int rows)
-{
-    return pairs_floats(rows) + (int64_t)rows * D;
-}
-
-template <int D, int NG>
-__host__ __device__ __forceinline__ int64_t prefix_part_floats(const AttnParams &p)
-{
-    return (int64_t)(row_tiles<NG>(p.batch * p.group) * p.n_kv + p.ctas) * slot_floats<D>(128 * NG);
-}
-
-// rows of a slot of the requests' part: an item's
-template <int NG>
-__host__ __device__ __forceinline__ int slot_rows(const AttnParams &p)
-{
-    return p.kv_len != nullptr ? p.group : 128 * NG;
-}
-
-template <int D, int NG>
-__device__ __forceinline__ float *slot_of(const AttnParams &p, const Segment &s, int cta, int *rows)
-{
-    if (s.b < 0) {
-        *rows = 128 * NG;
-        return p.part + (int64_t)(s.item + cta) * slot_floats<D>(128 * NG);
-    }
-    *rows = slot_rows<NG>(p);
-    if (p.prefix_len > 0)
-        return p.part + prefix_part_floats<D, NG>(p) + (int64_t)(s.item + cta) * slot_floats<D>(*rows);
-    return p.part + (int64_t)(2 * cta + (s.kt0 == 0)) * slot_floats<D>(*rows);
-}
 
 // ---- element types -------------------------------------------------------------------------
 
@@ -447,9 +145,10 @@ __device__ __forceinline__ float ex2(float x)
 
 // ---- the kernel ----------------------------------------------------------------------------
 
-template <typename T, int D, int NG>
+template <typename T, int D, int NG, class Plan>
 __global__ void __launch_bounds__(Cfg<D, NG>::kThreads, NG == 2 ? 1 : 2)
-attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map)
+attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan plan,
+            const __grid_constant__ CUtensorMap map)
 {
     using C = Cfg<D, NG>;
     using Sm = Smem<D, NG>;
@@ -486,8 +185,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         for (int g = 0; g < NG; ++g) {
             mbar_init(smem_u32(&sm.q_full[g]), 128);
             mbar_init(smem_u32(&sm.s_full[g]), 1);
-            mbar_init(smem_u32(&sm.p_full[g][0]), 128);
-            mbar_init(smem_u32(&sm.p_full[g][1]), 128);
+            mbar_init(smem_u32(&sm.p_full[g]), 128);
             mbar_init(smem_u32(&sm.o_full[g]), 1);
             mbar_init(smem_u32(&sm.drain[g]), 1);
         }
@@ -502,9 +200,14 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     if (p.joined)
         pdl_release();     // the join takes its place as CTAs end
     if (warp == C::kSoftmax + 3) {
-        int before = 0;
-        const int own = p.kv_len != nullptr ? read_lengths(p, sm.len, lane, cta == 0, 0, &before) : 0;
-        const Start st = find_start<NG>(p, sm.len, own, cta, lane);
+        Start st;
+        if constexpr (Plan::kDecode) {
+            int before = 0;
+            const int own = read_lengths(p, sm.len, lane, cta == 0, 0, &before);
+            st = find_start<NG>(p, sm.len, own, cta, lane);
+        } else {
+            st = find_start<NG>(p, plan, cta);
+        }
         if (lane == 0)
             sm.start = st;
     }
@@ -512,7 +215,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sm.tmem;
-    Walk<NG> walk(p, sm.len, sm.start);
+    Walk<NG, Plan> walk(p, plan, sm.len, sm.start);
     Segment s;
 
     if (warp >= C::kSoftmax) {
@@ -527,11 +230,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         uint32_t is_raw = 0, ph_raw = 0;          // by stage: filled behind `raw`; its last phase
         bool go = true;
         while (go && walk.next(s)) {
-            int keys = group_keys<NG>(p, sm.len, s, NG - 1);
-            if (NG == 2 && keys == 0)
-                keys = group_keys<NG>(p, sm.len, s, 0);
+            const int keys = walk.all_keys(s);
             const int tiles = group_tiles(s, keys);
-            const int common = common_keys<NG>(p, sm.len, s);
+            const int common = walk.common_keys(s);
             const int32_t *const table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
             // block ids a tile ahead of their copies
             auto block = [&](int kt) -> int32_t {
@@ -591,7 +292,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         const int g = warp - C::kSoftmax;
         const uint32_t s_at = tmem + g * 256, o_at = s_at + 128;
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
-        const uint32_t bar_p = smem_u32(&sm.p_full[g][0]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
         const uint64_t q_desc = sdesc_sw128(q_at + g * C::kTile, 16, 1024);
         const uint64_t k_desc = sdesc_sw128(st_at, 16, kHalf * 1024);
         const uint64_t v_desc = sdesc_sw128(st_at, 1024, kHalf * 1024);
@@ -626,57 +327,50 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         uint32_t ph_q = 0, ph_p = 0;
         bool go = true;
         while (go && walk.next(s)) {
-            const int keys = group_keys<NG>(p, sm.len, s, g);
+            const int keys = walk.group_keys(s, g);
             const int mine = group_tiles(s, keys);
-            int most = mine;
-            if (NG == 2) {
-                const int other = group_tiles(s, group_keys<NG>(p, sm.len, s, 1 - g));
-                most = other > most ? other : most;
-            }
-            if (mine > 0) {
+            const int most = group_tiles(s, walk.all_keys(s));
+            if (most > 0) {
+                // also where the group has no part: so that it is never more than a segment behind
                 go = wait(bar_q, ph_q) && wait(full(st), ph);
                 ph_q ^= 1;
                 if (!go)
                     break;
                 tc_fence_after();
-                qk();
-                next_stage();
-            } else if (most > 0) {
-                go = pass();
+                if (mine > 0) {
+                    qk();
+                    next_stage();
+                } else {
+                    go = pass();
+                }
             }
             int left = keys - s.kt0 * kKeys;
             for (int j = 0; j < most && go; ++j, left -= kKeys) {
                 if (j >= mine) {
                     go = pass() && (j + 1 == most || pass());
+                    if (mine == 0 && j + 1 == most && lane == 0)
+                        mbar_arrive(bar_o);      // its softmax warps wait for every segment's end
                     continue;
                 }
                 const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
-                const uint32_t v_st = st, v_ph = ph;
-                next_stage();
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    go = go && wait(bar_p + 8 * h, ph_p) && (h == 1 || wait(full(v_st), v_ph));
-                    if (!go)
-                        break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t b = v_desc + v_st * (C::kTile / 16);
-#pragma unroll
-                        for (int k = h * 4; k < h * 4 + 4; ++k)
-                            if (k < steps)
-                                mma_f16_ts(o_at, s_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
-                                           Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
-                        if (h == 1) {
-                            if (j + 1 == mine)
-                                tc_commit(bar_o);
-                            tc_commit(empty(v_st));
-                        }
-                    }
-                    __syncwarp();
-                }
+                go = wait(bar_p, ph_p) && wait(full(st), ph);
                 ph_p ^= 1;
                 if (!go)
                     break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t b = v_desc + st * (C::kTile / 16);
+#pragma unroll
+                    for (int k = 0; k < kKeys / 16; ++k)
+                        if (k < steps)
+                            mma_f16_ts(o_at, s_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
+                                       Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
+                    if (j + 1 == mine)
+                        tc_commit(bar_o);
+                    tc_commit(empty(st));
+                }
+                __syncwarp();
+                next_stage();
                 if (j + 1 < mine) {
                     go = wait(full(st), ph);
                     if (!go)
@@ -716,13 +410,11 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         auto pair_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWho) : "memory"); };
         bool go = true;
         for (; go && walk.next(s); ++seg) {
-            int all = group_keys<NG>(p, sm.len, s, NG - 1);
-            if (NG == 2 && all == 0)
-                all = group_keys<NG>(p, sm.len, s, 0);
+            const int all = walk.all_keys(s);
             const int tiles = group_tiles(s, all);
-            const int common = common_keys<NG>(p, sm.len, s);
+            const int common = walk.common_keys(s);
             int32_t *const any = &sm.marks.any[seg % C::kMarks], *const from = sm.marks.from[seg % C::kMarks];
-            bool clean = p.kv_len != nullptr;        // a decode step has no keys that only some rows see
+            bool clean = Plan::kDecode;              // a decode step has no keys that only some rows see
             for (int j = 0; j < tiles && go; ++j, ++n) {
                 const int k0 = (s.kt0 + j) * kKeys;
                 if (k0 + kKeys <= common)
@@ -795,33 +487,33 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t s_at = tmem + g * 256 + lanes, o_at = s_at + 128;
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
-        const uint32_t bar_p = smem_u32(&sm.p_full[g][0]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
         uint32_t ph_s = 0, ph_o = 0;
         // this thread's row of a segment: its token row, head and keys
-        int64_t row = 0;
-        int head = 0, keys = 0, gkeys = 0;
-        bool ok = false;
+        int row = 0, head = 0, keys = 0, gkeys = 0;
+        bool ok = false, asked = false;      // asked: some group has tiles, so queries are due
         auto enter = [&](const Segment &x) {
             const int rr = (x.rt * NG + g) * 128 + r;
             ok = rr < x.rows;
             const int t = ok ? rr / p.group : 0;
             head = x.kvh * p.group + (ok ? rr - t * p.group : 0);
-            gkeys = group_keys<NG>(p, sm.len, x, g);
+            gkeys = walk.group_keys(x, g);
+            asked = group_tiles(x, walk.all_keys(x)) > 0;
             if (x.b < 0) {
                 row = t;
                 keys = p.prefix_len;
-            } else if (p.kv_len != nullptr) {
+            } else if constexpr (Plan::kDecode) {
                 row = x.b;
                 keys = sm.len[x.b];
             } else {
-                row = (int64_t)p.row0[x.b] + t;
-                keys = p.pos0[x.b] + t + 1;
+                row = plan.req[x.b].row0 + t;
+                keys = plan.req[x.b].pos0 + t + 1;
             }
         };
         // a warp copies its 32 rows, a row's 16-byte chunks by neighbouring lanes
         auto load_q = [&]() {
             constexpr int kChunks = D / 8, kRows = 32 / kChunks;
-            const int64_t from = ok ? row * p.q_stride + head * D : 0;
+            const int64_t from = ok ? (int64_t)row * p.q_stride + head * D : 0;
             const unsigned real = __ballot_sync(0xffffffffu, ok);
             const int c = lane % kChunks;
 #pragma unroll
@@ -841,7 +533,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
         bool have = walk.next(s), go = true;
         if (have) {
             enter(s);
-            if (group_tiles(s, gkeys) > 0) {
+            if (asked) {
                 load_q();
                 q_done();
             }
@@ -850,12 +542,27 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
             const int tiles = group_tiles(s, gkeys);
             float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
             int valid = keys - s.kt0 * kKeys;   // keys of the row from this tile on
+            const Segment was = s;
+            const int was_row = row, was_head = head, was_keys = keys, was_tiles = tiles_of(gkeys);
+            const bool was_ok = ok, was_asked = asked;
+            // the next segment's queries: where this one's last scores are here, its queries are done with
+            auto ahead = [&]() {
+                have = walk.next(s);
+                asked = false;
+                if (have) {
+                    enter(s);
+                    if (asked)
+                        load_q();
+                }
+            };
             for (int j = 0; j < tiles; ++j, valid -= kKeys) {
                 go = wait(bar_s, ph_s);
                 ph_s ^= 1;
                 if (!go)
                     break;
                 tc_fence_after();
+                if (j + 1 == tiles)
+                    ahead();
                 float x[kKeys];
 #pragma unroll
                 for (int c = 0; c < kKeys; c += 32)
@@ -901,64 +608,50 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                 const float shift = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
                 uint64_t l01 = 0, l23 = 0;
-                // the product with the first half of the values runs during the second half here
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int c = 0; c < kKeys; c += 32) {
+                    uint32_t w[16];
 #pragma unroll
-                    for (int c = h * 64; c < h * 64 + 64; c += 32) {
-                        uint32_t w[16];
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            const int e = c + 2 * i;
-                            const float2 y0 = unpair(fma2(pair(x[e], x[e + 1]), scale2, shift2));
-                            const float2 y1 = unpair(fma2(pair(x[e + 2], x[e + 3]), scale2, shift2));
-                            const float a0 = ex2(y0.x), a1 = ex2(y0.y), a2 = ex2(y1.x), a3 = ex2(y1.y);
-                            l01 = add2(l01, pair(a0, a1));
-                            l23 = add2(l23, pair(a2, a3));
-                            w[i] = Elem<T>::pack(a0, a1);
-                            w[i + 1] = Elem<T>::pack(a2, a3);
-                        }
-                        tmem_st16(s_at + c / 2, w);
+                    for (int i = 0; i < 16; i += 2) {
+                        const int e = c + 2 * i;
+                        const float2 y0 = unpair(fma2(pair(x[e], x[e + 1]), scale2, shift2));
+                        const float2 y1 = unpair(fma2(pair(x[e + 2], x[e + 3]), scale2, shift2));
+                        const float a0 = ex2(y0.x), a1 = ex2(y0.y), a2 = ex2(y1.x), a3 = ex2(y1.y);
+                        l01 = add2(l01, pair(a0, a1));
+                        l23 = add2(l23, pair(a2, a3));
+                        w[i] = Elem<T>::pack(a0, a1);
+                        w[i + 1] = Elem<T>::pack(a2, a3);
                     }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(bar_p + 8 * h);
+                    tmem_st16(s_at + c / 2, w);
                 }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar_p);
                 const float2 ls = unpair(add2(l01, l23));
                 l += ls.x + ls.y;
             }
             if (!go)
                 break;
-            // the next segment's queries while the last product runs: the scores of this one's last
-            // tile are here, so its queries are done with
-            const Segment was = s;
-            const int64_t was_row = row;
-            const int was_head = head, was_keys = keys, was_tiles = tiles_of(gkeys);
-            const bool was_ok = ok;
-            have = walk.next(s);
-            if (have) {
-                enter(s);
-                if (group_tiles(s, gkeys) > 0)
-                    load_q();
-            }
-            if (tiles > 0) {
+            if (tiles == 0)
+                ahead();
+            if (was_asked) {
                 go = wait(bar_o, ph_o);
                 ph_o ^= 1;
                 if (!go)
                     break;
                 tc_fence_after();
             }
-            if (have && group_tiles(s, gkeys) > 0)
+            if (asked)
                 q_done();
-            const bool marked = p.kv_len == nullptr && tiles > 0 &&
+            const bool marked = !Plan::kDecode && tiles > 0 &&
                                 (was.kt1 < was_tiles ? was.kt1 : was_tiles) * kKeys >
-                                    common_keys<NG>(p, sm.len, was) &&
+                                    walk.common_keys(was) &&
                                 *(volatile int32_t *)&sm.marks.any[seg % C::kMarks] != 0;
             const int32_t *const from = sm.marks.from[seg % C::kMarks];
-            const bool direct = was.whole && p.prefix_len == 0;
+            const bool direct = was.whole && (!Plan::kDecode || p.prefix_len == 0);
             if (direct) {
                 const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-                T *const o = static_cast<T *>(p.o) + was_row * p.o_stride + was_head * D;
+                T *const o = static_cast<T *>(p.o) + (int64_t)was_row * p.o_stride + was_head * D;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float a[32];
@@ -986,11 +679,11 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                     }
                 }
                 if (was_ok && p.lse != nullptr)
-                    p.lse[was_row * p.n_heads + was_head] =
+                    p.lse[(int64_t)was_row * p.n_heads + was_head] =
                         l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
             } else {
                 int rows = 0;
-                float *const slot = slot_of<D, NG>(p, was, cta, &rows);
+                float *const slot = slot_of<D, NG, Plan>(p, was, cta, &rows);
                 const int at = g * 128 + r;
                 const bool put = at < rows && was_ok;
                 if (put)
@@ -1006,7 +699,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtens
                             for (int i = 0; i < 32; ++i)
                                 a[i] = was_keys > from[c + i] ? NAN : a[i];
                         }
-                        if (put && p.kv_len == nullptr) {
+                        if (put && !Plan::kDecode) {
                             float *const to = slot + pairs_floats(rows) + c * rows + at;
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
@@ -1180,143 +873,9 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, Joined<D> x, int
         write_row<T, D>(p, x, row, head, lane);
 }
 
-// prefill: block (x, y, z) takes 32 rows and 32 columns of the x-th item that is split between CTAs,
-// a lane a row and a warp four columns
-template <typename T, int D, int NG>
-__global__ void __launch_bounds__(kMergeWarps * 32)
-attn_merge_prefill_kernel(const __grid_constant__ AttnParams p)
-{
-    constexpr int R = 128 * NG, kAhead = 8;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Start st = find_start<NG>(p, nullptr, 0, p.split_at[blockIdx.x], lane);
-    const Walk<NG> w(p, nullptr, st);
-    const int u0 = st.u - st.kt, u1 = u0 + w.tiles();      // the item's units
-    const int c0 = cta_of(p.units, p.ctas, u0), c1 = cta_of(p.units, p.ctas, u1 - 1);
-    const int64_t size = slot_floats<D>(R);
-    const int r = blockIdx.y * 32 + lane, rr = w.rt * R + r, col = blockIdx.z * 32 + warp * 4;
-    const bool on = rr < w.rows();
-    pdl_wait_and_release();
-    if (!on)
-        return;
-    // part i of the item: CTA c0's last segment, then the first ones of the CTAs behind it
-    const float *const first = p.part + (2 * c0 + 1) * size, *const rest = p.part + 2 * c0 * size;
-    const int parts = c1 - c0 + 1;
-    float m = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < parts; i0 += kAhead) {
-        float2 ml[kAhead];
-        float v[kAhead][4];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            ml[i] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                v[i][e] = 0.f;
-            if (i0 + i < parts) {
-                const float *const slot = i0 + i == 0 ? first : rest + 2 * (i0 + i) * size;
-                ml[i] = reinterpret_cast<const float2 *>(slot)[r];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[i][e] = slot[pairs_floats(R) + (col + e) * R + r];
-            }
-        }
-        float top = m;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            top = fmaxf(top, ml[i].x);
-        const float f = m == -INFINITY && l == 0.f ? 0.f : ex2(m - top);
-        m = top;
-        l *= f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            a[e] *= f;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            // a part without a key of this row: what it holds of a means nothing
-            if (ml[i].x == -INFINITY && ml[i].y == 0.f)
-                continue;
-            const float h = ex2(ml[i].x - top);
-            l = fmaf(ml[i].y, h, l);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                a[e] = fmaf(v[i][e], h, a[e]);
-        }
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    const int t = rr / p.group, head = w.kvh * p.group + rr - t * p.group;
-    const int64_t row = (int64_t)p.row0[w.b] + t;
-    *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + row * p.o_stride + head * D + col) =
-        make_uint2(Elem<T>::pack(a[0] * inv, a[1] * inv), Elem<T>::pack(a[2] * inv, a[3] * inv));
-    if (p.lse != nullptr && col == 0)
-        p.lse[row * p.n_heads + head] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
-}
+// ---- launch --------------------------------------------------------------------------------
 
-// decode: block (request and KV head, y); with a shared prefix its parts first
-template <typename T, int D, int NG>
-__global__ void __launch_bounds__(kMergeWarps * 32)
-attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
-{
-    __shared__ int32_t len[HS_MAX_BATCH];
-    __shared__ int sums[2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int b = blockIdx.x / p.n_kv, kvh = blockIdx.x - b * p.n_kv;
-    // the lengths may be read before the wait: the kernel in front, which has waited itself, only
-    // reads them
-    if (warp == 0) {
-        int before = 0;
-        const int n = read_lengths(p, len, lane, false, b, &before);
-        if (lane == 0) {
-            sums[0] = before;
-            sums[1] = n;
-        }
-    }
-    __syncthreads();
-    const int per = tiles_of(p.prefix_len), own = len[b] > 0 ? tiles_of(len[b]) : 1;
-    const int pre = per * p.n_kv * row_tiles<NG>(p.batch * p.group);
-    const int units = pre + sums[1];
-    const int u0 = pre + sums[0] + kvh * own;
-    const int item = b * p.n_kv + kvh;
-    const bool skip = len[b] < 0;
-    // an unsplit item belongs to the CTA in whose run it begins
-    const int c0 = skip ? 0 : cta_of(units, p.ctas, u0);
-    const int c1 = skip || p.unsplit ? c0 : cta_of(units, p.ctas, u0 + own - 1);
-    pdl_wait_and_release();
-    if (skip || (per == 0 && c0 == c1))
-        return;
-    const int64_t own_at = per > 0 ? prefix_part_floats<D, NG>(p) : 0, size = slot_floats<D>(p.group);
-    const int64_t pre_size = slot_floats<D>(128 * NG);
-    const int some = kMergeWarps / per_row;
-    for (int h0 = blockIdx.y * some; h0 < p.group; h0 += gridDim.y * some) {
-        const int h = h0 + warp / per_row;
-        const bool on = h < p.group;
-        const int rr = b * p.group + h, rt = rr / (128 * NG), r = rr - rt * 128 * NG;
-        const int pitem = rt * p.n_kv + kvh;
-        int p0 = 0, p1 = -1;
-        if (on && per > 0) {
-            p0 = cta_of(units, p.ctas, pitem * per);
-            p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (pitem + 1) * per - 1);
-        }
-        const int n = p1 - p0 + 1;
-        const Joined<D> x = join_parts<D>(
-            p.part, on ? n + c1 - c0 + 1 : 0, warp % per_row, per_row, lane,
-            [&](int i, int64_t &at_pair, int64_t &at_a) {
-                const bool pre_part = i < n;
-                const int c = pre_part ? p0 + i : c0 + i - n;
-                const int64_t slot =
-                    pre_part ? (pitem + c) * pre_size
-                    : per > 0 ? own_at + (item + c) * size
-                              : (int64_t)(c == c0 ? 2 * c + 1 : 2 * c) * size;
-                const int row = pre_part ? r : h;
-                at_pair = slot + 2 * row;
-                at_a = slot + pairs_floats(pre_part ? 128 * NG : p.group) + (int64_t)row * D;
-                return has_units(units, p.ctas, c);
-            });
-        finish_row<T, D>(p, x, per_row, warp, lane, on, b, kvh * p.group + h);
-    }
-}
-
-// ---- launches ------------------------------------------------------------------------------
-
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
+inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
 {
     // resolved once per process from the driver; a pure function pointer
     static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
@@ -1354,133 +913,16 @@ bool encode_cache(CUtensorMap *m, const AttnParams &p)
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int prefill_rows(const AttnParams &p)
-{
-    int most = 0;
-    for (int b = 0; b < p.batch; ++b)
-        most = p.n_tokens[b] > most ? p.n_tokens[b] : most;
-    return most * p.group;
-}
-
-// tiles of rows of an item: two where a request (or the rows in front of a shared prefix) has them
-int groups_of(const AttnParams &p)
-{
-    if (p.kv_len == nullptr)
-        return prefill_rows(p) > 128 ? 2 : 1;
-    return p.prefix_len > 0 && p.batch * p.group > 128 ? 2 : 1;
-}
-
-// most parts of an item of `tiles` key tiles
-int parts_of(int64_t tiles, int64_t units, int ctas)
-{
-    return (int)(tiles / (units / ctas > 0 ? units / ctas : 1)) + 2;
-}
-
-template <int NG>
-bool plan_prefill(AttnParams &p, int most)
-{
-    int64_t units = 0;
-    int longest = 0;
-    for (int b = 0; b < p.batch; ++b)
-        for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group); ++rt) {
-            const int n = prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
-            units += (int64_t)p.n_kv * n;
-            longest = n > longest ? n : longest;
-        }
-    if (units > INT_MAX)
-        return false;
-    p.units = (int)units;
-    p.ctas = (int)(units < most ? units : most);
-    p.parts = parts_of(longest, units, p.ctas);
-    int c = 0;
-    int64_t u = 0, split = -1;
-    p.n_split = 0;
-    for (int b = 0; b < p.batch && c < p.ctas; ++b)
-        for (int rt = 0; rt < row_tiles<NG>(p.n_tokens[b] * p.group) && c < p.ctas; ++rt) {
-            const int n = prefill_tiles<NG>(p.pos0[b], p.n_tokens[b], p.group, rt);
-            for (; c < p.ctas && first_unit(p.units, p.ctas, c) < u + (int64_t)n * p.n_kv; ++c) {
-                const int64_t v = first_unit(p.units, p.ctas, c) - u;
-                p.start_b[c] = (int16_t)b;
-                p.start_item[c] = rt * p.n_kv + (int)(v / n);
-                p.start_kt[c] = (int)(v % n);
-                // the first run that begins inside an item names it for the join
-                if (p.start_kt[c] != 0 && v / n * n + u != split) {
-                    split = v / n * n + u;
-                    p.split_at[p.n_split++] = (int16_t)c;
-                }
-            }
-            u += (int64_t)n * p.n_kv;
-        }
-    return true;
-}
-
-template <typename T, int D, int NG>
-cudaError_t launch(const AttnParams &p, cudaStream_t s)
+template <typename T, int D, int NG, class Plan>
+cudaError_t launch_tc(const AttnParams &p, const Plan &plan, cudaStream_t s)
 {
     CUtensorMap map;
     if (!encode_cache<D>(&map, p))
         return cudaErrorInvalidValue;
     static std::atomic<uint64_t> smem_set{0};
-    cudaError_t e = launch_pdl_big_smem(attn_kernel<T, D, NG>, dim3((unsigned)p.ctas),
-                                        dim3(Cfg<D, NG>::kThreads), smem_bytes<D, NG>(), s, smem_set, p,
-                                        map);
-    if (e != cudaSuccess || !p.joined)
-        return e;
-    if (p.kv_len == nullptr)
-        return launch_pdl(attn_merge_prefill_kernel<T, D, NG>,
-                          dim3((unsigned)p.n_split, 128 * NG / 32, D / 32), dim3(kMergeWarps * 32), 0, s, p);
-    // warps to a row: about eight parts each
-    int per_row = 1;
-    while (per_row < kMergeWarps && per_row * 8 < p.parts)
-        per_row *= 2;
-    const unsigned y = (unsigned)((p.group * per_row + kMergeWarps - 1) / kMergeWarps);
-    return launch_pdl(attn_merge_decode_kernel<T, D, NG>, dim3((unsigned)(p.batch * p.n_kv), y),
-                      dim3(kMergeWarps * 32), 0, s, p, per_row);
+    return launch_pdl_big_smem(attn_kernel<T, D, NG, Plan>, dim3((unsigned)p.ctas),
+                               dim3(Cfg<D, NG>::kThreads), smem_bytes<D, NG>(), s, smem_set, p, plan, map);
 }
 
-template <typename T>
-cudaError_t launch(const AttnParams &p, int d, cudaStream_t s)
-{
-    if (groups_of(p) == 2)
-        return d == 128 ? launch<T, 128, 2>(p, s) : launch<T, 64, 2>(p, s);
-    return d == 128 ? launch<T, 128, 1>(p, s) : launch<T, 64, 1>(p, s);
-}
-
-}  // namespace
-
-int64_t plan_attn(AttnParams &p, int d, int sm_count)
-{
-    const int ng = groups_of(p);
-    int most = sm_count * (ng == 2 ? 1 : 2);
-    if (most > kAttnMaxCtas)
-        most = kAttnMaxCtas;
-    auto slot = [&](int rows) {
-        return (int64_t)sizeof(float) * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows));
-    };
-    if (p.kv_len == nullptr) {
-        if (!(ng == 2 ? plan_prefill<2>(p, most) : plan_prefill<1>(p, most)))
-            return -1;
-        p.joined = !p.unsplit && p.n_split > 0;
-        return p.joined ? 2 * p.ctas * slot(128 * ng) : 0;
-    }
-    const int64_t own = (int64_t)p.batch * p.n_kv * (p.max_kv > 0 ? tiles_of(p.max_kv) : 1);
-    const int64_t items = (ng == 2 ? row_tiles<2>(p.batch * p.group) : row_tiles<1>(p.batch * p.group)) *
-                          (int64_t)p.n_kv;
-    const int64_t units = own + items * tiles_of(p.prefix_len);
-    if (units > INT_MAX)
-        return -1;
-    p.ctas = (int)(units < most ? units : most);
-    const int longest = p.max_kv > p.prefix_len ? p.max_kv : p.prefix_len;
-    p.parts = parts_of(tiles_of(longest), units, p.ctas);
-    p.joined = p.prefix_len > 0 || (!p.unsplit && p.ctas > 1 && tiles_of(p.max_kv) > 1);
-    if (p.prefix_len > 0)
-        return (items + p.ctas) * slot(128 * ng) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
-    return p.joined ? 2 * p.ctas * slot(p.group) : 0;
-}
-
-cudaError_t launch_attn(const AttnParams &p, int d, int dtype, cudaStream_t s)
-{
-    return dtype == HS_FP16 ? launch<__half>(p, d, s) : launch<__nv_bfloat16>(p, d, s);
-}
-
+}  // namespace attn
 }  // namespace hs
