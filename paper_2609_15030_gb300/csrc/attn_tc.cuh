@@ -52,19 +52,32 @@ struct Cfg {
     static constexpr int kTile = kKeys * D * 2;            // bytes of a tile of keys, values or rows
     // two groups: one CTA per SM, as many stages as fit; one group: two CTAs per SM
     static constexpr int kStages = NG == 2 ? (D == 128 ? 5 : 8) : (D == 128 ? 2 : 5);
-    // segments whose notes on values are kept.  A value tile is searched once the stage it lies in
-    // is free of the tile kStages / 2 before; the MMAs of that tile's segment began after both
-    // groups had left the segment before the one before it
-    static constexpr int kMarks = kStages <= 5 ? 4 : 8;
     static constexpr int kSoftmax = NG * 4;               // warps
     static constexpr int kThreads = (kSoftmax + 4) * 32;
     // registers of a softmax thread and of another one, out of those of the launch (65,536 over the
     // resident threads, a multiple of 8): 256 x 216 + 128 x 72 = 384 x 168 and
-    // 128 x 184 + 128 x 72 = 256 x 128
+    // 128 x 200 + 128 x 56 = 256 x 128
     static constexpr int kRegs = NG == 2 ? 168 : 128;
-    static constexpr int kMoreRegs = NG == 2 ? 216 : 184, kLessRegs = 72;
+    static constexpr int kMoreRegs = NG == 2 ? 216 : 200, kLessRegs = NG == 2 ? 72 : 56;
     static_assert(kSoftmax * 32 * kMoreRegs + 128 * kLessRegs <= kThreads * kRegs, "");
     static constexpr int kTmemCols = NG == 2 ? 512 : 256;  // S and O of each group, 128 columns each
+};
+
+constexpr int kRing = 4;                 // segments described ahead
+
+// One segment as the loading warp describes it to the others.  (Each of them walking by itself cost
+// a softmax warp 1 to 2 us a segment, in integer divisions and cold constants.)
+struct Info {
+    int32_t kt0, most;                   // first key tile; tiles of the group with the most, -1: the end
+    int32_t all, common;                 // keys that the last row, that every row attends to
+    int32_t head0;                       // first head of the KV head
+    int32_t slot_rows;                   // rows of the slot for partial results
+    int64_t slot;                        // its place in the workspace (floats); -1: results are written
+    struct {
+        int32_t row0, key0;              // token row and keys of the group's first row's token
+        int32_t head, rows;              // that row's head in the group; rows, at most 128
+        int32_t keys, tiles;             // keys of its last row; its tiles in the segment
+    } g[2];
 };
 
 // shared memory behind the tiles
@@ -73,15 +86,16 @@ struct Smem {
     uint64_t full[8], empty[8];          // a stage may be read / its MMAs are done
     uint64_t raw[8];                     // a value tile with masked places has landed
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t info_full[kRing], info_empty[kRing];
     uint64_t drain[2];
     uint32_t tmem;
     int32_t abort;
-    Start start;
+    Info info[kRing];
     union {
         int32_t len[HS_MAX_BATCH];       // decode: keys, or -1 for a length out of bounds
         struct {                         // prefill: values that are not finite, by segment
-            int32_t any[Cfg<D, NG>::kMarks];
-            int32_t from[Cfg<D, NG>::kMarks][D];   // first such position in the column
+            int32_t any[kRing];
+            int32_t from[kRing][D];      // first such position in the column
         } marks;
     };
 };
@@ -189,7 +203,11 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             mbar_init(smem_u32(&sm.o_full[g]), 1);
             mbar_init(smem_u32(&sm.drain[g]), 1);
         }
-                fence_mbar_init();
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(smem_u32(&sm.info_full[i]), 1);
+            mbar_init(smem_u32(&sm.info_empty[i]), C::kSoftmax + 3);
+        }
+        fence_mbar_init();
         sm.abort = 0;
     }
     if (warp == C::kSoftmax + 3 && lane == 0)
@@ -199,40 +217,86 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
     pdl_wait();
     if (p.joined)
         pdl_release();     // the join takes its place as CTAs end
-    if (warp == C::kSoftmax + 3) {
-        Start st;
-        if constexpr (Plan::kDecode) {
-            int before = 0;
-            const int own = read_lengths(p, sm.len, lane, cta == 0, 0, &before);
-            st = find_start<NG>(p, sm.len, own, cta, lane);
-        } else {
-            st = find_start<NG>(p, plan, cta);
-        }
-        if (lane == 0)
-            sm.start = st;
-    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&sm.tmem;
-    Walk<NG, Plan> walk(p, plan, sm.len, sm.start);
-    Segment s;
+    // segment k as described, and the end of this warp's use of it
+    auto described = [&](uint32_t k) -> bool {
+        return wait(smem_u32(&sm.info_full[k % kRing]), (k / kRing) & 1);
+    };
+    auto done_with = [&](uint32_t k) {
+        __syncwarp();
+        if (lane == 0)
+            mbar_arrive(smem_u32(&sm.info_empty[k % kRing]));
+    };
 
     if (warp >= C::kSoftmax) {
     fewer_registers<C::kLessRegs>();
     if (warp == C::kSoftmax + 3) {
-        // ---- loads: key and value tiles in turn through the stages
+        // ---- the walk, and loads: key and value tiles in turn through the stages
+        Start start;
+        if constexpr (Plan::kDecode) {
+            int before = 0;
+            const int own = read_lengths(p, sm.len, lane, cta == 0, 0, &before);
+            start = find_start<NG>(p, sm.len, own, cta, lane);
+        } else {
+            start = find_start<NG>(p, plan, cta);
+        }
+        Walk<NG, Plan> walk(p, plan, sm.len, start);
+        Segment s;
         const int per = p.page_shift >= 7 ? 1 : kKeys >> p.page_shift;      // pages of a tile
         const int box = p.page_shift >= 7 ? kKeys : 1 << p.page_shift;      // keys of a copy
         const int groups = 1 << (p.page_shift - 3);                         // 8-key rows of a page
         const int32_t none = (int32_t)(p.num_blocks * 2 * groups);          // beyond the cache: zeros
-        uint32_t n = 0;                                                     // stages filled
+        uint32_t n = 0, st = 0, ph = 1;           // stages filled; the next one and the phase that frees it
         uint32_t is_raw = 0, ph_raw = 0;          // by stage: filled behind `raw`; its last phase
         bool go = true;
-        while (go && walk.next(s)) {
-            const int keys = walk.all_keys(s);
-            const int tiles = group_tiles(s, keys);
-            const int common = walk.common_keys(s);
+        for (uint32_t seg = 0; go; ++seg) {
+            const bool have = walk.next(s);
+            int keys = 0, common = 0, tiles = -1;
+            Info *const info = &sm.info[seg % kRing];
+            if (seg >= kRing && !wait(smem_u32(&sm.info_empty[seg % kRing]), (seg / kRing - 1) & 1))
+                break;
+            if (have) {
+                keys = walk.all_keys(s);
+                common = walk.common_keys(s);
+                tiles = group_tiles(s, keys);
+                if (lane < NG) {
+                    const int r0 = (s.rt * NG + lane) * 128, left = s.rows - r0;
+                    const int t = s.b < 0 || !Plan::kDecode ? r0 / p.group : 0;
+                    const int own = walk.group_keys(s, lane);
+                    info->g[lane].head = r0 - t * p.group;
+                    info->g[lane].rows = left < 0 ? 0 : left < 128 ? left : 128;
+                    info->g[lane].keys = own;
+                    info->g[lane].tiles = group_tiles(s, own);
+                    if constexpr (Plan::kDecode) {
+                        info->g[lane].row0 = s.b < 0 ? t : s.b;
+                        info->g[lane].key0 = keys;
+                    } else {
+                        info->g[lane].row0 = plan.req[s.b].row0 + t;
+                        info->g[lane].key0 = plan.req[s.b].pos0 + t + 1;
+                    }
+                }
+                if (lane == 0) {
+                    info->kt0 = s.kt0;
+                    info->all = keys;
+                    info->common = common;
+                    info->head0 = s.kvh * p.group;
+                    int rows = 0;
+                    info->slot = s.whole && (!Plan::kDecode || p.prefix_len == 0)
+                                     ? -1
+                                     : slot_of<D, NG, Plan>(p, s, cta, &rows);
+                    info->slot_rows = rows;
+                }
+            }
+            if (lane == 0)
+                info->most = tiles;
+            __syncwarp();
+            if (lane == 0)
+                mbar_arrive(smem_u32(&sm.info_full[seg % kRing]));
+            if (!have)
+                break;
             const int32_t *const table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
             // block ids a tile ahead of their copies
             auto block = [&](int kt) -> int32_t {
@@ -254,9 +318,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     report(p.d_err, HS_DEVERR_BLOCK_OOB);
                 const int pages = __popc(__ballot_sync(0xffffffffu, mine));
                 const int in_page = (first & ((1 << p.page_shift) - 1)) >> 3;
-                for (int plane = 0; plane < 2; ++plane, ++n) {
-                    const int st = n % kSt;
-                    if (n >= kSt && !wait(empty(st), (n / kSt - 1) & 1)) {
+                for (int plane = 0; plane < 2; ++plane) {
+                    // the first round of waits passes: no phase is over yet
+                    if (!wait(empty(st), ph)) {
                         go = false;
                         break;
                     }
@@ -272,17 +336,22 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                                     s.kvh * kHalf,
                                     good ? (blk * 2 + plane) * groups + in_page : none, bar);
                     __syncwarp();
+                    ++n;
+                    if (++st == kSt) {
+                        st = 0;
+                        ph ^= 1;
+                    }
                 }
             }
         }
         // the copies and MMAs in flight end (bounded) before their memory goes away
         for (uint32_t i = n > kSt ? n - kSt : 0; i < n; ++i) {
-            const uint32_t st = i % kSt;
-            if (!wait(empty(st), (i / kSt) & 1)) {
-                if ((is_raw >> st) & 1)
-                    mbar_wait_bounded(smem_u32(&sm.raw[st]), ((ph_raw >> st) & 1) ^ 1, kTimeoutNs);
+            const uint32_t at = i % kSt;
+            if (!wait(empty(at), (i / kSt) & 1)) {
+                if ((is_raw >> at) & 1)
+                    mbar_wait_bounded(smem_u32(&sm.raw[at]), ((ph_raw >> at) & 1) ^ 1, kTimeoutNs);
                 else
-                    mbar_wait_bounded(full(st), (i / kSt) & 1, kTimeoutNs);
+                    mbar_wait_bounded(full(at), (i / kSt) & 1, kTimeoutNs);
             }
         }
     } else if (warp < C::kSoftmax + NG) {
@@ -326,30 +395,30 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         };
         uint32_t ph_q = 0, ph_p = 0;
         bool go = true;
-        while (go && walk.next(s)) {
-            const int keys = walk.group_keys(s, g);
-            const int mine = group_tiles(s, keys);
-            const int most = group_tiles(s, walk.all_keys(s));
-            if (most > 0) {
-                // also where the group has no part: so that it is never more than a segment behind
+        for (uint32_t seg = 0; go; ++seg) {
+            go = described(seg);
+            if (!go)
+                break;
+            const Info &info = sm.info[seg % kRing];
+            const int most = info.most, mine = info.g[g].tiles;
+            int left = info.g[g].keys - info.kt0 * kKeys;
+            done_with(seg);
+            if (most < 0)
+                break;
+            if (mine > 0) {
                 go = wait(bar_q, ph_q) && wait(full(st), ph);
                 ph_q ^= 1;
                 if (!go)
                     break;
                 tc_fence_after();
-                if (mine > 0) {
-                    qk();
-                    next_stage();
-                } else {
-                    go = pass();
-                }
+                qk();
+                next_stage();
+            } else if (most > 0) {
+                go = pass();
             }
-            int left = keys - s.kt0 * kKeys;
             for (int j = 0; j < most && go; ++j, left -= kKeys) {
                 if (j >= mine) {
                     go = pass() && (j + 1 == most || pass());
-                    if (mine == 0 && j + 1 == most && lane == 0)
-                        mbar_arrive(bar_o);      // its softmax warps wait for every segment's end
                     continue;
                 }
                 const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
@@ -394,7 +463,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
     } else {
         // ---- values at masked places: the warps that are left
         constexpr int kWho = (3 - NG) * 32;
-        uint32_t n = 0, seg = 0, ph_raw = 0;
+        uint32_t st_v = 1, ph_raw = 0;         // the stage of the next value tile
         const int who = tid - (C::kSoftmax + NG) * 32;
         auto pair_and = [](bool x) {
             int r;
@@ -409,14 +478,18 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         };
         auto pair_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWho) : "memory"); };
         bool go = true;
-        for (; go && walk.next(s); ++seg) {
-            const int all = walk.all_keys(s);
-            const int tiles = group_tiles(s, all);
-            const int common = walk.common_keys(s);
-            int32_t *const any = &sm.marks.any[seg % C::kMarks], *const from = sm.marks.from[seg % C::kMarks];
+        for (uint32_t seg = 0; go; ++seg) {
+            go = pair_and(described(seg));
+            if (!go)
+                break;
+            const Info &info = sm.info[seg % kRing];
+            const int tiles = info.most, all = info.all, common = info.common, kt0 = info.kt0;
+            if (tiles < 0)
+                break;
+            int32_t *const any = &sm.marks.any[seg % kRing], *const from = sm.marks.from[seg % kRing];
             bool clean = Plan::kDecode;              // a decode step has no keys that only some rows see
-            for (int j = 0; j < tiles && go; ++j, ++n) {
-                const int k0 = (s.kt0 + j) * kKeys;
+            for (int j = 0; j < tiles; ++j, st_v = (st_v + 2) % kSt) {
+                const int k0 = (kt0 + j) * kKeys;
                 if (k0 + kKeys <= common)
                     continue;
                 if (!clean) {
@@ -427,11 +500,10 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     clean = true;
                     pair_sync();
                 }
-                const uint32_t st = (2 * n + 1) % kSt;
-                go = wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1);
-                ph_raw ^= 1u << st;
+                const uint32_t st = st_v;
                 // these warps go on or none: they meet in a plain barrier below
-                go = pair_and(go);
+                go = pair_and(wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1));
+                ph_raw ^= 1u << st;
                 if (!go)
                     break;
                 uint8_t *const v = smem_raw + (NG + st) * C::kTile;
@@ -477,6 +549,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 if (who == 0)
                     mbar_arrive(full(st));
             }
+            if (go)
+                done_with(seg);
         }
     }
     } else {
@@ -489,40 +563,25 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
         const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
         uint32_t ph_s = 0, ph_o = 0;
-        // this thread's row of a segment: its token row, head and keys
-        int row = 0, head = 0, keys = 0, gkeys = 0;
-        bool ok = false, asked = false;      // asked: some group has tiles, so queries are due
-        auto enter = [&](const Segment &x) {
-            const int rr = (x.rt * NG + g) * 128 + r;
-            ok = rr < x.rows;
-            const int t = ok ? rr / p.group : 0;
-            head = x.kvh * p.group + (ok ? rr - t * p.group : 0);
-            gkeys = walk.group_keys(x, g);
-            asked = group_tiles(x, walk.all_keys(x)) > 0;
-            if (x.b < 0) {
-                row = t;
-                keys = p.prefix_len;
-            } else if constexpr (Plan::kDecode) {
-                row = x.b;
-                keys = sm.len[x.b];
-            } else {
-                row = plan.req[x.b].row0 + t;
-                keys = plan.req[x.b].pos0 + t + 1;
-            }
-        };
-        // a warp copies its 32 rows, a row's 16-byte chunks by neighbouring lanes
-        auto load_q = [&]() {
+        // row x of the group's rows, counted from its first one's token: x / p.group by multiplication,
+        // exact for x < 256, p.group <= 128 (the error of the factor is at most p.group, 256 * 128 < 2^16)
+        const uint32_t inv_group = 65536u / (uint32_t)p.group + 1;
+        auto token_of = [&](int x) { return (int)(((uint32_t)x * inv_group) >> 16); };
+        // a warp copies its 32 rows of a segment's queries, a row's 16-byte chunks by neighbouring lanes;
+        // what lies in the rows that do not exist reaches no other row
+        auto load_q = [&](const Info &x) {
             constexpr int kChunks = D / 8, kRows = 32 / kChunks;
-            const int64_t from = ok ? (int64_t)row * p.q_stride + head * D : 0;
-            const unsigned real = __ballot_sync(0xffffffffu, ok);
+            const int head = x.g[g].head, rows = x.g[g].rows, row0 = x.g[g].row0, head0 = x.head0;
             const int c = lane % kChunks;
+            const uint32_t to = q_at + g * C::kTile + (c >> 3) * 16384;
 #pragma unroll
             for (int i = 0; i < 32; i += kRows) {
-                const int rr = i + lane / kChunks;
-                const int64_t at = __shfl_sync(0xffffffffu, from, rr);
-                cp_async_16(q_at + g * C::kTile + (c >> 3) * 16384 + ((warp & 3) * 32 + rr) * 128 +
-                                (((c & 7) ^ (rr & 7)) << 4),
-                            static_cast<const T *>(p.q) + at + c * 8, (real >> rr) & 1);
+                const int rr = (warp & 3) * 32 + i + lane / kChunks;
+                const int t = token_of(head + rr);
+                if (rr < rows)
+                    cp_async_16(to + rr * 128 + (((c & 7) ^ (rr & 7)) << 4),
+                                static_cast<const T *>(p.q) + (row0 + t) * p.q_stride +
+                                    (head0 + head + rr - t * p.group) * D + c * 8);
             }
         };
         auto q_done = [&]() {
@@ -530,39 +589,49 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             fence_proxy_async_smem();
             mbar_arrive(bar_q);
         };
-        bool have = walk.next(s), go = true;
-        if (have) {
-            enter(s);
-            if (asked) {
-                load_q();
-                q_done();
-            }
+        bool go = described(0);
+        int most = go ? sm.info[0].most : -1, tiles = go ? sm.info[0].g[g].tiles : 0;
+        if (most > 0 && tiles > 0) {
+            load_q(sm.info[0]);
+            q_done();
         }
-        for (uint32_t seg = 0; have && go; ++seg) {
-            const int tiles = group_tiles(s, gkeys);
-            float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
-            int valid = keys - s.kt0 * kKeys;   // keys of the row from this tile on
-            const Segment was = s;
-            const int was_row = row, was_head = head, was_keys = keys, was_tiles = tiles_of(gkeys);
-            const bool was_ok = ok, was_asked = asked;
+        for (uint32_t seg = 0; go && most >= 0; ++seg) {
+            const Info &info = sm.info[seg % kRing];
+            const int rows = info.g[g].rows, head = info.g[g].head;
+            const int t = token_of(head + r);
+            const int keys = Plan::kDecode ? info.g[g].key0 : info.g[g].key0 + t;
+            const bool ok = r < rows;
+            const bool some = (warp & 3) * 32 < rows;      // the warp has a row
             // the next segment's queries: where this one's last scores are here, its queries are done with
-            auto ahead = [&]() {
-                have = walk.next(s);
-                asked = false;
-                if (have) {
-                    enter(s);
-                    if (asked)
-                        load_q();
-                }
+            int next_most = -1, next_tiles = 0;
+            auto ahead = [&]() -> bool {
+                if (!described(seg + 1))
+                    return false;
+                const Info &x = sm.info[(seg + 1) % kRing];
+                next_most = x.most;
+                next_tiles = next_most > 0 ? x.g[g].tiles : 0;
+                if (next_tiles > 0)
+                    load_q(x);
+                return true;
             };
+            float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
+            int valid = keys - info.kt0 * kKeys;   // keys of the row from this tile on
             for (int j = 0; j < tiles; ++j, valid -= kKeys) {
                 go = wait(bar_s, ph_s);
                 ph_s ^= 1;
                 if (!go)
                     break;
                 tc_fence_after();
-                if (j + 1 == tiles)
-                    ahead();
+                if (j + 1 == tiles) {
+                    go = ahead();
+                    if (!go)
+                        break;
+                }
+                if (!some) {
+                    tc_fence_before();
+                    mbar_arrive(bar_p);
+                    continue;
+                }
                 float x[kKeys];
 #pragma unroll
                 for (int c = 0; c < kKeys; c += 32)
@@ -632,26 +701,28 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             }
             if (!go)
                 break;
-            if (tiles == 0)
-                ahead();
-            if (was_asked) {
+            if (tiles == 0) {
+                go = ahead();
+            } else {
                 go = wait(bar_o, ph_o);
                 ph_o ^= 1;
-                if (!go)
-                    break;
-                tc_fence_after();
             }
-            if (asked)
+            if (!go)
+                break;
+            tc_fence_after();
+            if (next_tiles > 0)
                 q_done();
-            const bool marked = !Plan::kDecode && tiles > 0 &&
-                                (was.kt1 < was_tiles ? was.kt1 : was_tiles) * kKeys >
-                                    walk.common_keys(was) &&
-                                *(volatile int32_t *)&sm.marks.any[seg % C::kMarks] != 0;
-            const int32_t *const from = sm.marks.from[seg % C::kMarks];
-            const bool direct = was.whole && (!Plan::kDecode || p.prefix_len == 0);
-            if (direct) {
+            const int last = info.kt0 + tiles;             // behind the group's last tile here
+            const bool marked = !Plan::kDecode && tiles > 0 && last * kKeys > info.common &&
+                                *(volatile int32_t *)&sm.marks.any[seg % kRing] != 0;
+            const int32_t *const from = sm.marks.from[seg % kRing];
+            const int row = info.g[g].row0 + t, head_at = info.head0 + head + r - t * p.group;
+            const int64_t slot_at = info.slot;
+            if (!some) {
+                // nothing to write
+            } else if (slot_at < 0) {
                 const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-                T *const o = static_cast<T *>(p.o) + (int64_t)was_row * p.o_stride + was_head * D;
+                T *const o = static_cast<T *>(p.o) + row * p.o_stride + head_at * D;
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float a[32];
@@ -666,9 +737,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     if (marked) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            a[i] = was_keys > from[c + i] ? NAN : a[i];
+                            a[i] = keys > from[c + i] ? NAN : a[i];
                     }
-                    if (was_ok) {
+                    if (ok) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
                             *reinterpret_cast<uint4 *>(o + c + i) =
@@ -678,15 +749,13 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                                            Elem<T>::pack(a[i + 6] * inv, a[i + 7] * inv));
                     }
                 }
-                if (was_ok && p.lse != nullptr)
-                    p.lse[(int64_t)was_row * p.n_heads + was_head] =
+                if (ok && p.lse != nullptr)
+                    p.lse[(int64_t)row * p.n_heads + head_at] =
                         l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
             } else {
-                int rows = 0;
-                float *const slot = slot_of<D, NG, Plan>(p, was, cta, &rows);
-                const int at = g * 128 + r;
-                const bool put = at < rows && was_ok;
-                if (put)
+                float *const slot = p.part + slot_at;
+                const int at = g * 128 + r, slot_rows = info.slot_rows;
+                if (ok)
                     reinterpret_cast<float2 *>(slot)[at] = make_float2(m, l);
                 if (tiles > 0) {
 #pragma unroll
@@ -697,16 +766,16 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         if (marked) {
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                a[i] = was_keys > from[c + i] ? NAN : a[i];
+                                a[i] = keys > from[c + i] ? NAN : a[i];
                         }
-                        if (put && !Plan::kDecode) {
-                            float *const to = slot + pairs_floats(rows) + c * rows + at;
+                        if (ok && !Plan::kDecode) {
+                            float *const to = slot + pairs_floats(128 * NG) + c * 128 * NG + at;
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
-                                to[i * rows] = a[i];
-                        } else if (put) {
+                                to[i * 128 * NG] = a[i];
+                        } else if (ok) {
                             float *const to =
-                                slot + pairs_floats(rows) + (int64_t)at * D + c;
+                                slot + pairs_floats(slot_rows) + (int64_t)at * D + c;
 #pragma unroll
                             for (int i = 0; i < 32; i += 4)
                                 *reinterpret_cast<float4 *>(to + i) =
@@ -716,6 +785,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 }
             }
             tc_fence_before();
+            done_with(seg);
+            most = next_most;
+            tiles = next_tiles;
         }
     }
     tc_fence_before();

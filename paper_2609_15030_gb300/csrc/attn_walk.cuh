@@ -66,7 +66,7 @@ __host__ __device__ __forceinline__ int prefill_tiles(int pos0, int n_tokens, in
 template <class Plan, int NG>
 __host__ __device__ constexpr int extra_units()
 {
-    return Plan::kDecode ? 1 : 2;
+    return Plan::kDecode ? 0 : 2;
 }
 
 // one item's key tiles [kt0, kt1) as one CTA has them
@@ -332,17 +332,18 @@ __host__ __device__ __forceinline__ int64_t prefix_part_floats(const AttnParams 
     return (int64_t)(row_tiles<NG>(p.batch * p.group) * p.n_kv + p.ctas) * slot_floats<D>(128 * NG);
 }
 
+// where a segment's slot lies in the workspace, in floats
 template <int D, int NG, class Plan>
-__device__ __forceinline__ float *slot_of(const AttnParams &p, const Segment &s, int cta, int *rows)
+__device__ __forceinline__ int64_t slot_of(const AttnParams &p, const Segment &s, int cta, int *rows)
 {
     if (s.b < 0) {
         *rows = 128 * NG;
-        return p.part + (int64_t)(s.item + cta) * slot_floats<D>(128 * NG);
+        return (int64_t)(s.item + cta) * slot_floats<D>(128 * NG);
     }
     *rows = Plan::kDecode ? p.group : 128 * NG;
     if (Plan::kDecode && p.prefix_len > 0)
-        return p.part + prefix_part_floats<D, NG>(p) + (int64_t)(s.item + cta) * slot_floats<D>(*rows);
-    return p.part + (int64_t)(2 * cta + (s.kt0 == 0)) * slot_floats<D>(*rows);
+        return prefix_part_floats<D, NG>(p) + (int64_t)(s.item + cta) * slot_floats<D>(*rows);
+    return (int64_t)(2 * cta + (s.kt0 == 0)) * slot_floats<D>(*rows);
 }
 
 }  // namespace attn

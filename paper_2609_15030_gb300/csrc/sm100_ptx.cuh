@@ -122,12 +122,10 @@ __device__ __forceinline__ void prefetch_tensormap(const void *tmap)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
 }
 
-// 16 bytes of global memory to shared memory, zeros where `ok` is false (nothing is read then)
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src, bool ok)
+// 16 bytes of global memory to shared memory
+__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-                 "r"(ok ? 16 : 0)
-                 : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 __device__ __forceinline__ void cp_async_wait_all()
