@@ -55,7 +55,8 @@ hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
         return HS_ERR_INVALID_ARG;
     if (st != HS_OK)
         return st;
-    if (s.batch > HS_MAX_BATCH || s.n_heads / s.n_kv_heads > 128)
+    if (s.batch > HS_MAX_BATCH || s.n_heads / s.n_kv_heads > 128 || s.q_stride > INT32_MAX ||
+        s.o_stride > INT32_MAX)
         return HS_ERR_UNSUPPORTED;
     const int64_t inner = (int64_t)s.n_heads * s.head_dim;
     if ((s.q_stride != 0 && s.q_stride < inner) || (s.o_stride != 0 && s.o_stride < inner))
@@ -71,6 +72,8 @@ hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
     p.n_heads = s.n_heads;
     p.n_kv = s.n_kv_heads;
     p.group = s.n_heads / s.n_kv_heads;
+    p.by_group.set(p.group);
+    p.by_kv.set(p.n_kv);
     p.page_shift = page_shift(s.page_size);
     p.unsplit = s.unsplit;
     p.scale_log2 = s.scale * 1.4426950408889634f;

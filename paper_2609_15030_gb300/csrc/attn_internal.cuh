@@ -8,6 +8,25 @@ namespace hs {
 // most CTAs of one attention launch
 constexpr int kAttnMaxCtas = 320;
 
+// x / d for 0 <= x < 2^31 and 1 <= d < 2^31 as one multiplication: with mul = ceil(2^(31 + s) / d) and
+// 2^(s - 1) < d <= 2^s the product is too large by less than x / 2^31 of a 2^s-th, so its floor is x / d.
+struct Divisor {
+    uint32_t mul, shift;
+    int32_t d;
+    void set(int32_t by)
+    {
+        d = by;
+        shift = 0;
+        while ((int64_t)1 << shift < by)
+            ++shift;
+        mul = (uint32_t)((((uint64_t)1 << (31 + shift)) + (uint32_t)by - 1) / (uint32_t)by);
+    }
+    __device__ __forceinline__ int32_t div(int32_t x) const
+    {
+        return (int32_t)(((uint64_t)(uint32_t)x * mul) >> 31 >> shift);
+    }
+};
+
 // One attention call, passed by value to the kernels.  A decode step is the call in which every
 // request has one token, row b, and the lengths lie on the device.  (What only a prefill needs is a
 // parameter of its own: a launch moves all of them.)
@@ -40,6 +59,7 @@ struct AttnParams {
     int32_t parts;                // decode: about the most CTAs that share an item
     int32_t joined;               // partial results are left and joined
     float scale_log2;             // scale * log2(e)
+    Divisor by_group, by_kv;      // group, n_kv
 };
 
 // The requests of a prefill, and its schedule.

@@ -52,12 +52,18 @@ __host__ __device__ __forceinline__ int row_tiles(int rows)
     return (rows + 128 * NG - 1) / (128 * NG);
 }
 
+// prefill: keys of the last row before row `end` of a request
+__device__ __forceinline__ int keys_before(const AttnParams &p, int pos0, int end)
+{
+    return pos0 + p.by_group.div(end - 1) + 1;
+}
+
 // prefill: key tiles of a request's row tile
 template <int NG>
-__host__ __device__ __forceinline__ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
+int prefill_tiles(int pos0, int n_tokens, int group, int rt)
 {
-    const int64_t last = ((int64_t)(rt + 1) * 128 * NG - 1) / group;
-    return tiles_of(pos0 + (int)(last < n_tokens - 1 ? last : n_tokens - 1) + 1);
+    const int rows = n_tokens * group, end = (rt + 1) * 128 * NG;
+    return tiles_of(pos0 + ((end < rows ? end : rows) - 1) / group + 1);
 }
 
 // Units of an item before its tiles: what a segment costs beside them (its queries, the ends of its
@@ -102,7 +108,7 @@ struct Walk {
         if constexpr (Plan::kDecode)
             return len[b] > 0 ? tiles_of(len[b]) : 1;   // an empty row is written by someone
         else
-            return prefill_tiles<NG>(plan.req[b].pos0, plan.req[b].n, p.group, rt);
+            return tiles_of(keys_before(p, plan.req[b].pos0, min(rows(), (rt + 1) * 128 * NG)));
     }
     __device__ bool skip() const
     {
@@ -167,7 +173,7 @@ struct Walk {
         if constexpr (Plan::kDecode)
             return len[s.b];
         else
-            return plan.req[s.b].pos0 + ((s.rows - r0 < 128 ? s.rows : r0 + 128) - 1) / p.group + 1;
+            return keys_before(p, plan.req[s.b].pos0, min(s.rows, r0 + 128));
     }
     // the same of its last group that has rows
     __device__ int all_keys(const Segment &s) const
@@ -183,7 +189,7 @@ struct Walk {
         if constexpr (Plan::kDecode)
             return len[s.b];
         else
-            return plan.req[s.b].pos0 + s.rt * 128 * NG / p.group + 1;
+            return keys_before(p, plan.req[s.b].pos0, s.rt * 128 * NG + 1);
     }
 };
 
@@ -259,7 +265,7 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const PrefillPl
     s.left = first_unit(p.units, p.ctas, c + 1) - s.u;
     const PrefillPlan::Cta at = plan.cta[c];
     s.b = at.b;
-    s.rt = at.item / p.n_kv;
+    s.rt = p.by_kv.div(at.item);
     s.kvh = at.item - s.rt * p.n_kv;
     s.at = at.unit;
     return s;
