@@ -330,17 +330,23 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 return -1;
             return x.table[first >> p.page_shift];
         };
-        // a segment is described, and its first block ids requested, before the loads of the one in front
+        // a segment is described, and its first block ids requested, behind the first loads of the one in
+        // front
         Ahead now, then;
         bool go = describe(now);
         int32_t id = go ? block(now, now.kt0) : -1;
         while (go && now.tiles >= 0) {
-            go = describe(then);
-            if (!go)
-                break;
-            const int32_t then_id = block(then, then.kt0);
+            int32_t then_id = -1;
             const int tiles = now.tiles, keys = now.keys, common = now.common;
-            for (int j = 0; j < tiles && go; ++j) {
+            for (int j = 0; go && j < (tiles > 0 ? tiles : 1); ++j) {
+                if (j == (tiles > 1 ? 1 : 0)) {
+                    go = describe(then);
+                    if (!go)
+                        break;
+                    then_id = block(then, then.kt0);
+                    if (tiles == 0)
+                        break;
+                }
                 const int kt = now.kt0 + j;
                 const int32_t blk = id;
                 id = block(now, kt + 1);          // a tile ahead of its copies
