@@ -122,7 +122,9 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
         p.joined = 1;
         return (items + p.ctas) * slot(128 * p.groups) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
     }
-    p.joined = !p.unsplit && p.ctas > 1 && tiles_of(p.max_kv) > 1;
+    if (tiles_of(p.max_kv) + kExtra <= units / p.ctas + kJoinUnits)
+        p.unsplit = 1;
+    p.joined = !p.unsplit;
     return p.joined ? 2 * p.ctas * slot(p.group) : 0;
 }
 

@@ -71,7 +71,10 @@ struct PrefillPlan {
     struct Cta {                  // where its run of units begins
         int32_t b, item, unit, unused;   // item: row tile * n_kv + KV head; the unit of the item
     } cta[kAttnMaxCtas];
-    int16_t split_at[kAttnMaxCtas];      // CTAs whose run is the first to begin between an item's tiles
+    struct Split {                // an item whose tiles fall to the CTAs c0 to c1
+        int32_t item;
+        int16_t b, c0, c1, unused;
+    } split[kAttnMaxCtas];
 };
 
 // a decode step has all of it on the device

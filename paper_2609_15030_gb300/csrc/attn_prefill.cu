@@ -5,42 +5,46 @@ namespace hs {
 namespace attn {
 namespace {
 
-// prefill: block (x, y, z) takes 32 rows and 32 columns of the x-th item that is split between CTAs,
-// a lane a row and a warp four columns
-template <typename T, int D, int NG>
+// Block (x, y, z) takes 32 rows and 8 E columns of the x-th item that is split between CTAs, a lane a row
+// and a warp E columns: 4 where few items are split (of many parts each), all of them in one block
+// where many are (with 4 the 4,832 blocks of nine packed tails' 151 items took 11 us).
+template <typename T, int D, int NG, int E>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ PrefillPlan plan)
 {
-    constexpr int R = 128 * NG, kAhead = 8;
+    constexpr int R = 128 * NG, kAhead = 32 / E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Start st = find_start<NG>(p, plan, plan.split_at[blockIdx.x]);
-    const Walk<NG, PrefillPlan> w(p, plan, nullptr, st);
-    const int u0 = st.u - st.at + w.kExtra, u1 = u0 + w.tiles();      // the units of the item's tiles
-    const int c0 = cta_of(p.units, p.ctas, u0), c1 = cta_of(p.units, p.ctas, u1 - 1);
+    const PrefillPlan::Split it = plan.split[blockIdx.x];
+    const int rt = p.by_kv.div(it.item), kvh = it.item - rt * p.n_kv;
     const int64_t size = slot_floats<D>(R);
-    const int r = blockIdx.y * 32 + lane, rr = w.rt * R + r, col = blockIdx.z * 32 + warp * 4;
-    const bool on = rr < w.rows();
+    const int r = blockIdx.y * 32 + lane, rr = rt * R + r, col = (blockIdx.z * kMergeWarps + warp) * E;
+    const bool on = rr < plan.req[it.b].n * p.group;
+    const int t = p.by_group.div(on ? rr : 0), head = kvh * p.group + rr - t * p.group;
+    const int64_t row = plan.req[it.b].row0 + t;
     pdl_wait_and_release();
     if (!on)
         return;
     // part i of the item: CTA c0's last segment, then the first ones of the CTAs behind it
-    const float *const first = p.part + (2 * c0 + 1) * size, *const rest = p.part + 2 * c0 * size;
-    const int parts = c1 - c0 + 1;
-    float m = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+    const float *const first = p.part + (2 * it.c0 + 1) * size, *const rest = p.part + 2 * it.c0 * size;
+    const int parts = it.c1 - it.c0 + 1;
+    float m = -INFINITY, l = 0.f, a[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        a[e] = 0.f;
     for (int i0 = 0; i0 < parts; i0 += kAhead) {
         float2 ml[kAhead];
-        float v[kAhead][4];
+        float v[kAhead][E];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             ml[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < E; ++e)
                 v[i][e] = 0.f;
             if (i0 + i < parts) {
                 const float *const slot = i0 + i == 0 ? first : rest + 2 * (i0 + i) * size;
                 ml[i] = reinterpret_cast<const float2 *>(slot)[r];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < E; ++e)
                     v[i][e] = slot[pairs_floats(R) + (col + e) * R + r];
             }
         }
@@ -52,7 +56,7 @@ attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, const __grid_con
         m = top;
         l *= f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < E; ++e)
             a[e] *= f;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -62,15 +66,16 @@ attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, const __grid_con
             const float h = ex2(ml[i].x - top);
             l = fmaf(ml[i].y, h, l);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < E; ++e)
                 a[e] = fmaf(v[i][e], h, a[e]);
         }
     }
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-    const int t = rr / p.group, head = w.kvh * p.group + rr - t * p.group;
-    const int64_t row = plan.req[w.b].row0 + t;
-    *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + row * p.o_stride + head * D + col) =
-        make_uint2(Elem<T>::pack(a[0] * inv, a[1] * inv), Elem<T>::pack(a[2] * inv, a[3] * inv));
+    T *const o = static_cast<T *>(p.o) + row * p.o_stride + head * D + col;
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<uint2 *>(o + e) = make_uint2(Elem<T>::pack(a[e] * inv, a[e + 1] * inv),
+                                                       Elem<T>::pack(a[e + 2] * inv, a[e + 3] * inv));
     if (p.lse != nullptr && col == 0)
         p.lse[row * p.n_heads + head] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }
@@ -91,15 +96,20 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
 {
     constexpr int kExtra = extra_units<PrefillPlan, NG>();
     int64_t units = 0;
+    int longest = 0;
     for (int b = 0; b < p.batch; ++b)
-        for (int rt = 0; rt < row_tiles<NG>(plan.req[b].n * p.group); ++rt)
-            units += (int64_t)p.n_kv *
-                     (prefill_tiles<NG>(plan.req[b].pos0, plan.req[b].n, p.group, rt) + kExtra);
+        for (int rt = 0; rt < row_tiles<NG>(plan.req[b].n * p.group); ++rt) {
+            const int n = prefill_tiles<NG>(plan.req[b].pos0, plan.req[b].n, p.group, rt) + kExtra;
+            units += (int64_t)p.n_kv * n;
+            longest = n > longest ? n : longest;
+        }
     if (units > INT_MAX)
         return false;
     p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
     p.n_split = 0;
+    if (longest <= p.units / p.ctas + kJoinUnits)
+        p.unsplit = 1;
     int c = 0;
     int64_t u = 0, split = -1;
     for (int b = 0; b < p.batch && c < p.ctas; ++b)
@@ -111,10 +121,15 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
                 x.b = b;
                 x.item = rt * p.n_kv + (int)(v / n);
                 x.unit = (int)(v % n);
-                // the first run that begins between an item's tiles names it for the join
-                if (x.unit > kExtra && v / n * n + u != split) {
-                    split = v / n * n + u;
-                    plan.split_at[p.n_split++] = (int16_t)c;
+                // a run that begins between an item's tiles: the item is split
+                const int64_t item = u + v / n * n;
+                if (x.unit > kExtra && item != split) {
+                    split = item;
+                    PrefillPlan::Split &y = plan.split[p.n_split++];
+                    y.item = x.item;
+                    y.b = (int16_t)b;
+                    y.c0 = (int16_t)cta_of(p.units, p.ctas, (int)item + kExtra);
+                    y.c1 = (int16_t)cta_of(p.units, p.ctas, (int)item + n - 1);
                 }
             }
             u += (int64_t)n * p.n_kv;
@@ -128,8 +143,11 @@ cudaError_t launch(const AttnParams &p, const PrefillPlan &plan, cudaStream_t s)
     const cudaError_t e = launch_tc<T, D, NG>(p, plan, s);
     if (e != cudaSuccess || !p.joined)
         return e;
-    return launch_pdl(attn_merge_prefill_kernel<T, D, NG>, dim3((unsigned)p.n_split, 128 * NG / 32, D / 32),
-                      dim3(kMergeWarps * 32), 0, s, p, plan);
+    if (p.n_split > 64)
+        return launch_pdl(attn_merge_prefill_kernel<T, D, NG, D / kMergeWarps>,
+                          dim3((unsigned)p.n_split, 128 * NG / 32), dim3(kMergeWarps * 32), 0, s, p, plan);
+    return launch_pdl(attn_merge_prefill_kernel<T, D, NG, 4>,
+                      dim3((unsigned)p.n_split, 128 * NG / 32, D / 32), dim3(kMergeWarps * 32), 0, s, p, plan);
 }
 
 template <typename T>

@@ -77,6 +77,7 @@ struct Info {
         int32_t row0, key0;              // token row and keys of the group's first row's token
         int32_t head, rows;              // that row's head in the group; rows, at most 128
         int32_t keys, tiles;             // keys of its last row; its tiles in the segment
+        int32_t at, unused;              // its first row in the slot
     } g[2];
 };
 
@@ -288,12 +289,16 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 x.tiles = group_tiles(s, x.keys);
                 x.table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
                 if (lane < NG) {
-                    const int r0 = (s.rt * NG + lane) * 128, left = s.rows - r0;
+                    // a decode step's own items have one tile of rows: the groups have them in turn
+                    const bool own_item = Plan::kDecode && s.b >= 0;
+                    const int q = NG == 2 && own_item ? lane ^ (int)(seg & 1) : lane;
+                    const int r0 = (s.rt * NG + q) * 128, left = s.rows - r0;
                     const int t = s.b < 0 || !Plan::kDecode ? p.by_group.div(r0) : 0;
-                    const int own = walk.group_keys(s, lane);
+                    const int own = walk.group_keys(s, q);
                     info->g[lane].head = r0 - t * p.group;
                     info->g[lane].rows = left < 0 ? 0 : left < 128 ? left : 128;
                     info->g[lane].keys = own;
+                    info->g[lane].at = own_item ? 0 : lane * 128;
                     info->g[lane].tiles = group_tiles(s, own);
                     if constexpr (Plan::kDecode) {
                         info->g[lane].row0 = s.b < 0 ? t : s.b;
@@ -824,7 +829,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
             } else {
                 float *const slot = p.part + slot_at;
-                const int at = g * 128 + r, slot_rows = info.slot_rows;
+                const int at = info.g[g].at + r, slot_rows = info.slot_rows;
                 if (ok)
                     reinterpret_cast<float2 *>(slot)[at] = make_float2(m, l);
                 if (tiles > 0) {
@@ -899,13 +904,37 @@ __device__ __forceinline__ Joined<D> join_parts(const float *base, int count, in
 #pragma unroll
     for (int e = 0; e < E; ++e)
         x.a[e] = 0.f;
+    auto rows_of = [&](unsigned there, int64_t at_a, int j0, float (&v)[8][E]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = __shfl_sync(0xffffffffu, at_a, j0 + j);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                v[j][e] = 0.f;
+            if ((there >> (j0 + j)) & 1) {
+                if constexpr (E == 4) {
+                    const float4 y = *reinterpret_cast<const float4 *>(base + at + lane * 4);
+                    v[j][0] = y.x, v[j][1] = y.y, v[j][2] = y.z, v[j][3] = y.w;
+                } else {
+                    const float2 y = *reinterpret_cast<const float2 *>(base + at + lane * 2);
+                    v[j][0] = y.x, v[j][1] = y.y;
+                }
+            }
+        }
+    };
     for (int i0 = first; i0 < count; i0 += 32 * step) {
         const int i = i0 + lane * step;
         int64_t at_pair = 0, at_a = 0;
         float2 ml = make_float2(-INFINITY, 0.f);
-        if (i < count && part(i, at_pair, at_a))
+        const bool here = i < count && part(i, at_pair, at_a);
+        if (here)
             ml = *reinterpret_cast<const float2 *>(base + at_pair);
-        const bool live = !(ml.x == -INFINITY && ml.y == 0.f);   // else no key: its a is not written
+        const unsigned there = __ballot_sync(0xffffffffu, here);
+        const int last = 32 - __clz(there);
+        float v[8][E];
+        rows_of(there, at_a, 0, v);
+        // a part without a key of this row: what it holds of a means nothing
+        const bool live = !(ml.x == -INFINITY && ml.y == 0.f);
         float top = ml.x;
 #pragma unroll
         for (int w = 16; w > 0; w >>= 1)
@@ -913,7 +942,7 @@ __device__ __forceinline__ Joined<D> join_parts(const float *base, int count, in
         top = fmaxf(top, x.m);
         const float f = x.m == -INFINITY && x.l == 0.f ? 0.f : ex2(x.m - top);
         const float h = live ? ex2(ml.x - top) : 0.f;
-        float l = ml.y * h;
+        float l = live ? ml.y * h : 0.f;
 #pragma unroll
         for (int w = 16; w > 0; w >>= 1)
             l += __shfl_xor_sync(0xffffffffu, l, w);
@@ -923,31 +952,18 @@ __device__ __forceinline__ Joined<D> join_parts(const float *base, int count, in
         for (int e = 0; e < E; ++e)
             x.a[e] *= f;
         const unsigned any = __ballot_sync(0xffffffffu, live);
-        const int last = 32 - __clz(any);
         for (int j0 = 0; j0 < last; j0 += 8) {
-            float v[8][E], hj[8];
+            if (j0 > 0)
+                rows_of(there, at_a, j0, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int64_t at = __shfl_sync(0xffffffffu, at_a, j0 + j);
-                hj[j] = __shfl_sync(0xffffffffu, h, j0 + j);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    v[j][e] = 0.f;
+                const float hj = __shfl_sync(0xffffffffu, h, j0 + j);
                 if ((any >> (j0 + j)) & 1) {
-                    if constexpr (E == 4) {
-                        const float4 y = *reinterpret_cast<const float4 *>(base + at + lane * 4);
-                        v[j][0] = y.x, v[j][1] = y.y, v[j][2] = y.z, v[j][3] = y.w;
-                    } else {
-                        const float2 y = *reinterpret_cast<const float2 *>(base + at + lane * 2);
-                        v[j][0] = y.x, v[j][1] = y.y;
-                    }
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        x.a[e] = fmaf(v[j][e], hj, x.a[e]);
                 }
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    x.a[e] = fmaf(v[j][e], hj[j], x.a[e]);
         }
     }
     return x;

@@ -33,7 +33,7 @@ __host__ __device__ __forceinline__ int first_unit(int units, int ctas, int c)
 }
 
 // the CTA that has unit u: the largest c with first_unit(c) <= u
-__device__ __forceinline__ int cta_of(int units, int ctas, int u)
+__host__ __device__ __forceinline__ int cta_of(int units, int ctas, int u)
 {
     if (units < 1 << 22)
         return (int)(((uint32_t)(u + 1) * (uint32_t)ctas - 1) / (uint32_t)units);
@@ -74,6 +74,10 @@ __host__ __device__ constexpr int extra_units()
 {
     return Plan::kDecode ? 0 : 2;
 }
+
+// What a join costs, in tiles (2 to 4 us): a call whose longest item is no more than this above an even
+// share is not split.
+constexpr int kJoinUnits = 2;
 
 // one item's key tiles [kt0, kt1) as one CTA has them
 struct Segment {
