@@ -26,15 +26,14 @@ attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
         }
     }
     __syncthreads();
-    constexpr int kExtra = extra_units<DecodePlan, NG>();
-    const int per = prefix_units(p), own = item_units(len[b]);
+    const int per = prefix_units(p), own = item_units(p, len[b]);
     const int pre = per * p.n_kv * row_tiles<NG>(p.batch * p.group);
     const int units = pre + sums[1];
     const int u0 = pre + sums[0] + kvh * own;
     const int item = b * p.n_kv + kvh;
     const bool skip = len[b] < 0;
     // an unsplit item belongs to the CTA in whose run it begins, else the CTAs with its tiles have it
-    const int c0 = skip ? 0 : cta_of(units, p.ctas, p.unsplit ? u0 : u0 + kExtra);
+    const int c0 = skip ? 0 : cta_of(units, p.ctas, p.unsplit ? u0 : u0 + p.extra);
     const int c1 = skip || p.unsplit ? c0 : cta_of(units, p.ctas, u0 + own - 1);
     pdl_wait_and_release();
     if (skip || (per == 0 && c0 == c1))
@@ -49,7 +48,7 @@ attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
         const int pitem = rt * p.n_kv + kvh;
         int p0 = 0, p1 = -1;
         if (on && per > 0) {
-            p0 = cta_of(units, p.ctas, pitem * per + (p.unsplit ? 0 : kExtra));
+            p0 = cta_of(units, p.ctas, pitem * per + (p.unsplit ? 0 : p.extra));
             p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (pitem + 1) * per - 1);
         }
         const int n = p1 - p0 + 1;
@@ -108,8 +107,10 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
     auto slot = [&](int rows) {
         return (int64_t)sizeof(float) * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows));
     };
-    constexpr int kExtra = extra_units<DecodePlan, 1>();
-    const int64_t own = (int64_t)p.batch * p.n_kv * ((p.max_kv > 0 ? tiles_of(p.max_kv) : 1) + kExtra);
+    // 32 ragged requests: 53.6 us with 1 where 0 took 55; behind a shared prefix 8 and 64 requests took 11.2
+    // and 71 us with 0, 12.5 and 74.7 with 1
+    p.extra = p.prefix_len > 0 ? 0 : 1;
+    const int64_t own = (int64_t)p.batch * p.n_kv * ((p.max_kv > 0 ? tiles_of(p.max_kv) : 1) + p.extra);
     const int rows = p.batch * p.group;
     const int64_t items = (int64_t)p.n_kv * (p.groups == 2 ? row_tiles<2>(rows) : row_tiles<1>(rows));
     const int64_t units = own + items * prefix_units(p);
@@ -122,7 +123,7 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
         p.joined = 1;
         return (items + p.ctas) * slot(128 * p.groups) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
     }
-    if (tiles_of(p.max_kv) + kExtra <= units / p.ctas + kJoinUnits)
+    if (tiles_of(p.max_kv) + p.extra <= units / p.ctas + kJoinUnits)
         p.unsplit = 1;
     p.joined = !p.unsplit;
     return p.joined ? 2 * p.ctas * slot(p.group) : 0;

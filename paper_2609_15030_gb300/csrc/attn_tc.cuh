@@ -273,9 +273,16 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             int kt0, tiles, keys, common, kvh;
             const int32_t *table;
         };
+        // this lane's block id of a tile's pages
+        auto block = [&](const Ahead &x, int kt) -> int32_t {
+            const int first = kt * kKeys + lane * box;
+            if (kt >= x.kt0 + x.tiles || lane >= per || first >= x.keys)
+                return -1;
+            return x.table[first >> p.page_shift];
+        };
         // the next segment, described to the other warps; tiles = -1: there is none
         uint32_t seg = 0;
-        auto describe = [&](Ahead &x) -> bool {
+        auto describe = [&](Ahead &x, int32_t &id) -> bool {
             Info *const info = &sm.info[seg % kRing];
             const bool have = walk.next(s);
             x.tiles = -1;
@@ -288,6 +295,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 x.common = walk.common_keys(s);
                 x.tiles = group_tiles(s, x.keys);
                 x.table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
+                id = block(x, x.kt0);             // on its way while the segment is described
                 if (lane < NG) {
                     // a decode step's own items have one tile of rows: the groups have them in turn
                     const bool own_item = Plan::kDecode && s.b >= 0;
@@ -328,27 +336,19 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             ++seg;
             return true;
         };
-        // this lane's block id of a tile's pages
-        auto block = [&](const Ahead &x, int kt) -> int32_t {
-            const int first = kt * kKeys + lane * box;
-            if (kt >= x.kt0 + x.tiles || lane >= per || first >= x.keys)
-                return -1;
-            return x.table[first >> p.page_shift];
-        };
         // a segment is described, and its first block ids requested, behind the first loads of the one in
         // front
         Ahead now, then;
-        bool go = describe(now);
-        int32_t id = go ? block(now, now.kt0) : -1;
+        int32_t id = -1;
+        bool go = describe(now, id);
         while (go && now.tiles >= 0) {
             int32_t then_id = -1;
             const int tiles = now.tiles, keys = now.keys, common = now.common;
             for (int j = 0; go && j < (tiles > 0 ? tiles : 1); ++j) {
                 if (j == (tiles > 1 ? 1 : 0)) {
-                    go = describe(then);
+                    go = describe(then, then_id);
                     if (!go)
                         break;
-                    then_id = block(then, then.kt0);
                     if (tiles == 0)
                         break;
                 }

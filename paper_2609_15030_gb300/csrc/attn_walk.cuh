@@ -66,15 +66,6 @@ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
     return tiles_of(pos0 + ((end < rows ? end : rows) - 1) / group + 1);
 }
 
-// Units of an item before its tiles: what a segment costs beside them (its queries, the ends of its
-// pipeline, its outputs), in tiles.  Without them CTAs with many short items ended long after the
-// others: nine packed tails 104 us, with them XX.
-template <class Plan, int NG>
-__host__ __device__ constexpr int extra_units()
-{
-    return Plan::kDecode ? 0 : 2;
-}
-
 // What a join costs, in tiles (2 to 4 us): a call whose longest item is no more than this above an even
 // share is not split.
 constexpr int kJoinUnits = 2;
@@ -89,7 +80,6 @@ struct Segment {
 
 template <int NG, class Plan>
 struct Walk {
-    static constexpr int kExtra = extra_units<Plan, NG>();
     const AttnParams &p;
     const Plan &plan;
     const int32_t *len;                  // decode: the lengths in shared memory
@@ -138,7 +128,7 @@ struct Walk {
         : p(params), plan(plan_), len(lens), left(s.left), b(s.b), rt(s.rt), kvh(s.kvh), at(s.at)
     {
         if (p.unsplit && left > 0 && at != 0) {       // begins with the next whole item
-            left -= tiles() + kExtra - at;
+            left -= tiles() + p.extra - at;
             next_item();
         }
     }
@@ -146,11 +136,11 @@ struct Walk {
     {
         while (left > 0) {
             const int n = tiles();
-            int end = n + kExtra;
+            int end = n + p.extra;
             if (!p.unsplit && end - at > left)
                 end = at + left;
-            s.kt0 = at > kExtra ? at - kExtra : 0;
-            s.kt1 = end > kExtra ? end - kExtra : 0;
+            s.kt0 = at > p.extra ? at - p.extra : 0;
+            s.kt1 = end > p.extra ? end - p.extra : 0;
             s.b = b;
             s.rt = rt;
             s.kvh = kvh;
@@ -159,7 +149,7 @@ struct Walk {
             s.item = (b < 0 ? rt : b) * p.n_kv + kvh;
             left -= end - at;
             at = end;
-            if (at == n + kExtra)
+            if (at == n + p.extra)
                 next_item();
             if (s.kt1 > s.kt0)
                 return true;
@@ -206,20 +196,20 @@ __device__ __forceinline__ int group_tiles(const Segment &s, int keys)
 }
 
 // decode: units of an item of `len` keys, and of a request (0: its length is out of bounds)
-__device__ __forceinline__ int item_units(int len)
+__device__ __forceinline__ int item_units(const AttnParams &p, int len)
 {
-    return (len > 0 ? tiles_of(len) : 1) + extra_units<DecodePlan, 1>();
+    return (len > 0 ? tiles_of(len) : 1) + p.extra;
 }
 
 __device__ __forceinline__ int own_units(const AttnParams &p, int len)
 {
-    return len < 0 ? 0 : item_units(len) * p.n_kv;
+    return len < 0 ? 0 : item_units(p, len) * p.n_kv;
 }
 
 // units of an item of the shared prefix (0: there is none)
 __host__ __device__ __forceinline__ int prefix_units(const AttnParams &p)
 {
-    return p.prefix_len > 0 ? tiles_of(p.prefix_len) + extra_units<DecodePlan, 1>() : 0;
+    return p.prefix_len > 0 ? tiles_of(p.prefix_len) + p.extra : 0;
 }
 
 __device__ __forceinline__ int warp_scan(int x, int lane)
@@ -306,7 +296,7 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *
             const int first = __ffs(hit) - 1;
             v -= __shfl_sync(0xffffffffu, incl - x, first);
             s.b = b0 + first;
-            const int n = item_units(len[s.b]);
+            const int n = item_units(p, len[s.b]);
             s.kvh = v / n;
             s.at = v - s.kvh * n;
             return s;
