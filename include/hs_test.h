@@ -1,6 +1,6 @@
 /*
- * hs_test.h -- a fault-injection entry point for the failure-detection tests.
- * It is not part of the restore-and-resume path and no product code calls it.
+ * hs_test.h -- fault-injection entry points for the failure-detection tests.
+ * They are not part of the restore-and-resume path and no product code calls them.
  *
  * hs_test_prefill_stalled takes the arguments of hs_linattn_prefill_from_state
  * (hs.h) and requires shp->kernel == HS_LINATTN_CHUNKED_TC (else
@@ -29,6 +29,16 @@ hs_status hs_test_prefill_stalled(const hs_linattn_shape *shp, const uint16_t *q
                                   const int64_t *pos0, const int32_t *n_tokens,
                                   int32_t ckpt_interval, float *const *ckpt_slots, int32_t *d_err,
                                   cudaStream_t stream);
+
+/*
+ * hs_test_attn_stalled takes the arguments of hs_attn_prefill.  In every CTA the warp that issues the
+ * first rows' products first waits on an mbarrier that nothing completes; when that wait runs out
+ * (1 s) the CTA leaves through its abort path, as above, without writing an output of those rows.
+ */
+hs_status hs_test_attn_stalled(const hs_attn_shape *shp, const void *q, const void *cache,
+                               const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
+                               const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
+                               int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

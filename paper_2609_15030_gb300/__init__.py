@@ -54,7 +54,8 @@ EXPORTED = ("hs_status_string", "hs_version", "hs_align_prefix", "hs_restore_kv_
             "hs_test_prefill_stalled", "hs_linattn_prefill_scan", "hs_linattn_scan_workspace_bytes",
             "hs_linattn_prefill_scan_noalloc", "hs_kv_append", "hs_attn_prefill",
             "hs_attn_prefill_workspace_bytes", "hs_attn_decode", "hs_attn_decode_workspace_bytes",
-            "hs_attn_decode_shared", "hs_attn_decode_shared_workspace_bytes")
+            "hs_attn_decode_shared", "hs_attn_decode_shared_workspace_bytes",
+            "hs_test_attn_stalled")
 
 
 class HsError(RuntimeError):
@@ -116,6 +117,7 @@ def load() -> C.CDLL:
             ash = C.POINTER(hs_attn_shape)
             L.hs_kv_append.argtypes = [ash, vp, vp, i64, vp, i64, vp, vp, vp]
             L.hs_attn_prefill.argtypes = [ash, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+            L.hs_test_attn_stalled.argtypes = L.hs_attn_prefill.argtypes
             L.hs_attn_prefill_workspace_bytes.argtypes = [ash, vp, vp, vp]
             L.hs_attn_decode.argtypes = [ash, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp]
             L.hs_attn_decode_workspace_bytes.argtypes = [ash, i64, vp]
@@ -415,18 +417,32 @@ def hs_attn_prefill_workspace_bytes(shape: hs_attn_shape, pos0, n_tokens) -> int
     return out.value
 
 
-def hs_attn_prefill(shape: hs_attn_shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows,
-                    workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
-    """Causal attention of packed tails over the paged cache.  pos0 / n_tokens / cu_rows: host
-    sequences of length batch, batch, batch + 1; lse may be None."""
+def _attn_prefill_call(name, shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows, workspace,
+                       workspace_bytes, d_err, stream):
     B = int(shape.batch)
     p0, keep_p0 = _i64(pos0, B)
     nt, keep_nt = _i32(n_tokens, B)
     cu, keep_cu = _i64(cu_rows, B + 1)
-    rc = (_lib or load()).hs_attn_prefill(
+    rc = getattr(_lib or load(), name)(
         C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(o), _ptr(lse), p0, nt, cu,
         _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
-    _check(rc, "hs_attn_prefill")
+    _check(rc, name)
+
+
+def hs_attn_prefill(shape: hs_attn_shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows,
+                    workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """Causal attention of packed tails over the paged cache.  pos0 / n_tokens / cu_rows: host
+    sequences of length batch, batch, batch + 1; lse may be None."""
+    _attn_prefill_call("hs_attn_prefill", shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows,
+                       workspace, workspace_bytes, d_err, stream)
+
+
+def hs_test_attn_stalled(shape: hs_attn_shape, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows,
+                         workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """Failure-detection hook (include/hs_test.h): hs_attn_prefill with one wait per CTA that nothing
+    completes; it reports HS_DEVERR_TIMEOUT."""
+    _attn_prefill_call("hs_test_attn_stalled", shape, q, cache, block_table, o, lse, pos0, n_tokens,
+                       cu_rows, workspace, workspace_bytes, d_err, stream)
 
 
 def hs_attn_decode_workspace_bytes(shape: hs_attn_shape, max_kv_len: int) -> int:

@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "attn_internal.cuh"
+#include "hs_test.h"
 
 namespace {
 
@@ -96,7 +97,6 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
                         hs::PrefillPlan &plan, bool *any)
 {
     *any = false;
-    std::memset(&plan, 0, sizeof plan);
     if (s.batch == 0)
         return HS_OK;
     if (pos0 == nullptr || n_tokens == nullptr || (rows && cu_rows == nullptr))
@@ -112,6 +112,7 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
             return HS_ERR_INVALID_ARG;
     }
     for (int32_t b = 0; b < s.batch; ++b) {
+        plan.req[b] = {};
         if (n_tokens[b] == 0)
             continue;
         *any = true;
@@ -221,10 +222,11 @@ hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, i
                                             shp->num_blocks, d_err, sms, stream));
 }
 
-hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *cache,
-                          const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
-                          const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
-                          int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream)
+static hs_status prefill(const hs_attn_shape *shp, const void *q, const void *cache,
+                         const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
+                         const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
+                         int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream,
+                         bool stall_for_test)
 {
     hs::AttnParams p;
     hs::PrefillPlan plan;
@@ -240,6 +242,7 @@ hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *c
     p.o = o;
     p.lse = lse;
     p.d_err = d_err;
+    p.stall_for_test = stall_for_test;
     st = check_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
@@ -250,6 +253,24 @@ hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *c
     if (st != HS_OK)
         return st;
     return cuda_status(hs::launch_attn_prefill(p, plan, shp->head_dim, shp->dtype, stream));
+}
+
+hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *cache,
+                          const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
+                          const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
+                          int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream)
+{
+    return prefill(shp, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows, workspace, workspace_bytes,
+                   d_err, stream, false);
+}
+
+hs_status hs_test_attn_stalled(const hs_attn_shape *shp, const void *q, const void *cache,
+                               const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
+                               const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
+                               int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream)
+{
+    return prefill(shp, q, cache, block_table, o, lse, pos0, n_tokens, cu_rows, workspace, workspace_bytes,
+                   d_err, stream, true);
 }
 
 hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_t *pos0,

