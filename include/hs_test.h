@@ -19,6 +19,7 @@
 #define HS_TEST_H
 
 #include "hs.h"
+#include "hs_attn.h"
 
 #ifdef __cplusplus
 extern "C" {

@@ -1,7 +1,7 @@
 """Python binding of libhs (checkpoint-aligned restore-and-resume, sm_103a).
 
 Argument marshalling only: every function forwards to the C entry point of
-the same name in ``libhs.so`` (declared in ``include/hs.h``); all GPU work
+the same name in ``libhs.so`` (declared in ``include/hs.h`` and ``include/hs_attn.h``); all GPU work
 runs in the library's kernels.  Tensors are accepted wherever the C call
 takes a pointer (their ``data_ptr()`` is passed); plain ints are passed as
 addresses.  A non-OK status raises ``HsError``.

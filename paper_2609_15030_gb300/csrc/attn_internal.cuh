@@ -1,9 +1,19 @@
 // Declarations shared by the full-attention calls (attn_api.cu) and their kernels.
 #pragma once
 
+#include "hs_attn.h"
 #include "hs_internal.cuh"
 
 namespace hs {
+
+// the current device's SM count, queried once per device (hs_api.cu)
+hs_status device_sm_count(int *out);
+
+// the release of programmatic dependents alone, for a kernel that has waited before
+__device__ __forceinline__ void pdl_release()
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 
 // most CTAs of one attention launch
 constexpr int kAttnMaxCtas = 320;

@@ -26,6 +26,16 @@
 // wherever some row of the tile does not attend: rows behind the last key are zeroed in shared
 // memory, and keys that only some rows see (the causal diagonal) are searched; a value there that
 // is not finite is zeroed and noted, and the rows that do see it get NaN in its column at the end.
+//
+// What bounds it.  A key tile's two products take a group 533 ns of tensor core (M = N = 128, 8,192
+// operations a clock, 1.92 GHz), its softmax 650 ns (128 exponentials a thread at 8 lanes a clock
+// and scheduler take 270; the rest are maxima, sums, conversions and the passage through TMEM), and
+// some 250 ns go into the hand-overs, so a pair of tiles takes 1.45 us where the tensor core alone
+// would take 1.07; with a shorter softmax (two threads to a row) registers spilled and it took 2.3.
+// Two 16k-token prompts of 32 heads: 2.87 ms, 1,530 TFLOP/s, at the power limit (a cuBLAS product
+// sustains 1,692 there).  A decode step is bound by HBM where its contexts are long (four requests at
+// 98k to 131k keys: 269 us, 7.0 TB/s), a short call by latency: 3.5 us until the first scores, 0.7 us
+// of softmax, 2 us for sums of 256 rows that go to the workspace, 3 to 4 us for the join.
 #pragma once
 
 #include <cuda.h>
@@ -33,8 +43,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "attn_ptx.cuh"
 #include "attn_walk.cuh"
-#include "sm100_ptx.cuh"
 
 namespace hs {
 namespace attn {
@@ -233,8 +243,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
     if (warp == C::kSoftmax)
         tmem_alloc(smem_u32(&sm.tmem), C::kTmemCols);
     pdl_wait();
-    // a decode step's join takes its place as CTAs end (one step 10.2 us instead of 10.6; a prefill's does
-    // not: drafts 13.9 us instead of 15.4)
+    // a decode step's join takes its place as CTAs end (one step 10.2 us instead of 10.6); a prefill's does
+    // not (packed drafts 13.9 us instead of 15.4)
     if (Plan::kDecode && p.joined)
         pdl_release();
     tc_fence_before();
@@ -251,9 +261,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             mbar_arrive(smem_u32(&sm.info_empty[k % kRing]));
     };
 
-    if (warp >= C::kSoftmax) {
-    fewer_registers<C::kLessRegs>();
     if (warp == C::kSoftmax + 3) {
+        fewer_registers<C::kLessRegs>();
         // ---- the walk, and loads: key and value tiles in turn through the stages
         Start start;
         if constexpr (Plan::kDecode) {
@@ -402,7 +411,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     mbar_wait_bounded(full(at), (i / kSt) & 1, kTimeoutNs);
             }
         }
-    } else if (warp < C::kSoftmax + NG) {
+    } else if (warp >= C::kSoftmax && warp < C::kSoftmax + NG) {
+        fewer_registers<C::kLessRegs>();
         // ---- MMAs, a warp to a group, in the order QK(0), PV(0), QK(1), PV(1), ...: the scores of the
         // next tile overwrite the weights of the last one behind the product that reads them.  A stage
         // is free once both groups are done with it
@@ -450,7 +460,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             if (!go)
                 break;
             const Info &info = sm.info[seg % kRing];
-            const int most = info.most, mine = info.g[g].tiles, both = NG == 2 ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
+            const int most = info.most, mine = info.g[g].tiles;
+            const int both = NG == 2 ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
             int left = info.g[g].keys - info.kt0 * kKeys;
             done_with(seg);
             if (most < 0)
@@ -522,7 +533,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             }
             __syncwarp();
         }
-    } else {
+    } else if (warp >= C::kSoftmax) {
+        fewer_registers<C::kLessRegs>();
         // ---- values at masked places: the warps that are left
         constexpr int kWho = (3 - NG) * 32;
         uint32_t st_v = 1, ph_raw = 0;         // the stage of the next value tile
@@ -614,7 +626,6 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             if (go)
                 done_with(seg);
         }
-    }
     } else {
         // ---- softmax: thread = row
         more_registers<C::kMoreRegs>();

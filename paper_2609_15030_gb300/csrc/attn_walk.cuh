@@ -313,11 +313,11 @@ __device__ __forceinline__ Start find_start(const AttnParams &p, const int32_t *
 // ---- partial results -----------------------------------------------------------------------
 //
 // A slot holds R rows: R pairs (m, l), padded to 16 bytes, then the sums a: of decode R rows of D
-// floats, of prefill D columns of R (a warp stores 32 rows of a column, and the join reads them so).  Without a shared prefix an item
-// leaves a partial result in at most two places of a CTA's run: at its beginning, where it does not
-// start the item (slot 2 cta), and at its end, where it does (slot 2 cta + 1).  Behind a shared
-// prefix every segment is partial; its slot is item + cta, which no other segment of its part
-// (prefix, requests) has, since both only grow along the run.
+// floats, of prefill D columns of R (a warp stores 32 rows of a column, and the join reads them so).
+// Without a shared prefix an item leaves a partial result in at most two places of a CTA's run: at its
+// beginning, where it does not start the item (slot 2 cta), and at its end, where it does (slot
+// 2 cta + 1).  Behind a shared prefix every segment is partial; its slot is item + cta, which no other
+// segment of its part (prefix, requests) has, since both only grow along the run.
 
 __host__ __device__ __forceinline__ int pairs_floats(int rows)
 {

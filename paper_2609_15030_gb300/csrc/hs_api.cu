@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cstring>
 
+#include "attn_internal.cuh"
 #include "gla_dstate.cuh"
 #include "hs_internal.cuh"
 #include "hs_test.h"

@@ -35,12 +35,6 @@ __device__ __forceinline__ void pdl_wait()
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// the release alone, for a kernel that has waited before
-__device__ __forceinline__ void pdl_release()
-{
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                               cudaStream_t stream, Args &&...args)
@@ -122,9 +116,6 @@ struct GlaParams {
                                     // start state in state
     int32_t row0[HS_MAX_BATCH];     // token row of the problem's first token in q/k/v/log_g/o
 };
-
-// the current device's SM count, queried once per device (hs_api.cu)
-hs_status device_sm_count(int *out);
 
 // launchers (return the launch's cudaError_t)
 cudaError_t launch_kv_scatter(const void *const *staging, void *const *cache, int32_t n_layers,

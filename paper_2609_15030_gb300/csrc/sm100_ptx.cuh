@@ -73,19 +73,6 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
     }
 }
 
-// registers per thread of this warpgroup (all four of its warps), out of those the block was launched with
-template <int N>
-__device__ __forceinline__ void more_registers()
-{
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-template <int N>
-__device__ __forceinline__ void fewer_registers()
-{
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
 // ---------------------------------------------------------------- TMA
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, int32_t x, int32_t y,
@@ -105,32 +92,6 @@ __device__ __forceinline__ void tma_prefetch_2d(const void *tmap, int32_t x, int
                      reinterpret_cast<uint64_t>(tmap)),
                  "r"(x), "r"(y)
                  : "memory");
-}
-
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t y,
-                                            int32_t z, int32_t w, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
-        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
-        : "memory");
-}
-
-__device__ __forceinline__ void prefetch_tensormap(const void *tmap)
-{
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
-}
-
-// 16 bytes of global memory to shared memory
-__device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
-__device__ __forceinline__ void cp_async_wait_all()
-{
-    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 __device__ __forceinline__ void fence_proxy_async_smem()
@@ -214,13 +175,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
     return r;
 }
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 // a value all lanes of the warp agree on, known to the compiler as warp-uniform
 __device__ __forceinline__ int uniform(int x)
 {
@@ -299,28 +253,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&u)[16
         : "memory");
 }
 
-// 32 lanes x one column
-__device__ __forceinline__ void tmem_st1(uint32_t taddr, float x)
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(x) : "memory");
-}
-
-// 32 lanes x 8 consecutive 32-bit columns
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&u)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
-                 "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
-                 : "memory");
-}
-
-// valid behind tmem_wait_ld
-__device__ __forceinline__ float tmem_ld1(uint32_t taddr)
-{
-    float x;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=f"(x) : "r"(taddr));
-    return x;
-}
-
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&u)[16])
 {
     asm volatile(
@@ -362,12 +294,6 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uin
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, int b_mn = 0)
 {
     return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-
-// the same with bf16 A and B (format 1)
-__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn = 0)
-{
-    return idesc_f16(M, N, b_mn) | (1u << 7) | (1u << 10);
 }
 
 __device__ __forceinline__ void tmem_wait_ld()
