@@ -123,7 +123,7 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
         p.joined = 1;
         return (items + p.ctas) * slot(128 * p.groups) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
     }
-    if (better_whole(p, tiles_of(p.max_kv), units))
+    if (better_whole(p, (int64_t)p.batch * p.n_kv, tiles_of(p.max_kv), units))
         p.unsplit = 1;
     p.joined = !p.unsplit;
     return p.joined ? 2 * p.ctas * slot(p.group) : 0;

@@ -97,12 +97,13 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
     // Without this CTAs with many short items end long after the others: nine packed tails took 85 us with 1
     // unit where 2 took 75, 3 take 53.6 where 2 took 54.5; 4 cost two 16k-token prompts 2 %.
     p.extra = 3;
-    int64_t units = 0;
+    int64_t units = 0, items = 0;
     int longest = 0;
     for (int b = 0; b < p.batch; ++b)
         for (int rt = 0; rt < row_tiles<NG>(plan.req[b].n * p.group); ++rt) {
             const int n = prefill_tiles<NG>(plan.req[b].pos0, plan.req[b].n, p.group, rt) + p.extra;
             units += (int64_t)p.n_kv * n;
+            items += p.n_kv;
             longest = n > longest ? n : longest;
         }
     if (units > INT_MAX)
@@ -110,7 +111,7 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
     p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
     p.n_split = 0;
-    if (better_whole(p, longest - p.extra, units))
+    if (better_whole(p, items, longest - p.extra, units))
         p.unsplit = 1;
     int c = 0;
     int64_t u = 0, split = -1;
@@ -174,8 +175,8 @@ int64_t plan_attn_prefill(AttnParams &p, PrefillPlan &plan, int d, int sm_count)
         return -1;
     p.joined = !p.unsplit && p.n_split > 0;
     const int rows = 128 * p.groups;
-    return p.joined ? (int64_t)sizeof(float) * 2 * p.ctas * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows))
-                    : 0;
+    const int64_t slot = (int64_t)sizeof(float) * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows));
+    return p.joined ? 2 * p.ctas * slot : 0;
 }
 
 cudaError_t launch_attn_prefill(const AttnParams &p, const PrefillPlan &plan, int d, int dtype,

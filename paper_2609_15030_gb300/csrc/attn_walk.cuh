@@ -67,11 +67,13 @@ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
 }
 
 // Whether a call is better not split: a join costs what 3 tiles cost (2 to 4 us), and a second launch
-// its host time.  One request of 2 heads with 256 keys: 6.9 us a call, host bound, instead of 9.1 split.
-inline bool better_whole(const AttnParams &p, int longest, int64_t units)
+// its host time; whole items leave a CTA at most the longest above an even share (with an item or less
+// to each, the longest).  One request of 2 heads with 256 keys: 6.9 us a call, host bound, instead of 9.1
+// split.
+inline bool better_whole(const AttnParams &p, int64_t items, int longest, int64_t units)
 {
-    const int64_t share = units / p.ctas - p.extra;
-    return longest <= (share > 1 ? share : 1) + 3;
+    const int64_t even = units / p.ctas - p.extra, share = even > 1 ? even : 1;
+    return (items <= p.ctas ? 0 : share) + longest <= share + 3;
 }
 
 // one item's key tiles [kt0, kt1) as one CTA has them

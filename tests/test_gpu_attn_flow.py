@@ -222,11 +222,13 @@ def test_blocks_beyond_4_gib_of_a_cache(dev):
 
 
 def test_workspaces_that_are_too_small_are_refused(dev):
-    shape = hs.make_attn_shape(1, 4, 1, 128, 16, 1000, 400)
+    # 240 items of many keys: shared out over CTAs, whose sums go through the workspace
+    B = 30
+    shape = hs.make_attn_shape(B, 32, 8, 128, 16, 1000, 400)
+    lens, cu = ([4000] * B, [40] * B), [40 * b for b in range(B + 1)]
     for size, call in (
-            (hs.hs_attn_prefill_workspace_bytes(shape, [4000], [40]),
-             lambda ws, n: hs.hs_attn_prefill(shape, 1 << 20, 1 << 20, 1 << 20, 1 << 20, None, [4000], [40],
-                                              [0, 40], ws, n)),
+            (hs.hs_attn_prefill_workspace_bytes(shape, *lens),
+             lambda ws, n: hs.hs_attn_prefill(shape, 1 << 20, 1 << 20, 1 << 20, 1 << 20, None, *lens, cu, ws, n)),
             (hs.hs_attn_decode_workspace_bytes(shape, 6000),
              lambda ws, n: hs.hs_attn_decode(shape, 1 << 20, 1 << 20, 1 << 20, 1 << 20, 6000, 1 << 20, None,
                                              ws, n)),
