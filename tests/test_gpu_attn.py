@@ -28,7 +28,7 @@ def dev():
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("kv_heads,d,page,rows,pad", [
     (1, 64, 16, 1, 0), (2, 64, 16, 33, 8), (4, 128, 16, 257, 512), (8, 128, 32, 1000, 0),
-    (3, 128, 64, 77, 24), (4, 64, 256, 600, 0)])
+    (3, 128, 64, 77, 24), (4, 64, 256, 600, 0), (72, 128, 16, 5, 8), (200, 64, 16, 40, 0)])
 def test_append_writes_each_row_to_its_slot(dev, dtype, kv_heads, d, page, rows, pad):
     g = torch.Generator().manual_seed(rows)
     dt = DT[dtype]
@@ -173,6 +173,85 @@ def test_prefill_reports_pages_outside_the_cache(dev):
         assert ((got - good[r][1]).abs() <= good[r][3]).all(), r
     p.table[0, 3] = -7
     assert run_prefill(p, [0, 0], [100, 50], dev).err.item() == hs.HS_DEVERR_BLOCK_OOB
+
+
+@pytest.mark.parametrize("at", [0, 100, 140])
+def test_prefill_keeps_later_keys_out_of_earlier_rows(dev, at):
+    """A key of NaN reaches the rows at and behind its position."""
+    n = 150
+    p = Problem(21, 2, 1, 128, 16, "fp16", [n], n)
+    clean = run_prefill(p, [0], [n], dev)
+    p.cache[p.table[0, at // 16].item(), 0, at % 16] = math.nan
+    out = run_prefill(p, [0], [n], dev)
+    assert torch.equal(out.o[:at].view(torch.int16), clean.o[:at].view(torch.int16))
+    assert torch.equal(out.lse[:at], clean.lse[:at])
+    assert torch.isnan(out.o[at:n, :256]).all()
+
+
+def test_prefill_keeps_a_bad_query_to_itself(dev):
+    p = Problem(22, 4, 2, 128, 16, "bf16", [300], 40)
+    clean = run_prefill(p, [260], [40], dev)
+    p.q[7, 130] = math.nan            # token 7, head 1
+    p.q[20, 0] = math.inf             # token 20, head 0
+    out = run_prefill(p, [260], [40], dev)
+    o, ref = (x.o[:40, :512].reshape(40, 4, 128).cpu() for x in (out, clean))
+    bad = torch.zeros(40, 4, dtype=torch.bool)
+    bad[7, 1] = bad[20, 0] = True
+    assert torch.isnan(o[bad]).all()
+    assert torch.equal(o[~bad].view(torch.int16), ref[~bad].view(torch.int16))
+
+
+@pytest.mark.parametrize("unsplit", [False, True])
+def test_prefill_of_the_largest_batch(dev, unsplit):
+    """384 requests of 0 to 3 tokens, the first and last without one, some tables sharing pages."""
+    n = [0] + [(5 * b) % 4 for b in range(1, 383)] + [0]
+    pos0 = [(41 * b) % 150 for b in range(384)]
+    p = Problem(23, 6, 2, 64, 16, "bf16", [a + b for a, b in zip(pos0, n)], sum(n))
+    for b in range(4, 384, 4):        # the pages in front of the new tokens are another request's
+        whole = min(pos0[b], pos0[b - 1]) // 16
+        p.table[b, :whole] = p.table[b - 1, :whole]
+        for x in (p.K, p.V):
+            x[b][:whole * 16] = x[b - 1][:whole * 16]
+    run_prefill(p, pos0, n, dev, unsplit=unsplit).check(p.prefill_rows(pos0, n, cu_of(n)))
+
+
+@pytest.mark.parametrize("scale", [0.003, 0.7])
+def test_scales(dev, scale):
+    p = Problem(24, 4, 2, 64, 16, "fp16", [333, 20], 25)
+    p.scale = scale
+    run_prefill(p, [310, 18], [23, 2], dev, scale=scale).check(p.prefill_rows([310, 18], [23, 2], [0, 23, 25]))
+
+
+def test_captured_prefill_and_shared_decode_replay_with_new_contents(dev):
+    """The lists of a captured prefill are part of the graph; queries, pages and tables are read anew."""
+    pos0, n = [700, 3], [90, 40]
+    a, b = (Problem(25 + i, 8, 2, 128, 16, "bf16", [790, 43], 130, prefix_len=200) for i in range(2))
+    shape, side = a.shape(2), torch.cuda.Stream()
+    size = max(hs.hs_attn_prefill_workspace_bytes(shape, pos0, n),
+               hs.hs_attn_decode_shared_workspace_bytes(shape, 200, 790))
+    q, cache, table, pre = (x.to(dev) for x in (a.q, a.cache, a.table, a.prefix_table))
+    lens = torch.tensor([790, 43], dtype=torch.int32, device=dev)
+    ws, err = workspace(size, dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    o, o2 = torch.zeros_like(q), torch.zeros_like(q)
+    lse, lse2 = (torch.zeros(131, 8, device=dev) for _ in range(2))
+
+    def calls():
+        hs.hs_attn_prefill(shape, q, cache, table, o, lse, pos0, n, [0, 90, 130], ws, size, err, side)
+        hs.hs_attn_decode_shared(shape, q, cache, pre, 200, table, lens, 790, o2, lse2, ws, size, err, side)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for p in (a, b, a):
+        for x, y in ((q, p.q), (cache, p.cache), (table, p.table), (pre, p.prefix_table)):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert err.item() == 0
+        for got, rows in ((o, p.prefill_rows(pos0, n, [0, 90, 130])), (o2, p.decode_rows([790, 43]))):
+            for r, want, _, bound, _ in rows:
+                assert ((got[r, :1024].cpu().double().reshape(8, 128) - want).abs() <= bound).all(), r
+    assert guarded(ws, size)
 
 
 # ---- decode --------------------------------------------------------------------------------
