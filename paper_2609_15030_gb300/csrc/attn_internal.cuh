@@ -48,7 +48,7 @@ struct AttnParams {
     const int32_t *kv_len;        // decode: device lengths; prefill: nullptr
     void *o;
     float *lse;                   // or nullptr
-    float *part;                  // workspace: partial results (see attn.cu)
+    float *part;                  // workspace: partial results (attn_walk.cuh)
     int32_t *d_err;
     int64_t num_blocks;
     int64_t max_pages;

@@ -6,10 +6,12 @@
 //
 // Mathematics, per row, with s_j = scale * log2(e) * q . k_j:  m is a number near max s_j,
 // l = sum 2^(s_j - m), a = sum 2^(s_j - m) v_j, all float32;  o = a / l, lse = ln 2 (m + log2 l).
-// m follows the maximum lazily: only when a tile's maximum exceeds it by more than 8 are l and a
-// rescaled by 2^(m_old - m_new) (weights then reach 2^8 at most, and nothing is lost: the scale
-// of 16-bit weights is free).  Weights are rounded to the element type for the product with v (the
-// tensor core takes 16-bit operands); l sums them before that rounding.
+// m follows the maximum lazily: only when a tile's maximum exceeds it by more than 8 (fp16: 15) are l
+// and a rescaled by 2^(m_old - m_new), and nothing is lost, since the scale of 16-bit weights is free.  In
+// fp16 m is then set 8 below the maximum: weights lie between 2^15 and 2^-24, so that a key's is rounded
+// to nothing only below 2^-33 of the largest (with m at the maximum, many keys of 2^-25 each were lost).
+// Weights are rounded to the element type for the product with v (the tensor core takes 16-bit
+// operands); l sums them before that rounding.
 //
 // Schedule.  The units of all items in order are shared out evenly over the CTAs, each a
 // contiguous run, so that one long request or many ragged ones fill the SMs alike.  An item whose
@@ -52,7 +54,6 @@ namespace attn {
 using namespace ptx;
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLazy = 8.0f;            // log2 of the largest weight
 constexpr uint64_t kTimeoutNs = 1000000000ull;
 
 // ---- shapes of a launch --------------------------------------------------------------------
@@ -128,6 +129,7 @@ struct Elem;
 template <>
 struct Elem<__nv_bfloat16> {
     static constexpr uint32_t kExp = 0x7F807F80u, kOne = 0x00800080u;
+    static constexpr float kMost = 8.f, kBelow = 0.f;       // log2 of the largest weight, of a new m's
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         uint32_t r;
@@ -139,6 +141,7 @@ struct Elem<__nv_bfloat16> {
 template <>
 struct Elem<__half> {
     static constexpr uint32_t kExp = 0x7C007C00u, kOne = 0x04000400u;
+    static constexpr float kMost = 15.f, kBelow = 8.f;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         uint32_t r;
@@ -726,11 +729,11 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 t0 = max3(t0, x[124], x[125]);
                 t1 = max3(t1, x[126], x[127]);
                 const float top = max3(t0, t1, fmaxf(t2, t3)) * p.scale_log2;
-                const bool up = top > m + kLazy;
+                const bool up = top > m + Elem<T>::kMost;
                 if (__any_sync(0xffffffffu, up)) {
-                    const float f = up ? ex2(m - top) : 1.f;
+                    const float f = up ? ex2(m - (top - Elem<T>::kBelow)) : 1.f;
                     if (up)
-                        m = top;
+                        m = top - Elem<T>::kBelow;
                     if (j > 0) {
                         // the previous product is done: the scores came after it
                         l *= f;

@@ -391,3 +391,51 @@ def test_calls_at_once_on_two_streams(dev):
                                out.err, s)
     for p, out, h in zip(ps, outs, held):
         out.check(p.prefill_rows(h[6], h[7], [0, 1, 2]))
+
+
+# ---- small weights -------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("at", [0, 2500, 4999])
+@pytest.mark.parametrize("call", ["prefill", "unsplit", "decode", "shared"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_many_small_weights_beside_a_large_one(dev, dtype, call, at):
+    """4,999 keys with 2^-25.5 of the weight of one more each, below half the smallest fp16 number: the
+    values of the small ones are 1, of the large one 0.  Weights are rounded with 2^8 of room below the
+    largest, so that one of 2^-25.5 is off by at most half a step of 2^-24 beside 2^-17.5, which is 2^-7.5 of
+    it; the output, near 2^-13.2, is rounded in steps of 2^-24 in fp16, by 2^-8 of it in bf16.  lse: the
+    scale's two roundings and the result's, each at most 2^-24 of 25.5."""
+    n, d, dt = 5000, 64, DT[dtype]
+    cache = torch.zeros(20, 2, 256, 1, d, dtype=dt, device=dev)
+    cache[:, 1] = 1
+    cache[at // 256, 0, at % 256, 0, 0] = 16
+    cache[at // 256, 1, at % 256] = 0
+    q, o = torch.zeros(1, d, dtype=dt, device=dev), torch.full((1, d), math.nan, dtype=dt, device=dev)
+    q[0, 0] = 1
+    lse = torch.zeros(1, 1, device=dev)
+    err = torch.zeros(1, dtype=torch.int32, device=dev)
+    table = torch.arange(20, dtype=torch.int32, device=dev)[None]
+    scale = 25.5 * math.log(2) / 16
+    shape = hs.make_attn_shape(1, 1, 1, d, 256, 20, 20, HSDT[dtype], scale=scale, unsplit=call == "unsplit")
+    if call in ("prefill", "unsplit"):
+        size = hs.hs_attn_prefill_workspace_bytes(shape, [n - 1], [1])
+        hs.hs_attn_prefill(shape, q, cache, table, o, lse, [n - 1], [1], [0, 1], workspace(size, dev), size,
+                           err)
+    elif call == "decode":
+        size = hs.hs_attn_decode_workspace_bytes(shape, n)
+        lens = torch.tensor([n], dtype=torch.int32, device=dev)
+        hs.hs_attn_decode(shape, q, cache, table, lens, n, o, lse, workspace(size, dev), size, err)
+    else:
+        front = 2048
+        size = hs.hs_attn_decode_shared_workspace_bytes(shape, front, n - front)
+        lens = torch.tensor([n - front], dtype=torch.int32, device=dev)
+        own = torch.zeros_like(table)
+        own[0, :12] = table[0, 8:]
+        hs.hs_attn_decode_shared(shape, q, cache, table[0], front, own, lens, n - front, o, lse,
+                                 workspace(size, dev), size, err)
+    torch.cuda.synchronize()
+    assert err.item() == 0
+    small = (n - 1) * 2.0 ** -25.5
+    want = small / (1 + small)
+    assert (o.double() / want - 1).abs().max().item() <= 2.0 ** -7.5 + 2.0 ** -8 + 2.0 ** -16
+    assert abs(lse.item() - (scale * 16 + math.log1p(small))) <= 2.0 ** -17
