@@ -168,6 +168,8 @@ hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache,
         return HS_OK;
     if (kv_len == nullptr || (prefix_len > 0 && prefix_table == nullptr))
         return HS_ERR_INVALID_ARG;
+    if (((reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(prefix_table)) & 3u) != 0)
+        return HS_ERR_MISALIGNED;
     p.q = q;
     p.cache = cache;
     p.table = block_table;

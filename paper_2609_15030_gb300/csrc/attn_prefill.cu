@@ -105,9 +105,9 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
             units += (int64_t)p.n_kv * n;
             items += p.n_kv;
             longest = n > longest ? n : longest;
+            if (units > INT_MAX)
+                return false;
         }
-    if (units > INT_MAX)
-        return false;
     p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
     p.n_split = 0;

@@ -1,6 +1,7 @@
 """Host-only checks of the full-attention calls: every argument error is reported before any CUDA
 call, and what is empty returns without one (no GPU needed)."""
 import math
+import time
 
 import pytest
 
@@ -130,6 +131,28 @@ def test_prefixes_are_checked(kw, code):
     with pytest.raises(hs.HsError) as e:
         shared(**kw)
     assert e.value.status == code
+
+
+@pytest.mark.parametrize("call,kw", [(decode, dict(kv_len=FAKE + 2)), (shared, dict(kv_len=FAKE + 1)),
+                                     (shared, dict(prefix_table=FAKE + 2))], ids=str)
+def test_device_arrays_of_lengths_and_blocks_are_aligned(call, kw):
+    with pytest.raises(hs.HsError) as e:
+        call(**kw)
+    assert e.value.status == MIS
+
+
+def test_a_prefill_of_too_many_tiles_is_refused_at_once():
+    """384 requests of 8 M row tiles each: the count stops where 31 bits are exceeded."""
+    batch, n = 384, (1 << 31) // 128 - (1 << 14)
+    sh = shape(batch=batch, n_heads=128, n_kv_heads=1, max_pages=1 << 30)
+    start = time.monotonic()
+    try:
+        hs.hs_attn_prefill_workspace_bytes(sh, [0] * batch, [n] * batch)
+        status = hs.HS_OK
+    except hs.HsError as e:
+        status = e.status
+    assert status in (UNS, hs.HS_ERR_CUDA)        # HS_ERR_CUDA: without a device
+    assert time.monotonic() - start < 1
 
 
 def test_nothing_to_do_needs_no_gpu():
