@@ -71,7 +71,11 @@ struct Cfg {
     static constexpr int kRegs = NG == 2 ? 168 : 128;
     static constexpr int kMoreRegs = NG == 2 ? 216 : 200, kLessRegs = NG == 2 ? 72 : 56;
     static_assert(kSoftmax * 32 * kMoreRegs + 128 * kLessRegs <= kThreads * kRegs, "");
-    static constexpr int kTmemCols = NG == 2 ? 512 : 256;  // S and O of each group, 128 columns each
+    // of each group S in 128 columns, O in D, and with D = 64 the weights in 64 of their own, so that the
+    // next scores need not wait for the product that reads these
+    static constexpr int kTmemCols = NG == 2 ? 512 : 256;
+    static constexpr bool kOwnWeights = D == 64;
+    static constexpr int kWeightsAt = kOwnWeights ? 192 : 0;
 };
 
 constexpr int kRing = 4;                 // segments described ahead
@@ -98,6 +102,7 @@ struct Smem {
     uint64_t full[8], empty[8];          // a stage may be read / its MMAs are done
     uint64_t raw[8];                     // a value tile with masked places has landed
     uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t s_read[2];                  // weights in columns of their own: the scores are in registers
     uint64_t info_full[kRing], info_empty[kRing];
     uint64_t turn[2];                    // which group's products are next
     uint64_t drain[2];
@@ -231,6 +236,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             mbar_init(smem_u32(&sm.s_full[g]), 1);
             mbar_init(smem_u32(&sm.p_full[g]), 128);
             mbar_init(smem_u32(&sm.o_full[g]), 1);
+            mbar_init(smem_u32(&sm.s_read[g]), 128);
             mbar_init(smem_u32(&sm.drain[g]), 1);
             mbar_init(smem_u32(&sm.turn[g]), 1);
         }
@@ -420,9 +426,10 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         // next tile overwrite the weights of the last one behind the product that reads them.  A stage
         // is free once both groups are done with it
         const int g = warp - C::kSoftmax;
-        const uint32_t s_at = tmem + g * 256, o_at = s_at + 128;
+        const uint32_t s_at = tmem + g * 256, o_at = s_at + 128, p_at = s_at + C::kWeightsAt;
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
         const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint32_t bar_r = smem_u32(&sm.s_read[g]);
         const uint64_t q_desc = sdesc_sw128(q_at + g * C::kTile, 16, 1024);
         const uint64_t k_desc = sdesc_sw128(st_at, 16, kHalf * 1024);
         const uint64_t v_desc = sdesc_sw128(st_at, 1024, kHalf * 1024);
@@ -454,6 +461,19 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             next_stage();
             return true;
         };
+        // the next tile's scores, or its keys left to the other group
+        auto next_scores = [&](int j, int mine, int most) -> bool {
+            if (j + 1 < mine) {
+                if (!wait(full(st), ph))
+                    return false;
+                tc_fence_after();
+                qk();
+                next_stage();
+            } else if (j + 1 < most) {
+                return pass();
+            }
+            return true;
+        };
         uint32_t ph_q = 0, ph_p = 0, ph_turn = (uint32_t)g ^ 1;    // the first group has the first turn
         bool go = true;
         if (p.stall_for_test && g == 0)
@@ -464,7 +484,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 break;
             const Info &info = sm.info[seg % kRing];
             const int most = info.most, mine = info.g[g].tiles;
-            const int both = NG == 2 ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
+            const int both = NG == 2 && !C::kOwnWeights ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
             int left = info.g[g].keys - info.kt0 * kKeys;
             done_with(seg);
             if (most < 0)
@@ -486,7 +506,13 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     continue;
                 }
                 const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
-                go = wait(bar_p, ph_p) && wait(full(st), ph);
+                const uint32_t st_v = st, ph_v = ph;
+                if constexpr (C::kOwnWeights) {
+                    go = wait(bar_r, ph_p);
+                    next_stage();
+                    go = go && next_scores(j, mine, most);
+                }
+                go = go && wait(bar_p, ph_p) && wait(full(st_v), ph_v);
                 ph_p ^= 1;
                 // The groups take turns, a product with v and the next scores each.  Where both had their
                 // products in flight at once they ended at once, did their softmax at once and stayed so: 2.1 us
@@ -499,27 +525,22 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     break;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t b = v_desc + st * (C::kTile / 16);
+                    const uint64_t b = v_desc + st_v * (C::kTile / 16);
 #pragma unroll
                     for (int k = 0; k < kKeys / 16; ++k)
                         if (k < steps)
-                            mma_f16_ts(o_at, s_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
+                            mma_f16_ts(o_at, p_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
                                        Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
-                    if (j + 1 == mine)
+                    if (C::kOwnWeights || j + 1 == mine)
                         tc_commit(bar_o);
-                    tc_commit(empty(st));
+                    tc_commit(empty(st_v));
                 }
                 __syncwarp();
-                next_stage();
-                if (j + 1 < mine) {
-                    go = wait(full(st), ph);
+                if constexpr (!C::kOwnWeights) {
+                    next_stage();
+                    go = next_scores(j, mine, most);
                     if (!go)
                         break;
-                    tc_fence_after();
-                    qk();
-                    next_stage();
-                } else if (j + 1 < most) {
-                    go = pass();
                 }
                 if (j < both) {
                     if (lane == 0)
@@ -635,9 +656,10 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         const int g = warp >> 2;
         const int r = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_at = tmem + g * 256 + lanes, o_at = s_at + 128;
+        const uint32_t s_at = tmem + g * 256 + lanes, o_at = s_at + 128, p_at = s_at + C::kWeightsAt;
         const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
         const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
+        const uint32_t bar_r = smem_u32(&sm.s_read[g]);
         uint32_t ph_s = 0, ph_o = 0;
         // row x of the group's rows, counted from its first one's token: x / p.group by multiplication,
         // exact for x < 256, p.group <= 128 (the error of the factor is at most p.group, 256 * 128 < 2^16)
@@ -702,8 +724,23 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     if (!go)
                         break;
                 }
+                // the product before this one, where the scores did not wait for it
+                bool behind = !C::kOwnWeights || j == 0;
+                auto last_product = [&]() {
+                    if (!behind) {
+                        go = wait(bar_o, ph_o);
+                        ph_o ^= 1;
+                        tc_fence_after();
+                        behind = true;
+                    }
+                };
                 if (!some) {
                     tc_fence_before();
+                    if constexpr (C::kOwnWeights)
+                        mbar_arrive(bar_r);
+                    last_product();
+                    if (!go)
+                        break;
                     mbar_arrive(bar_p);
                     continue;
                 }
@@ -712,6 +749,10 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 for (int c = 0; c < kKeys; c += 32)
                     tmem_ld32(s_at + c, *reinterpret_cast<float(*)[32]>(&x[c]));
                 tmem_wait_ld();
+                if constexpr (C::kOwnWeights) {
+                    tc_fence_before();
+                    mbar_arrive(bar_r);
+                }
                 if (__any_sync(0xffffffffu, valid < kKeys)) {
 #pragma unroll
                     for (int c = 0; c < kKeys; ++c)
@@ -735,7 +776,8 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     if (up)
                         m = top - Elem<T>::kBelow;
                     if (j > 0) {
-                        // the previous product is done: the scores came after it
+                        // the previous product is done: the scores came after it, or it is waited for
+                        last_product();
                         l *= f;
 #pragma unroll
                         for (int c = 0; c < D; c += 16) {      // few registers: the scores hold theirs
@@ -766,8 +808,12 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         w[i] = Elem<T>::pack(a0, a1);
                         w[i + 1] = Elem<T>::pack(a2, a3);
                     }
-                    tmem_st16(s_at + c / 2, w);
+                    if (c == 0)
+                        last_product();
+                    tmem_st16(p_at + c / 2, w);
                 }
+                if (!go)
+                    break;
                 tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive(bar_p);
