@@ -477,7 +477,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         uint32_t ph_q = 0, ph_p = 0, ph_turn = (uint32_t)g ^ 1;    // the first group has the first turn
         bool go = true;
         if (p.stall_for_test && g == 0)
-            go = wait(smem_u32(&sm.drain[1]), 0);     // (the first group never commits to the second's)
+            go = wait(smem_u32(&sm.drain[0]), 0);     // only this warp commits to it, at the end
         for (uint32_t seg = 0; go; ++seg) {
             go = described(seg);
             if (!go)
