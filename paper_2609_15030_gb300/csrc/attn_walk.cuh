@@ -234,22 +234,30 @@ __device__ __forceinline__ int warp_scan(int x, int lane)
 __device__ __forceinline__ int read_lengths(const AttnParams &p, int32_t *len, int lane, bool complain,
                                             int upto, int *before)
 {
+    constexpr int kAhead = 6;             // loads that do not wait for one another; HS_MAX_BATCH takes two rounds
     int sum = 0, part = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const int b = b0 + lane;
-        int n = -1;
-        if (b < p.batch) {
-            n = p.kv_len[b];
-            if (n < 0 || n > p.max_kv) {
-                if (complain)
-                    report(p.d_err, HS_DEVERR_LENGTH);
-                n = -1;
-            }
-            len[b] = n;
+    for (int b0 = 0; b0 < p.batch; b0 += 32 * kAhead) {
+        int n[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int b = b0 + i * 32 + lane;
+            n[i] = b < p.batch ? p.kv_len[b] : -1;
         }
-        const int x = own_units(p, n);
-        sum += x;
-        part += b < upto ? x : 0;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int b = b0 + i * 32 + lane;
+            if (b < p.batch) {
+                if (n[i] < 0 || n[i] > p.max_kv) {
+                    if (complain)
+                        report(p.d_err, HS_DEVERR_LENGTH);
+                    n[i] = -1;
+                }
+                len[b] = n[i];
+            }
+            const int x = own_units(p, n[i]);
+            sum += x;
+            part += b < upto ? x : 0;
+        }
     }
     __syncwarp();
     *before = __reduce_add_sync(0xffffffffu, part);
