@@ -696,7 +696,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             const T *const from = static_cast<const T *>(p.q) + x.g[g].row0 * p.q_stride +
                                   (x.head0 + first) * D + c * 8;
             const int turn = (int)(p.q_stride - p.group * D);      // from a token's last head to the next
-#pragma unroll
+#pragma unroll 2
             for (int i = 0; i < 32; i += kRows)
                 if (i < left)
                     cp_async_16(to + i * 128 + (((c & 7) ^ ((r0 + i) & 7)) << 4),
@@ -800,7 +800,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         // the previous product is done: the scores came after it, or it is waited for
                         last_product();
                         l *= f;
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D; c += 16) {      // few registers: the scores hold theirs
                             uint32_t a[16];
                             tmem_ld16(o_at + c, a);
@@ -860,23 +860,23 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             const int32_t *const from = sm.marks.from[seg % kRing];
             const int row = info.g[g].row0 + t, head_at = info.head0 + head + r - t * p.group;
             const int64_t slot_at = info.slot;
-            // all columns at once: read 32 at a time between their stores they took 2 us
-            float a[D];
-            if (some && tiles > 0) {
+            // 32 columns of the sums.  The loops over them stay loops: straight code that is run once a
+            // segment waits for its instructions (a segment's outputs took 2 us of it, 0.5 of a loop)
+            auto columns = [&](int c, float (&a)[32]) {
+                if (tiles > 0) {
+                    tmem_ld32(o_at + c, a);
+                    tmem_wait_ld();
+                } else {
 #pragma unroll
-                for (int c = 0; c < D; c += 32)
-                    tmem_ld32(o_at + c, *reinterpret_cast<float(*)[32]>(&a[c]));
-                tmem_wait_ld();
+                    for (int i = 0; i < 32; ++i)
+                        a[i] = 0.f;
+                }
                 if (marked) {
 #pragma unroll
-                    for (int c = 0; c < D; ++c)
-                        a[c] = keys > from[c] ? NAN : a[c];
+                    for (int i = 0; i < 32; ++i)
+                        a[i] = keys > from[c + i] ? NAN : a[i];
                 }
-            } else {
-#pragma unroll
-                for (int c = 0; c < D; ++c)
-                    a[c] = 0.f;
-            }
+            };
             if (!some) {
                 // nothing to write
             } else if (slot_at < 0) {
@@ -892,12 +892,14 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     o[k] = static_cast<T *>(p.o) + (info.g[g].row0 + tt) * p.o_stride +
                            (info.head0 + head + rr - tt * p.group) * D + (lane & 3) * 8;
                 }
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
+                    float a[32];
+                    columns(c, a);
                     uint4 v[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const int i = c + 8 * k;
+                        const int i = 8 * k;
                         v[k] = make_uint4(Elem<T>::pack(a[i] * inv, a[i + 1] * inv),
                                           Elem<T>::pack(a[i + 2] * inv, a[i + 3] * inv),
                                           Elem<T>::pack(a[i + 4] * inv, a[i + 5] * inv),
@@ -920,17 +922,22 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 const int at = info.g[g].at + r, slot_rows = info.slot_rows;
                 if (ok)
                     reinterpret_cast<float2 *>(slot)[at] = make_float2(m, l);
-                if (ok && tiles > 0 && !Plan::kDecode) {
-                    float *const to = slot + pairs_floats(128 * NG) + at;
+#pragma unroll 1
+                for (int c = 0; tiles > 0 && c < D; c += 32) {
+                    float a[32];
+                    columns(c, a);
+                    if (ok && !Plan::kDecode) {
+                        float *const to = slot + pairs_floats(128 * NG) + c * 128 * NG + at;
 #pragma unroll
-                    for (int c = 0; c < D; ++c)
-                        to[c * 128 * NG] = a[c];
-                } else if (ok && tiles > 0) {
-                    float *const to = slot + pairs_floats(slot_rows) + (int64_t)at * D;
+                        for (int i = 0; i < 32; ++i)
+                            to[i * 128 * NG] = a[i];
+                    } else if (ok) {
+                        float *const to = slot + pairs_floats(slot_rows) + (int64_t)at * D + c;
 #pragma unroll
-                    for (int c = 0; c < D; c += 4)
-                        *reinterpret_cast<float4 *>(to + c) =
-                            make_float4(a[c], a[c + 1], a[c + 2], a[c + 3]);
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4 *>(to + i) =
+                                make_float4(a[i], a[i + 1], a[i + 2], a[i + 3]);
+                    }
                 }
             }
             tc_fence_before();
