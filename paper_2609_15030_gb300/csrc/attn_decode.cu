@@ -48,7 +48,7 @@ attn_merge_decode_kernel(const __grid_constant__ AttnParams p, int per_row)
         const int pitem = rt * p.n_kv + kvh;
         int p0 = 0, p1 = -1;
         if (on && per > 0) {
-            p0 = cta_of(units, p.ctas, pitem * per + (p.unsplit ? 0 : p.extra));
+            p0 = cta_of(units, p.ctas, pitem * per + (p.unsplit ? 0 : p.extra_shared));
             p1 = p.unsplit ? p0 : cta_of(units, p.ctas, (pitem + 1) * per - 1);
         }
         const int n = p1 - p0 + 1;
@@ -107,13 +107,20 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
     auto slot = [&](int rows) {
         return (int64_t)sizeof(float) * (d == 128 ? slot_floats<128>(rows) : slot_floats<64>(rows));
     };
-    // 32 ragged requests: 53.6 us with 1 where 0 took 55; behind a shared prefix 8 and 64 requests took 11.2
-    // and 71 us with 0, 12.5 and 74.7 with 1
-    p.extra = p.prefix_len > 0 ? 0 : 1;
-    const int64_t own = (int64_t)p.batch * p.n_kv * ((p.max_kv > 0 ? tiles_of(p.max_kv) : 1) + p.extra);
+    const int own_tiles = p.max_kv > 0 ? tiles_of(p.max_kv) : 1, shared_tiles = tiles_of(p.prefix_len);
     const int rows = p.batch * p.group;
-    const int64_t items = (int64_t)p.n_kv * (p.groups == 2 ? row_tiles<2>(rows) : row_tiles<1>(rows));
-    const int64_t units = own + items * prefix_units(p);
+    const int64_t own = (int64_t)p.batch * p.n_kv;
+    const int64_t shared = p.prefix_len == 0 ? 0 : (int64_t)p.n_kv *
+                           (p.groups == 2 ? row_tiles<2>(rows) : row_tiles<1>(rows));
+    // What a segment costs beside its tiles.  32 ragged requests: 53.6 us with 1 where 0 took 55; behind a
+    // shared prefix, 32 requests of a tile each 22.9 us with 1 instead of 26.5, but where two tiles of rows
+    // take a CTA's own items in turn, 384 requests 96 us with 0 instead of 120.  A prefix's items end
+    // with the sums of all requests' rows: 64 requests behind 32,768 keys 64.2 us with 4 where 0 took 68.3,
+    // but 8 behind 4,608, less than a tile to a CTA, 11.2 us with 0 instead of 11.8 with 4.
+    const int64_t share = (own * own_tiles + shared * shared_tiles) / most;
+    p.extra = p.prefix_len == 0 || (p.groups == 1 && share >= 2) ? 1 : 0;
+    p.extra_shared = (int)(share / 2 < 4 ? share / 2 : 4);
+    const int64_t units = own * (own_tiles + p.extra) + shared * prefix_units(p);
     if (units > INT_MAX)
         return -1;
     p.ctas = (int)(units < most ? units : most);
@@ -121,9 +128,9 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
     p.parts = (int)(longest / (units / p.ctas > 0 ? units / p.ctas : 1)) + 2;
     if (p.prefix_len > 0) {
         p.joined = 1;
-        return (items + p.ctas) * slot(128 * p.groups) + ((int64_t)p.batch * p.n_kv + p.ctas) * slot(p.group);
+        return (shared + p.ctas) * slot(128 * p.groups) + (own + p.ctas) * slot(p.group);
     }
-    if (better_whole(p, (int64_t)p.batch * p.n_kv, tiles_of(p.max_kv), units))
+    if (better_whole(p, own, tiles_of(p.max_kv), units))
         p.unsplit = 1;
     p.joined = !p.unsplit;
     return p.joined ? 2 * p.ctas * slot(p.group) : 0;

@@ -66,6 +66,7 @@ struct AttnParams {
     int32_t ctas;
     int32_t extra;                // units of an item before its tiles: what a segment costs beside them (its
                                   // queries, the ends of its pipeline, its outputs), in tiles
+    int32_t extra_shared;         // the same of an item of the shared prefix
     int32_t groups;               // tiles of 128 rows to an item
     int32_t n_split;              // prefill: items that fall to several CTAs
     int32_t parts;                // decode: about the most CTAs that share an item

@@ -110,6 +110,10 @@ struct Walk {
         else
             return tiles_of(keys_before(p, plan.req[b].pos0, min(rows(), (rt + 1) * 128 * NG)));
     }
+    __device__ int extra() const
+    {
+        return b < 0 ? p.extra_shared : p.extra;
+    }
     __device__ bool skip() const
     {
         if constexpr (Plan::kDecode)
@@ -134,19 +138,19 @@ struct Walk {
         : p(params), plan(plan_), len(lens), left(s.left), b(s.b), rt(s.rt), kvh(s.kvh), at(s.at)
     {
         if (p.unsplit && left > 0 && at != 0) {       // begins with the next whole item
-            left -= tiles() + p.extra - at;
+            left -= tiles() + extra() - at;
             next_item();
         }
     }
     __device__ bool next(Segment &s)
     {
         while (left > 0) {
-            const int n = tiles();
-            int end = n + p.extra;
+            const int n = tiles(), extra = this->extra();
+            int end = n + extra;
             if (!p.unsplit && end - at > left)
                 end = at + left;
-            s.kt0 = at > p.extra ? at - p.extra : 0;
-            s.kt1 = end > p.extra ? end - p.extra : 0;
+            s.kt0 = at > extra ? at - extra : 0;
+            s.kt1 = end > extra ? end - extra : 0;
             s.b = b;
             s.rt = rt;
             s.kvh = kvh;
@@ -155,7 +159,7 @@ struct Walk {
             s.item = (b < 0 ? rt : b) * p.n_kv + kvh;
             left -= end - at;
             at = end;
-            if (at == n + p.extra)
+            if (at == n + extra)
                 next_item();
             if (s.kt1 > s.kt0)
                 return true;
@@ -215,7 +219,7 @@ __device__ __forceinline__ int own_units(const AttnParams &p, int len)
 // units of an item of the shared prefix (0: there is none)
 __host__ __device__ __forceinline__ int prefix_units(const AttnParams &p)
 {
-    return p.prefix_len > 0 ? tiles_of(p.prefix_len) + p.extra : 0;
+    return p.prefix_len > 0 ? tiles_of(p.prefix_len) + p.extra_shared : 0;
 }
 
 __device__ __forceinline__ int warp_scan(int x, int lane)
