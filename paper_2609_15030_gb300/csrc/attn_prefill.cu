@@ -94,9 +94,9 @@ int groups_of(const AttnParams &p, const PrefillPlan &plan)
 template <int NG>
 bool schedule(AttnParams &p, PrefillPlan &plan, int most)
 {
-    // Without this CTAs with many short items end long after the others: nine packed tails took 85 us with 1
-    // unit where 2 took 75, 3 take 53.6 where 2 took 54.5; 4 cost two 16k-token prompts 2 %.
-    p.extra = 3;
+    // With 1 CTAs with many short items end long after the others (nine packed tails 53.9 us, two 8k-token
+    // prompts of 64-wide heads 590); 2 take 50.5 and 515, 3 take 51.7 and 515, 4 53.0 and 521.
+    p.extra = 2;
     int64_t units = 0, items = 0;
     int longest = 0;
     for (int b = 0; b < p.batch; ++b)
