@@ -35,9 +35,12 @@
 // some 250 ns go into the hand-overs, so a pair of tiles takes 1.45 us where the tensor core alone
 // would take 1.07; with a shorter softmax (two threads to a row) registers spilled and it took 2.3.
 // Two 16k-token prompts of 32 heads: 2.87 ms, 1,530 TFLOP/s, at the power limit (a cuBLAS product
-// sustains 1,692 there).  A decode step is bound by HBM where its contexts are long (four requests at
-// 98k to 131k keys: 269 us, 7.0 TB/s), a short call by latency: 3.5 us until the first scores, 0.7 us
-// of softmax, 2 us for sums of 256 rows that go to the workspace, 3 to 4 us for the join.
+// sustains 1,692 there); one of 8k tokens 338 us, 1,625.  Heads of 64 have half the products to the same
+// softmax: 1.2 us a pair of tiles, 1,070 TFLOP/s.  A decode step is bound by HBM where its contexts are long
+// (four requests at 98k to 131k keys: 269 us, 7.0 TB/s), a short call by latency: 3.5 us until the first
+// scores, 0.7 us of softmax, 1.3 us for sums of 256 rows that go to the workspace, 3 to 4 us for the join.
+// A segment costs what two tiles cost beside its own: its description, queries, and outputs, code that runs
+// once and waits for its instructions.
 #pragma once
 
 #include <cuda.h>
@@ -857,7 +860,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             const int row = info.g[g].row0 + t, head_at = info.head0 + head + r - t * p.group;
             const int64_t slot_at = info.slot;
             // 32 columns of the sums.  The loops over them stay loops: straight code that is run once a
-            // segment waits for its instructions (a segment's outputs took 2 us of it, 0.5 of a loop)
+            // segment waits for its instructions (a segment's outputs took 2 us of it, as a loop 1.2)
             auto columns = [&](int c, float (&a)[32]) {
                 if (tiles > 0) {
                     tmem_ld32(o_at + c, a);
