@@ -29,3 +29,24 @@ def test_a_wait_that_runs_out_reports_timeout_and_leaves_the_context_usable(n):
     assert torch.isnan(out.o).all() and torch.isnan(out.lse).all()
     # the same context, the normal call
     run_prefill(p, [0], [n], dev).check(p.prefill_rows([0], [n], [0, n]))
+
+
+@pytest.mark.parametrize("n", [20, 200, 1500])
+def test_a_wait_that_runs_out_with_heads_of_64(n):
+    """The groups of 64-wide heads do not wait for one another: what the second one has finished may be
+    written, and it is right."""
+    dev = device()
+    p = Problem(21, 2, 1, 64, 16, "fp16", [n], n)
+    out = Outputs(p, dev)
+    shape = p.shape(1, unsplit=True)
+    t0 = time.perf_counter()
+    hs.hs_test_attn_stalled(shape, p.q.to(dev), p.cache.to(dev), p.table.to(dev), out.o, out.lse, [0], [n],
+                            [0, n], workspace(0, dev), 0, out.err)
+    torch.cuda.synchronize()
+    assert out.err.item() == hs.HS_DEVERR_TIMEOUT
+    assert 0.9 < time.perf_counter() - t0 < 30.0
+    o = out.o.cpu()
+    rows = [x for x in p.prefill_rows([0], [n], [0, n]) if not torch.isnan(o[x[0], :2 * 64]).any()]
+    for r, want, _, bound, _ in rows:
+        assert ((o[r, :2 * 64].double().reshape(2, 64) - want).abs() <= bound).all()
+    run_prefill(p, [0], [n], dev).check(p.prefill_rows([0], [n], [0, n]))
