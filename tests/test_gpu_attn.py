@@ -159,6 +159,28 @@ def test_prefill_keeps_later_values_out_of_earlier_rows(dev, bad, at, d):
     assert not torch.isfinite(o[at:, :, 5]).any()
 
 
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(2, 2, 128, "bf16"), (2, 2, 64, "fp16"), (6, 2, 128, "fp16"),
+                                                    (6, 2, 64, "bf16")])
+@pytest.mark.parametrize("n", [128, 300])
+def test_every_place_of_a_diagonal_tile_is_searched(dev, n, heads, kv_heads, d, dtype):
+    """One value that is not finite at a time, walking over the rows and columns (and so over the chunks
+    that the searching lanes hold) in the places that only some rows see: the rows in front keep their
+    values, those at and behind it lose that column alone."""
+    p = Problem(31, heads, kv_heads, d, 16, dtype, [n], n)
+    clean = run_prefill(p, [0], [n], dev).o.cpu()[:n, :heads * d].reshape(n, kv_heads, heads // kv_heads, d)
+    good = p.cache.clone()
+    for i in range(40):
+        at, col, kvh, bad = (1 + 37 * i) % n, (11 * i) % d, i % kv_heads, (math.nan, math.inf, -math.inf)[i % 3]
+        p.cache = good.clone()
+        p.cache[p.table[0, at // 16].long(), 1, at % 16, kvh, col] = bad
+        o = run_prefill(p, [0], [n], dev).o.cpu()[:n, :heads * d].reshape(n, kv_heads, heads // kv_heads, d)
+        hit = torch.zeros(n, kv_heads, 1, d, dtype=torch.bool)
+        hit[at:, kvh, :, col] = True
+        hit = hit.expand_as(o)
+        assert not torch.isfinite(o[hit]).any(), (at, col, kvh)
+        assert torch.equal(o[~hit], clean[~hit]), (at, col, kvh)
+
+
 def test_prefill_reports_pages_outside_the_cache(dev):
     """Rows that do not attend to the bad page keep their values; nothing faults."""
     p = Problem(8, 2, 1, 128, 16, "bf16", [100, 50], 150)
