@@ -1135,7 +1135,8 @@ inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
 // The cache of a layer as [8-token group][64-element block of a token's heads][token][64]: a copy's
 // box is one head of a page (or of 128 keys of one), 8-token groups outermost, which in shared
 // memory is the operand layout of both products: 128-byte rows, swizzled, in atoms of 8 tokens, the
-// atoms of a row's blocks side by side.
+// atoms of a row's blocks side by side.  Misses fetch 128 bytes: with 256 the neighbour's head of 64 came
+// along for nothing (64 decode steps of 8 such heads at 4,096 keys 126 us instead of 96).
 template <int D>
 bool encode_cache(CUtensorMap *m, const AttnParams &p)
 {
@@ -1149,7 +1150,7 @@ bool encode_cache(CUtensorMap *m, const AttnParams &p)
     cuuint32_t one[4] = {1, 1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void *>(p.cache), dim, stride, box, one,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int D, int NG, class Plan>
