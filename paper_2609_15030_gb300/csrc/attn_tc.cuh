@@ -12,6 +12,10 @@
 // to nothing only below 2^-33 of the largest (with m at the maximum, many keys of 2^-25 each were lost).
 // Weights are rounded to the element type for the product with v (the tensor core takes 16-bit
 // operands); l sums them before that rounding.
+// 2^(s_j - m) is one fused multiplication and addition of q . k_j, m a rounded product.  What that rounding
+// takes off is the same factor of all weights of the row and cancels in o; but with m beyond 2^31 it is
+// 2^+-128 and more (NaN, or weights of nothing but 0), and beyond 2^24 fp16 weights overflow.  So with m
+// beyond 2^20 all products are rounded before m is taken off, and the largest gets a weight of 2^0 (fp16: 2^8).
 //
 // Schedule.  The units of all items in order are shared out evenly over the CTAs, each a
 // contiguous run, so that one long request or many ragged ones fill the SMs alike.  An item whose
@@ -57,6 +61,7 @@ namespace attn {
 using namespace ptx;
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kFar = 1048576.f;         // scores that are rounded before m is taken off (units of log2)
 constexpr uint64_t kTimeoutNs = 1000000000ull;
 
 // ---- shapes of a launch --------------------------------------------------------------------
@@ -738,6 +743,9 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 return true;
             };
             float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
+            float limit = -INFINITY;            // m + kMost
+            float shift = 0.f;                  // -m, but 0 without a key and far from zero
+            bool far = false;                   // m lies beyond kFar
             int valid = keys - info.kt0 * kKeys;   // keys of the row from this tile on
             for (int j = 0; j < tiles; ++j, valid -= kKeys) {
                 go = wait(bar_s, ph_s);
@@ -791,11 +799,56 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 t0 = max3(t0, x[124], x[125]);
                 t1 = max3(t1, x[126], x[127]);
                 const float top = max3(t0, t1, fmaxf(t2, t3)) * p.scale_log2;
-                const bool up = top > m + Elem<T>::kMost;
-                if (__any_sync(0xffffffffu, up)) {
-                    const float f = up ? ex2(m - (top - Elem<T>::kBelow)) : 1.f;
-                    if (up)
-                        m = top - Elem<T>::kBelow;
+                const bool up = top > limit;
+                if (__any_sync(0xffffffffu, up || far)) {
+                    float to = m;
+                    if (up) {
+                        to = top - Elem<T>::kBelow;
+                        limit = to + Elem<T>::kMost;
+                        shift = -to;
+                        far = ok && fabsf(to) > kFar;
+                    }
+                    // Far from zero the scores are rounded before m is taken off, as their maximum was, and
+                    // what is left of them is brought back to the scale of the others.  In a loop of 16
+                    // columns, through the columns of the weights: as straight code, which hardly any call
+                    // runs, it cost the others up to 6 % (two 8k-token prompts of 64-wide heads 552 us instead
+                    // of 519), and asking for it by a second vote a tile as much.
+                    if (__builtin_expect(__any_sync(0xffffffffu, far), 0)) {
+                        if (far) {               // where 8 or 15 is half a step of float32 or less
+                            to = up && top - to > Elem<T>::kMost ? top : to;
+                            limit = to + Elem<T>::kMost;
+                            limit = limit - to > Elem<T>::kMost ? to : limit;
+                            shift = 0.f;
+                        }
+                        const float back = 1.f / p.scale_log2;
+                        last_product();
+#pragma unroll
+                        for (int h = 0; h < kKeys; h += 64) {
+#pragma unroll
+                            for (int c = 0; c < 64; c += 16)
+                                tmem_st16(p_at + c, *reinterpret_cast<uint32_t(*)[16]>(&x[h + c]));
+                            tmem_wait_st();
+#pragma unroll 1
+                            for (int c = 0; c < 64; c += 16) {
+                                uint32_t a[16];
+                                tmem_ld16(p_at + c, a);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const float y = __uint_as_float(a[i]);
+                                    const float z = __fsub_rn(__fmul_rn(y, p.scale_log2), to) * back;
+                                    a[i] = far ? __float_as_uint(z) : a[i];
+                                }
+                                tmem_st16(p_at + c, a);
+                            }
+                            tmem_wait_st();
+                            tmem_ld32(p_at, *reinterpret_cast<float(*)[32]>(&x[h]));
+                            tmem_ld32(p_at + 32, *reinterpret_cast<float(*)[32]>(&x[h + 32]));
+                            tmem_wait_ld();
+                        }
+                    }
+                    const float f = up ? ex2(m - to) : 1.f;
+                    m = to;
                     if (j > 0) {
                         // the previous product is done: the scores came after it, or it is waited for
                         last_product();
@@ -812,7 +865,6 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         }
                     }
                 }
-                const float shift = m == -INFINITY ? 0.f : -m;
                 const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
                 uint64_t l01 = 0, l23 = 0;
 #pragma unroll
