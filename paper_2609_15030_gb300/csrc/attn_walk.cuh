@@ -66,10 +66,10 @@ int prefill_tiles(int pos0, int n_tokens, int group, int rt)
     return tiles_of(pos0 + ((end < rows ? end : rows) - 1) / group + 1);
 }
 
-// Whether a call is better not split: a join costs what 3 tiles cost (2 to 4 us), and a second launch
-// its host time; whole items leave a CTA at most the longest above an even share (with an item or less
-// to each, the longest).  One request of 2 heads with 256 keys: 6.2 us a call, host bound, instead of 9
-// split.
+// Whether a call of `units` units is better not split: a join costs what 3 tiles cost (2 to 4 us), and a
+// second launch its host time; whole items leave a CTA at most the longest above an even share (with an item
+// or less to each, the longest).  One request of 2 heads with 256 keys: 6.2 us a call, host bound, instead of
+// 9 split.
 inline bool better_whole(const AttnParams &p, int64_t items, int longest, int64_t units)
 {
     const int64_t even = units / p.ctas - p.extra, share = even > 1 ? even : 1;

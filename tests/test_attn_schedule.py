@@ -1,0 +1,49 @@
+"""The schedule of the full-attention calls as the host makes it (no GPU needed): how units of work are
+shared out over CTAs, and which decode steps are split."""
+import os
+import subprocess
+
+import pytest
+
+from paper_2609_15030_gb300 import build
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+
+@pytest.fixture(scope="module")
+def schedule(tmp_path_factory):
+    lib = build.build()
+    exe = tmp_path_factory.mktemp("schedule") / "schedule"
+    subprocess.run([build._nvcc(), *build.ARCH, "-O1", "-std=c++17", "--expt-relaxed-constexpr", "-I", build.INCLUDE,
+                    "-I", build.CSRC, os.path.join(HERE, "attn_schedule", "schedule.cu"), "-o", str(exe), lib,
+                    "-Xlinker", "-rpath," + os.path.dirname(lib)], check=True, timeout=300)
+
+    def run(*args):
+        r = subprocess.run([str(exe), *map(str, args)], capture_output=True, text=True, timeout=60)
+        assert r.returncode == 0, r.stdout
+        return [int(x) for x in r.stdout.split()]
+    return run
+
+
+def test_every_unit_is_one_ctas(schedule):
+    """Below and above 2^22 units (one prompt of 131,072 tokens of 32 heads has 8.4 million), up to 2^31."""
+    assert schedule("shares")[0] > 50_000
+
+
+def decode(schedule, batch, kv_heads, max_kv, d=128, prefix=0, sms=152):
+    unsplit, joined, _, size = schedule("decode", batch, 4 * kv_heads, kv_heads, d, max_kv, prefix, sms)
+    assert joined == (not unsplit) and (size > 0) == bool(joined)
+    return bool(unsplit)
+
+
+@pytest.mark.parametrize("batch,kv_heads", [(38, 8), (37, 8), (76, 4), (64, 4), (304, 1), (1, 4), (384, 8)])
+def test_decode_steps_of_long_bounds_are_split(schedule, batch, kv_heads):
+    """The bound says nothing of the lengths: one request at it beside short ones must not be one CTA's."""
+    for max_kv in (4 * 128 + 1, 1000, 2304, 4096, 12_800, 131_072):
+        assert not decode(schedule, batch, kv_heads, max_kv), max_kv
+
+
+def test_decode_steps_of_short_bounds_are_not(schedule):
+    for batch, kv_heads in ((38, 8), (64, 4), (1, 2), (384, 8)):
+        for max_kv in (0, 1, 128, 300, 384):
+            assert decode(schedule, batch, kv_heads, max_kv), (batch, kv_heads, max_kv)
