@@ -288,396 +288,398 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             mbar_arrive(smem_u32(&sm.info_empty[k % kRing]));
     };
 
-    if (warp == C::kSoftmax + 3) {
+    // A warpgroup's four warps move their registers by one instruction, whatever each of them does then (and
+    // the roles lie within the branches: behind a join of these the compiler gives all the smaller share).
+    if (warp >= C::kSoftmax) {
         fewer_registers<C::kLessRegs>();
-        // ---- the walk, and loads: key and value tiles in turn through the stages
-        Start start;
-        if constexpr (Plan::kDecode) {
-            int before = 0;
-            const int own = read_lengths(p, sm.len, lane, cta == 0, 0, &before);
-            start = find_start<NG>(p, sm.len, own, cta, lane);
-        } else {
-            start = find_start<NG>(p, plan, cta);
-        }
-        Walk<NG, Plan> walk(p, plan, sm.len, start);
-        Segment s;
-        const int per = p.page_shift >= 7 ? 1 : kKeys >> p.page_shift;      // pages of a tile
-        const int box = p.page_shift >= 7 ? kKeys : 1 << p.page_shift;      // keys of a copy
-        const int groups = 1 << (p.page_shift - 3);                         // 8-key rows of a page
-        const int32_t none = (int32_t)(p.num_blocks * 2 * groups);          // beyond the cache: zeros
-        uint32_t n = 0, st = 0, ph = 1;           // stages filled; the next one and the phase that frees it
-        uint32_t is_raw = 0, ph_raw = 0;          // by stage: filled behind `raw`; its last phase
-        struct Ahead {                            // a segment as it is loaded
-            int kt0, tiles, keys, common, kvh;
-            const int32_t *table;
-        };
-        // this lane's block id of a tile's pages
-        auto block = [&](const Ahead &x, int kt) -> int32_t {
-            const int first = kt * kKeys + lane * box;
-            if (kt >= x.kt0 + x.tiles || lane >= per || first >= x.keys)
-                return -1;
-            return x.table[first >> p.page_shift];
-        };
-        // the next segment, described to the other warps; tiles = -1: there is none
-        uint32_t seg = 0;
-        auto describe = [&](Ahead &x, int32_t &id) -> bool {
-            Info *const info = &sm.info[seg % kRing];
-            const bool have = walk.next(s);
-            x.tiles = -1;
-            if (seg >= kRing && !wait(smem_u32(&sm.info_empty[seg % kRing]), (seg / kRing - 1) & 1))
-                return false;
-            if (have) {
-                x.kt0 = s.kt0;
-                x.kvh = s.kvh;
-                x.keys = walk.all_keys(s);
-                x.common = walk.common_keys(s);
-                x.tiles = group_tiles(s, x.keys);
-                x.table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
-                id = block(x, x.kt0);             // on its way while the segment is described
-                if (lane < NG) {
-                    // a decode step's own items have one tile of rows: the groups have them in turn
-                    const bool own_item = Plan::kDecode && s.b >= 0;
-                    const int q = NG == 2 && own_item ? lane ^ (int)(seg & 1) : lane;
-                    const int r0 = (s.rt * NG + q) * 128, left = s.rows - r0;
-                    const int t = s.b < 0 || !Plan::kDecode ? p.by_group.div(r0) : 0;
-                    const int own = walk.group_keys(s, q);
-                    info->g[lane].head = r0 - t * p.group;
-                    info->g[lane].rows = left < 0 ? 0 : left < 128 ? left : 128;
-                    info->g[lane].keys = own;
-                    info->g[lane].at = own_item ? 0 : lane * 128;
-                    info->g[lane].tiles = group_tiles(s, own);
-                    if constexpr (Plan::kDecode) {
-                        info->g[lane].row0 = s.b < 0 ? t : s.b;
-                        info->g[lane].key0 = x.keys;
-                    } else {
-                        info->g[lane].row0 = plan.req[s.b].row0 + t;
-                        info->g[lane].key0 = plan.req[s.b].pos0 + t + 1;
-                    }
-                }
-                if (lane == 0) {
-                    info->kt0 = s.kt0;
-                    info->all = x.keys;
-                    info->common = x.common;
-                    info->head0 = s.kvh * p.group;
-                    int rows = 0;
-                    info->slot = s.whole && (!Plan::kDecode || p.prefix_len == 0)
-                                     ? -1
-                                     : slot_of<D, NG, Plan>(p, s, cta, &rows);
-                    info->slot_rows = rows;
-                }
+        if (warp == C::kSoftmax + 3) {
+            // ---- the walk, and loads: key and value tiles in turn through the stages
+            Start start;
+            if constexpr (Plan::kDecode) {
+                int before = 0;
+                const int own = read_lengths(p, sm.len, lane, cta == 0, 0, &before);
+                start = find_start<NG>(p, sm.len, own, cta, lane);
+            } else {
+                start = find_start<NG>(p, plan, cta);
             }
-            if (lane == 0)
-                info->most = x.tiles;
-            __syncwarp();
-            if (lane == 0)
-                mbar_arrive(smem_u32(&sm.info_full[seg % kRing]));
-            ++seg;
-            return true;
-        };
-        // a segment is described, and its first block ids requested, behind the first loads of the one in
-        // front
-        Ahead now, then;
-        int32_t id = -1;
-        bool go = describe(now, id);
-        while (go && now.tiles >= 0) {
-            int32_t then_id = -1;
-            const int tiles = now.tiles, keys = now.keys, common = now.common;
-            for (int j = 0; go && j < (tiles > 0 ? tiles : 1); ++j) {
-                if (j == (tiles > 1 ? 1 : 0)) {
-                    go = describe(then, then_id);
-                    if (!go)
-                        break;
-                    if (tiles == 0)
-                        break;
-                }
-                const int kt = now.kt0 + j;
-                const int32_t blk = id;
-                id = block(now, kt + 1);          // a tile ahead of its copies
+            Walk<NG, Plan> walk(p, plan, sm.len, start);
+            Segment s;
+            const int per = p.page_shift >= 7 ? 1 : kKeys >> p.page_shift;      // pages of a tile
+            const int box = p.page_shift >= 7 ? kKeys : 1 << p.page_shift;      // keys of a copy
+            const int groups = 1 << (p.page_shift - 3);                         // 8-key rows of a page
+            const int32_t none = (int32_t)(p.num_blocks * 2 * groups);          // beyond the cache: zeros
+            uint32_t n = 0, st = 0, ph = 1;           // stages filled; the next one and the phase that frees it
+            uint32_t is_raw = 0, ph_raw = 0;          // by stage: filled behind `raw`; its last phase
+            struct Ahead {                            // a segment as it is loaded
+                int kt0, tiles, keys, common, kvh;
+                const int32_t *table;
+            };
+            // this lane's block id of a tile's pages
+            auto block = [&](const Ahead &x, int kt) -> int32_t {
                 const int first = kt * kKeys + lane * box;
-                const bool mine = lane < per && first < keys;
-                const bool good = blk >= 0 && blk < p.num_blocks;
-                if (mine && !good)
-                    report(p.d_err, HS_DEVERR_BLOCK_OOB);
-                const int pages = __popc(__ballot_sync(0xffffffffu, mine));
-                const int in_page = (first & ((1 << p.page_shift) - 1)) >> 3;
-                for (int plane = 0; plane < 2; ++plane) {
-                    // the first round of waits passes: no phase is over yet
-                    if (!wait(empty(st), ph)) {
-                        go = false;
-                        break;
-                    }
-                    const bool raw = plane == 1 && (kt + 1) * kKeys > common;
-                    const uint32_t bar = raw ? smem_u32(&sm.raw[st]) : full(st);
-                    is_raw = raw ? is_raw | 1u << st : is_raw & ~(1u << st);
-                    ph_raw ^= raw ? 1u << st : 0u;
-                    if (lane == 0)
-                        mbar_arrive_expect_tx(bar, (uint32_t)(pages * box * D * 2));
-                    __syncwarp();
-                    if (mine)
-                        tma_load_4d(st_at + st * C::kTile + lane * box * D * 2, &map, 0, 0,
-                                    now.kvh * kHalf,
-                                    good ? (blk * 2 + plane) * groups + in_page : none, bar);
-                    __syncwarp();
-                    ++n;
-                    if (++st == kSt) {
-                        st = 0;
-                        ph ^= 1;
-                    }
-                }
-            }
-            now = then;
-            id = then_id;
-        }
-        // the copies and MMAs in flight end (bounded) before their memory goes away
-        for (uint32_t i = n > kSt ? n - kSt : 0; i < n; ++i) {
-            const uint32_t at = i % kSt;
-            if (!wait(empty(at), (i / kSt) & 1)) {
-                if ((is_raw >> at) & 1)
-                    mbar_wait_bounded(smem_u32(&sm.raw[at]), ((ph_raw >> at) & 1) ^ 1, kTimeoutNs);
-                else
-                    mbar_wait_bounded(full(at), (i / kSt) & 1, kTimeoutNs);
-            }
-        }
-    } else if (warp >= C::kSoftmax && warp < C::kSoftmax + NG) {
-        fewer_registers<C::kLessRegs>();
-        // ---- MMAs, a warp to a group, in the order QK(0), PV(0), QK(1), PV(1), ...: the scores of the
-        // next tile overwrite the weights of the last one behind the product that reads them.  A stage
-        // is free once both groups are done with it
-        const int g = warp - C::kSoftmax;
-        const uint32_t s_at = tmem + g * 256, o_at = s_at + 128, p_at = s_at + C::kWeightsAt;
-        const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
-        const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
-        const uint32_t bar_r = smem_u32(&sm.s_read[g]);
-        const uint64_t q_desc = sdesc_sw128(q_at + g * C::kTile, 16, 1024);
-        const uint64_t k_desc = sdesc_sw128(st_at, 16, kHalf * 1024);
-        const uint64_t v_desc = sdesc_sw128(st_at, 1024, kHalf * 1024);
-        uint32_t st = 0, ph = 0;         // the stage at hand and the phase of its use
-        auto next_stage = [&]() {
-            if (++st == kSt) {
-                st = 0;
-                ph ^= 1;
-            }
-        };
-        auto qk = [&]() {                // the scores of the tile at hand; its stage is free behind them
-            if (elect_one()) {
-                const uint64_t b = k_desc + st * (C::kTile / 16);
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_f16_ss(s_at, q_desc + ((k >> 2) * 16384 + (k & 3) * 32) / 16,
-                               b + ((k >> 2) * 1024 + (k & 3) * 32) / 16, Elem<T>::idesc(kKeys, 0), k > 0);
-                tc_commit(bar_s);
-                tc_commit(empty(st));
-            }
-            __syncwarp();
-        };
-        auto pass = [&]() -> bool {      // a stage that this group has no use for
-            if (!wait(full(st), ph))
-                return false;
-            if (lane == 0)
-                mbar_arrive(empty(st));
-            __syncwarp();
-            next_stage();
-            return true;
-        };
-        // the next tile's scores, or its keys left to the other group
-        auto next_scores = [&](int j, int mine, int most) -> bool {
-            if (j + 1 < mine) {
-                if (!wait(full(st), ph))
+                if (kt >= x.kt0 + x.tiles || lane >= per || first >= x.keys)
+                    return -1;
+                return x.table[first >> p.page_shift];
+            };
+            // the next segment, described to the other warps; tiles = -1: there is none
+            uint32_t seg = 0;
+            auto describe = [&](Ahead &x, int32_t &id) -> bool {
+                Info *const info = &sm.info[seg % kRing];
+                const bool have = walk.next(s);
+                x.tiles = -1;
+                if (seg >= kRing && !wait(smem_u32(&sm.info_empty[seg % kRing]), (seg / kRing - 1) & 1))
                     return false;
-                tc_fence_after();
-                qk();
-                next_stage();
-            } else if (j + 1 < most) {
-                return pass();
+                if (have) {
+                    x.kt0 = s.kt0;
+                    x.kvh = s.kvh;
+                    x.keys = walk.all_keys(s);
+                    x.common = walk.common_keys(s);
+                    x.tiles = group_tiles(s, x.keys);
+                    x.table = s.b < 0 ? p.prefix_table : p.table + s.b * p.max_pages;
+                    id = block(x, x.kt0);             // on its way while the segment is described
+                    if (lane < NG) {
+                        // a decode step's own items have one tile of rows: the groups have them in turn
+                        const bool own_item = Plan::kDecode && s.b >= 0;
+                        const int q = NG == 2 && own_item ? lane ^ (int)(seg & 1) : lane;
+                        const int r0 = (s.rt * NG + q) * 128, left = s.rows - r0;
+                        const int t = s.b < 0 || !Plan::kDecode ? p.by_group.div(r0) : 0;
+                        const int own = walk.group_keys(s, q);
+                        info->g[lane].head = r0 - t * p.group;
+                        info->g[lane].rows = left < 0 ? 0 : left < 128 ? left : 128;
+                        info->g[lane].keys = own;
+                        info->g[lane].at = own_item ? 0 : lane * 128;
+                        info->g[lane].tiles = group_tiles(s, own);
+                        if constexpr (Plan::kDecode) {
+                            info->g[lane].row0 = s.b < 0 ? t : s.b;
+                            info->g[lane].key0 = x.keys;
+                        } else {
+                            info->g[lane].row0 = plan.req[s.b].row0 + t;
+                            info->g[lane].key0 = plan.req[s.b].pos0 + t + 1;
+                        }
+                    }
+                    if (lane == 0) {
+                        info->kt0 = s.kt0;
+                        info->all = x.keys;
+                        info->common = x.common;
+                        info->head0 = s.kvh * p.group;
+                        int rows = 0;
+                        info->slot = s.whole && (!Plan::kDecode || p.prefix_len == 0)
+                                         ? -1
+                                         : slot_of<D, NG, Plan>(p, s, cta, &rows);
+                        info->slot_rows = rows;
+                    }
+                }
+                if (lane == 0)
+                    info->most = x.tiles;
+                __syncwarp();
+                if (lane == 0)
+                    mbar_arrive(smem_u32(&sm.info_full[seg % kRing]));
+                ++seg;
+                return true;
+            };
+            // a segment is described, and its first block ids requested, behind the first loads of the one in
+            // front
+            Ahead now, then;
+            int32_t id = -1;
+            bool go = describe(now, id);
+            while (go && now.tiles >= 0) {
+                int32_t then_id = -1;
+                const int tiles = now.tiles, keys = now.keys, common = now.common;
+                for (int j = 0; go && j < (tiles > 0 ? tiles : 1); ++j) {
+                    if (j == (tiles > 1 ? 1 : 0)) {
+                        go = describe(then, then_id);
+                        if (!go)
+                            break;
+                        if (tiles == 0)
+                            break;
+                    }
+                    const int kt = now.kt0 + j;
+                    const int32_t blk = id;
+                    id = block(now, kt + 1);          // a tile ahead of its copies
+                    const int first = kt * kKeys + lane * box;
+                    const bool mine = lane < per && first < keys;
+                    const bool good = blk >= 0 && blk < p.num_blocks;
+                    if (mine && !good)
+                        report(p.d_err, HS_DEVERR_BLOCK_OOB);
+                    const int pages = __popc(__ballot_sync(0xffffffffu, mine));
+                    const int in_page = (first & ((1 << p.page_shift) - 1)) >> 3;
+                    for (int plane = 0; plane < 2; ++plane) {
+                        // the first round of waits passes: no phase is over yet
+                        if (!wait(empty(st), ph)) {
+                            go = false;
+                            break;
+                        }
+                        const bool raw = plane == 1 && (kt + 1) * kKeys > common;
+                        const uint32_t bar = raw ? smem_u32(&sm.raw[st]) : full(st);
+                        is_raw = raw ? is_raw | 1u << st : is_raw & ~(1u << st);
+                        ph_raw ^= raw ? 1u << st : 0u;
+                        if (lane == 0)
+                            mbar_arrive_expect_tx(bar, (uint32_t)(pages * box * D * 2));
+                        __syncwarp();
+                        if (mine)
+                            tma_load_4d(st_at + st * C::kTile + lane * box * D * 2, &map, 0, 0,
+                                        now.kvh * kHalf,
+                                        good ? (blk * 2 + plane) * groups + in_page : none, bar);
+                        __syncwarp();
+                        ++n;
+                        if (++st == kSt) {
+                            st = 0;
+                            ph ^= 1;
+                        }
+                    }
+                }
+                now = then;
+                id = then_id;
             }
-            return true;
-        };
-        uint32_t ph_q = 0, ph_p = 0, ph_turn = (uint32_t)g ^ 1;    // the first group has the first turn
-        bool go = true;
-        if (p.stall_for_test && g == 0)
-            go = wait(smem_u32(&sm.drain[0]), 0);     // only this warp commits to it, at the end
-        for (uint32_t seg = 0; go; ++seg) {
-            go = described(seg);
-            if (!go)
-                break;
-            const Info &info = sm.info[seg % kRing];
-            const int most = info.most, mine = info.g[g].tiles;
-            const int both = NG == 2 && !C::kOwnWeights ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
-            int left = info.g[g].keys - info.kt0 * kKeys;
-            done_with(seg);
-            if (most < 0)
-                break;
-            if (mine > 0) {
-                go = wait(bar_q, ph_q) && wait(full(st), ph);
-                ph_q ^= 1;
-                if (!go)
-                    break;
-                tc_fence_after();
-                qk();
-                next_stage();
-            } else if (most > 0) {
-                go = pass();
+            // the copies and MMAs in flight end (bounded) before their memory goes away
+            for (uint32_t i = n > kSt ? n - kSt : 0; i < n; ++i) {
+                const uint32_t at = i % kSt;
+                if (!wait(empty(at), (i / kSt) & 1)) {
+                    if ((is_raw >> at) & 1)
+                        mbar_wait_bounded(smem_u32(&sm.raw[at]), ((ph_raw >> at) & 1) ^ 1, kTimeoutNs);
+                    else
+                        mbar_wait_bounded(full(at), (i / kSt) & 1, kTimeoutNs);
+                }
             }
-            for (int j = 0; j < most && go; ++j, left -= kKeys) {
-                if (j >= mine) {
-                    go = pass() && (j + 1 == most || pass());
-                    continue;
+        } else if (warp >= C::kSoftmax && warp < C::kSoftmax + NG) {
+            // ---- MMAs, a warp to a group, in the order QK(0), PV(0), QK(1), PV(1), ...: the scores of the
+            // next tile overwrite the weights of the last one behind the product that reads them.  A stage
+            // is free once both groups are done with it
+            const int g = warp - C::kSoftmax;
+            const uint32_t s_at = tmem + g * 256, o_at = s_at + 128, p_at = s_at + C::kWeightsAt;
+            const uint32_t bar_q = smem_u32(&sm.q_full[g]), bar_s = smem_u32(&sm.s_full[g]);
+            const uint32_t bar_p = smem_u32(&sm.p_full[g]), bar_o = smem_u32(&sm.o_full[g]);
+            const uint32_t bar_r = smem_u32(&sm.s_read[g]);
+            const uint64_t q_desc = sdesc_sw128(q_at + g * C::kTile, 16, 1024);
+            const uint64_t k_desc = sdesc_sw128(st_at, 16, kHalf * 1024);
+            const uint64_t v_desc = sdesc_sw128(st_at, 1024, kHalf * 1024);
+            uint32_t st = 0, ph = 0;         // the stage at hand and the phase of its use
+            auto next_stage = [&]() {
+                if (++st == kSt) {
+                    st = 0;
+                    ph ^= 1;
                 }
-                const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
-                const uint32_t st_v = st, ph_v = ph;
-                if constexpr (C::kOwnWeights) {
-                    go = wait(bar_r, ph_p);
-                    next_stage();
-                    go = go && next_scores(j, mine, most);
-                }
-                go = go && wait(bar_p, ph_p) && wait(full(st_v), ph_v);
-                ph_p ^= 1;
-                // The groups take turns, a product with v and the next scores each.  Where both had their
-                // products in flight at once they ended at once, did their softmax at once and stayed so: 2.1 us
-                // a tile instead of 1.5.
-                if (go && j < both) {
-                    go = wait(smem_u32(&sm.turn[g]), ph_turn);
-                    ph_turn ^= 1;
-                }
-                if (!go)
-                    break;
-                tc_fence_after();
+            };
+            auto qk = [&]() {                // the scores of the tile at hand; its stage is free behind them
                 if (elect_one()) {
-                    const uint64_t b = v_desc + st_v * (C::kTile / 16);
-#pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        if (k < steps)
-                            mma_f16_ts(o_at, p_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
-                                       Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
-                    if (C::kOwnWeights || j + 1 == mine)
-                        tc_commit(bar_o);
-                    tc_commit(empty(st_v));
+                    const uint64_t b = k_desc + st * (C::kTile / 16);
+    #pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_f16_ss(s_at, q_desc + ((k >> 2) * 16384 + (k & 3) * 32) / 16,
+                                   b + ((k >> 2) * 1024 + (k & 3) * 32) / 16, Elem<T>::idesc(kKeys, 0), k > 0);
+                    tc_commit(bar_s);
+                    tc_commit(empty(st));
                 }
                 __syncwarp();
-                if constexpr (!C::kOwnWeights) {
+            };
+            auto pass = [&]() -> bool {      // a stage that this group has no use for
+                if (!wait(full(st), ph))
+                    return false;
+                if (lane == 0)
+                    mbar_arrive(empty(st));
+                __syncwarp();
+                next_stage();
+                return true;
+            };
+            // the next tile's scores, or its keys left to the other group
+            auto next_scores = [&](int j, int mine, int most) -> bool {
+                if (j + 1 < mine) {
+                    if (!wait(full(st), ph))
+                        return false;
+                    tc_fence_after();
+                    qk();
                     next_stage();
-                    go = next_scores(j, mine, most);
-                    if (!go)
-                        break;
+                } else if (j + 1 < most) {
+                    return pass();
                 }
-                if (j < both) {
-                    if (lane == 0)
-                        mbar_arrive(smem_u32(&sm.turn[1 - g]));
-                    __syncwarp();
-                }
-            }
-        }
-        if (*abort != 0) {
-            // the MMAs in flight end (bounded) before their memory goes away
-            if (elect_one()) {
-                tc_commit(smem_u32(&sm.drain[g]));
-                mbar_wait_bounded(smem_u32(&sm.drain[g]), 0, kTimeoutNs);
-            }
-            __syncwarp();
-        }
-    } else if (warp >= C::kSoftmax) {
-        fewer_registers<C::kLessRegs>();
-        // ---- values at masked places: the warps that are left
-        constexpr int kWho = (3 - NG) * 32, kRows = kWho / (D / 8);     // rows that they take at once
-        uint32_t st_v = 1, ph_raw = 0;         // the stage of the next value tile
-        const int who = tid - (C::kSoftmax + NG) * 32;
-        auto pair_and = [](bool x) {
-            int r;
-            asm volatile("{\n\t.reg .pred p, q;\n\t"
-                         "setp.ne.s32 p, %1, 0;\n\t"
-                         "bar.red.and.pred q, 1, %2, p;\n\t"
-                         "selp.s32 %0, 1, 0, q;\n\t}"
-                         : "=r"(r)
-                         : "r"((int)x), "n"(kWho)
-                         : "memory");
-            return r != 0;
-        };
-        auto pair_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWho) : "memory"); };
-        bool go = true;
-        for (uint32_t seg = 0; go; ++seg) {
-            go = pair_and(described(seg));
-            if (!go)
-                break;
-            const Info &info = sm.info[seg % kRing];
-            const int tiles = info.most, all = info.all, common = info.common, kt0 = info.kt0;
-            if (tiles < 0)
-                break;
-            int32_t *const any = &sm.marks.any[seg % kRing], *const from = sm.marks.from[seg % kRing];
-            bool clean = Plan::kDecode;              // a decode step has no keys that only some rows see
-            for (int j = 0; j < tiles; ++j, st_v = (st_v + 2) % kSt) {
-                const int k0 = (kt0 + j) * kKeys;
-                if (k0 + kKeys <= common)
-                    continue;
-                if (!clean) {
-                    for (int i = who; i < D; i += kWho)
-                        from[i] = INT_MAX;
-                    if (who == 0)
-                        *any = 0;
-                    clean = true;
-                    pair_sync();
-                }
-                const uint32_t st = st_v;
-                // these warps go on or none: they meet in a plain barrier below
-                go = pair_and(wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1));
-                ph_raw ^= 1u << st;
+                return true;
+            };
+            uint32_t ph_q = 0, ph_p = 0, ph_turn = (uint32_t)g ^ 1;    // the first group has the first turn
+            bool go = true;
+            if (p.stall_for_test && g == 0)
+                go = wait(smem_u32(&sm.drain[0]), 0);     // only this warp commits to it, at the end
+            for (uint32_t seg = 0; go; ++seg) {
+                go = described(seg);
                 if (!go)
                     break;
-                uint8_t *const v = smem_raw + (NG + st) * C::kTile;
-                // rows [common, all) are searched, rows behind them up to a step of the MMA zeroed
-                const int lo = common > k0 ? common - k0 : 0;
-                const int hi = all - k0 < kKeys ? all - k0 : kKeys;
-                const int end = (hi + 15) / 16 * 16;
-                // 16 bytes at a time: chunk x of row r is chunk x & 7 of half x >> 3, swizzled
-                auto chunk = [&](int r, int x) {
-                    return reinterpret_cast<uint4 *>(v + ((r >> 3) * kHalf + (x >> 3)) * 1024 +
-                                                     (r & 7) * 128 + (((x & 7) ^ (r & 7)) << 4));
-                };
-                const int x = who % (D / 8), r_who = who / (D / 8);
-                for (int r = hi + r_who; r < end; r += kRows)
-                    *chunk(r, x) = make_uint4(0, 0, 0, 0);
-                if (lo < hi)
-                    pair_sync();
-                // Searched are whole atoms of 8 rows, kRows of them at a time, so that a lane's places in
-                // an atom are constants; a product with zero for two values says whether one is not finite.
-                // (Testing exponents took over 10 us a tile of 128 rows: 8k tokens of 32 heads of their own
-                // 574 us instead of 398.)
-                for (int a0 = lo >> 3; lo < hi && a0 < (hi + 7) >> 3; a0 += kRows) {
-                    uint4 y[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int r = (a0 + k * kRows / 8) * 8 + k * kRows % 8 + r_who;
-                        y[k] = a0 + k * kRows / 8 < (hi + 7) >> 3 ? *chunk(r, x) : make_uint4(0, 0, 0, 0);
-                    }
-                    uint32_t z[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        z[0] = Elem<T>::plus_zero_times(z[0], y[k].x);
-                        z[1] = Elem<T>::plus_zero_times(z[1], y[k].y);
-                        z[2] = Elem<T>::plus_zero_times(z[2], y[k].z);
-                        z[3] = Elem<T>::plus_zero_times(z[3], y[k].w);
-                    }
-                    if (((z[0] | z[1] | z[2] | z[3]) & 0x7FFF7FFFu) == 0)
+                const Info &info = sm.info[seg % kRing];
+                const int most = info.most, mine = info.g[g].tiles;
+                const int both = NG == 2 && !C::kOwnWeights ? min(mine, info.g[(g + 1) % NG].tiles) : 0;
+                int left = info.g[g].keys - info.kt0 * kKeys;
+                done_with(seg);
+                if (most < 0)
+                    break;
+                if (mine > 0) {
+                    go = wait(bar_q, ph_q) && wait(full(st), ph);
+                    ph_q ^= 1;
+                    if (!go)
+                        break;
+                    tc_fence_after();
+                    qk();
+                    next_stage();
+                } else if (most > 0) {
+                    go = pass();
+                }
+                for (int j = 0; j < most && go; ++j, left -= kKeys) {
+                    if (j >= mine) {
+                        go = pass() && (j + 1 == most || pass());
                         continue;
-                    for (int k = 0; k < 8; ++k) {
-                        const int r = a0 * 8 + k * kRows + r_who;
-                        if (r < lo || r >= hi)
-                            continue;
-                        uint16_t *const e = reinterpret_cast<uint16_t *>(chunk(r, x));
-                        for (int w = 0; w < 8; ++w)
-                            if ((not_finite<T>(e[w]) & 0x8000u) != 0) {
-                                atomicMin(&from[x * 8 + w], k0 + r);
-                                e[w] = 0;
-                                *any = 1;
-                            }
+                    }
+                    const int steps = left >= kKeys ? kKeys / 16 : (left + 15) / 16;
+                    const uint32_t st_v = st, ph_v = ph;
+                    if constexpr (C::kOwnWeights) {
+                        go = wait(bar_r, ph_p);
+                        next_stage();
+                        go = go && next_scores(j, mine, most);
+                    }
+                    go = go && wait(bar_p, ph_p) && wait(full(st_v), ph_v);
+                    ph_p ^= 1;
+                    // The groups take turns, a product with v and the next scores each.  Where both had their
+                    // products in flight at once they ended at once, did their softmax at once and stayed so:
+                    // 2.1 us a tile instead of 1.5.
+                    if (go && j < both) {
+                        go = wait(smem_u32(&sm.turn[g]), ph_turn);
+                        ph_turn ^= 1;
+                    }
+                    if (!go)
+                        break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t b = v_desc + st_v * (C::kTile / 16);
+    #pragma unroll
+                        for (int k = 0; k < kKeys / 16; ++k)
+                            if (k < steps)
+                                mma_f16_ts(o_at, p_at + k * 8, b + k * 2 * kHalf * 1024 / 16,
+                                           Elem<T>::idesc(D, 1), (uint32_t)(j > 0 || k > 0));
+                        if (C::kOwnWeights || j + 1 == mine)
+                            tc_commit(bar_o);
+                        tc_commit(empty(st_v));
+                    }
+                    __syncwarp();
+                    if constexpr (!C::kOwnWeights) {
+                        next_stage();
+                        go = next_scores(j, mine, most);
+                        if (!go)
+                            break;
+                    }
+                    if (j < both) {
+                        if (lane == 0)
+                            mbar_arrive(smem_u32(&sm.turn[1 - g]));
+                        __syncwarp();
                     }
                 }
-                fence_proxy_async_smem();
-                pair_sync();
-                if (who == 0)
-                    mbar_arrive(full(st));
             }
-            if (go)
-                done_with(seg);
+            if (*abort != 0) {
+                // the MMAs in flight end (bounded) before their memory goes away
+                if (elect_one()) {
+                    tc_commit(smem_u32(&sm.drain[g]));
+                    mbar_wait_bounded(smem_u32(&sm.drain[g]), 0, kTimeoutNs);
+                }
+                __syncwarp();
+            }
+        } else {
+            // ---- values at masked places: the warps that are left
+            constexpr int kWho = (3 - NG) * 32, kRows = kWho / (D / 8);     // rows that they take at once
+            uint32_t st_v = 1, ph_raw = 0;         // the stage of the next value tile
+            const int who = tid - (C::kSoftmax + NG) * 32;
+            auto pair_and = [](bool x) {
+                int r;
+                asm volatile("{\n\t.reg .pred p, q;\n\t"
+                             "setp.ne.s32 p, %1, 0;\n\t"
+                             "bar.red.and.pred q, 1, %2, p;\n\t"
+                             "selp.s32 %0, 1, 0, q;\n\t}"
+                             : "=r"(r)
+                             : "r"((int)x), "n"(kWho)
+                             : "memory");
+                return r != 0;
+            };
+            auto pair_sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(kWho) : "memory"); };
+            bool go = true;
+            for (uint32_t seg = 0; go; ++seg) {
+                go = pair_and(described(seg));
+                if (!go)
+                    break;
+                const Info &info = sm.info[seg % kRing];
+                const int tiles = info.most, all = info.all, common = info.common, kt0 = info.kt0;
+                if (tiles < 0)
+                    break;
+                int32_t *const any = &sm.marks.any[seg % kRing], *const from = sm.marks.from[seg % kRing];
+                bool clean = Plan::kDecode;              // a decode step has no keys that only some rows see
+                for (int j = 0; j < tiles; ++j, st_v = (st_v + 2) % kSt) {
+                    const int k0 = (kt0 + j) * kKeys;
+                    if (k0 + kKeys <= common)
+                        continue;
+                    if (!clean) {
+                        for (int i = who; i < D; i += kWho)
+                            from[i] = INT_MAX;
+                        if (who == 0)
+                            *any = 0;
+                        clean = true;
+                        pair_sync();
+                    }
+                    const uint32_t st = st_v;
+                    // these warps go on or none: they meet in a plain barrier below
+                    go = pair_and(wait(smem_u32(&sm.raw[st]), (ph_raw >> st) & 1));
+                    ph_raw ^= 1u << st;
+                    if (!go)
+                        break;
+                    uint8_t *const v = smem_raw + (NG + st) * C::kTile;
+                    // rows [common, all) are searched, rows behind them up to a step of the MMA zeroed
+                    const int lo = common > k0 ? common - k0 : 0;
+                    const int hi = all - k0 < kKeys ? all - k0 : kKeys;
+                    const int end = (hi + 15) / 16 * 16;
+                    // 16 bytes at a time: chunk x of row r is chunk x & 7 of half x >> 3, swizzled
+                    auto chunk = [&](int r, int x) {
+                        return reinterpret_cast<uint4 *>(v + ((r >> 3) * kHalf + (x >> 3)) * 1024 +
+                                                         (r & 7) * 128 + (((x & 7) ^ (r & 7)) << 4));
+                    };
+                    const int x = who % (D / 8), r_who = who / (D / 8);
+                    for (int r = hi + r_who; r < end; r += kRows)
+                        *chunk(r, x) = make_uint4(0, 0, 0, 0);
+                    if (lo < hi)
+                        pair_sync();
+                    // Searched are whole atoms of 8 rows, kRows of them at a time, so that a lane's places in
+                    // an atom are constants; a product with zero for two values says whether one is not finite.
+                    // (Testing exponents took over 10 us a tile of 128 rows: 8k tokens of 32 heads of their own
+                    // 574 us instead of 398.)
+                    for (int a0 = lo >> 3; lo < hi && a0 < (hi + 7) >> 3; a0 += kRows) {
+                        uint4 y[8];
+    #pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int r = (a0 + k * kRows / 8) * 8 + k * kRows % 8 + r_who;
+                            y[k] = a0 + k * kRows / 8 < (hi + 7) >> 3 ? *chunk(r, x) : make_uint4(0, 0, 0, 0);
+                        }
+                        uint32_t z[4] = {0, 0, 0, 0};
+    #pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            z[0] = Elem<T>::plus_zero_times(z[0], y[k].x);
+                            z[1] = Elem<T>::plus_zero_times(z[1], y[k].y);
+                            z[2] = Elem<T>::plus_zero_times(z[2], y[k].z);
+                            z[3] = Elem<T>::plus_zero_times(z[3], y[k].w);
+                        }
+                        if (((z[0] | z[1] | z[2] | z[3]) & 0x7FFF7FFFu) == 0)
+                            continue;
+                        for (int k = 0; k < 8; ++k) {
+                            const int r = a0 * 8 + k * kRows + r_who;
+                            if (r < lo || r >= hi)
+                                continue;
+                            uint16_t *const e = reinterpret_cast<uint16_t *>(chunk(r, x));
+                            for (int w = 0; w < 8; ++w)
+                                if ((not_finite<T>(e[w]) & 0x8000u) != 0) {
+                                    atomicMin(&from[x * 8 + w], k0 + r);
+                                    e[w] = 0;
+                                    *any = 1;
+                                }
+                        }
+                    }
+                    fence_proxy_async_smem();
+                    pair_sync();
+                    if (who == 0)
+                        mbar_arrive(full(st));
+                }
+                if (go)
+                    done_with(seg);
+            }
         }
     } else {
         // ---- softmax: thread = row
