@@ -810,44 +810,12 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         shift = -to;
                         far = ok && fabsf(to) > kFar;
                     }
-                    // Far from zero the scores are rounded before m is taken off, as their maximum was, and
-                    // what is left of them is brought back to the scale of the others.  In a loop of 16
-                    // columns, through the columns of the weights: as straight code, which hardly any call
-                    // runs, it cost the others up to 6 % (two 8k-token prompts of 64-wide heads 552 us instead
-                    // of 519), and asking for it by a second vote a tile as much.
-                    if (__builtin_expect(__any_sync(0xffffffffu, far), 0)) {
-                        if (far) {               // where 8 or 15 is half a step of float32 or less
-                            to = up && top - to > Elem<T>::kMost ? top : to;
-                            limit = to + Elem<T>::kMost;
-                            limit = limit - to > Elem<T>::kMost ? to : limit;
-                            shift = 0.f;
-                        }
-                        const float back = 1.f / p.scale_log2;
-                        last_product();
-#pragma unroll
-                        for (int h = 0; h < kKeys; h += 64) {
-#pragma unroll
-                            for (int c = 0; c < 64; c += 16)
-                                tmem_st16(p_at + c, *reinterpret_cast<uint32_t(*)[16]>(&x[h + c]));
-                            tmem_wait_st();
-#pragma unroll 1
-                            for (int c = 0; c < 64; c += 16) {
-                                uint32_t a[16];
-                                tmem_ld16(p_at + c, a);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const float y = __uint_as_float(a[i]);
-                                    const float z = __fsub_rn(__fmul_rn(y, p.scale_log2), to) * back;
-                                    a[i] = far ? __float_as_uint(z) : a[i];
-                                }
-                                tmem_st16(p_at + c, a);
-                            }
-                            tmem_wait_st();
-                            tmem_ld32(p_at, *reinterpret_cast<float(*)[32]>(&x[h]));
-                            tmem_ld32(p_at + 32, *reinterpret_cast<float(*)[32]>(&x[h + 32]));
-                            tmem_wait_ld();
-                        }
+                    const bool any_far = __any_sync(0xffffffffu, far);
+                    if (__builtin_expect(any_far, 0) && far) {  // where 8 or 15 is half a step of float32 or less
+                        to = up && top - to > Elem<T>::kMost ? top : to;
+                        limit = to + Elem<T>::kMost;
+                        limit = limit - to > Elem<T>::kMost ? to : limit;
+                        shift = 0.f;
                     }
                     const float f = up ? ex2(m - to) : 1.f;
                     m = to;
@@ -864,6 +832,39 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                             for (int i = 0; i < 16; ++i)
                                 a[i] = __float_as_uint(__uint_as_float(a[i]) * f);
                             tmem_st16(o_at + c, a);
+                        }
+                    }
+                    // Far from zero the scores are rounded before m is taken off, as their maximum was, and
+                    // what is left of them is brought back to the scale of the others.  In a loop of 16
+                    // columns, through the columns of the weights, which are free by now: code that hardly
+                    // any call runs makes the others wait for theirs (as straight code, two 8k-token prompts
+                    // of 64-wide heads 546 us, so 528; 519 without).  Not in pairs: a product and a sum of
+                    // two float32 each become one fused instruction.
+                    if (__builtin_expect(any_far, 0)) {
+                        const float by = far ? p.scale_log2 : 1.f, off = far ? m : 0.f, back = 1.f / by;
+                        constexpr int kPart = C::kOwnWeights ? 64 : 128;
+#pragma unroll
+                        for (int h = 0; h < kKeys; h += kPart) {
+#pragma unroll
+                            for (int c = 0; c < kPart; c += 16)
+                                tmem_st16(p_at + c, *reinterpret_cast<uint32_t(*)[16]>(&x[h + c]));
+                            tmem_wait_st();
+#pragma unroll 1
+                            for (int c = 0; c < kPart; c += 16) {
+                                uint32_t a[16];
+                                tmem_ld16(p_at + c, a);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    a[i] = __float_as_uint(
+                                        __fsub_rn(__fmul_rn(__uint_as_float(a[i]), by), off) * back);
+                                tmem_st16(p_at + c, a);
+                            }
+                            tmem_wait_st();
+#pragma unroll
+                            for (int c = 0; c < kPart; c += 32)
+                                tmem_ld32(p_at + c, *reinterpret_cast<float(*)[32]>(&x[h + c]));
+                            tmem_wait_ld();
                         }
                     }
                 }
