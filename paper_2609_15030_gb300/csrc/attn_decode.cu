@@ -125,6 +125,7 @@ int64_t plan_attn_decode(AttnParams &p, int d, int sm_count)
         return -1;
     p.ctas = (int)(units < most ? units : most);
     const int longest = tiles_of(p.max_kv > p.prefix_len ? p.max_kv : p.prefix_len);
+    p.limit_ns = wait_limit_ns(p, longest, units);
     p.parts = (int)(longest / (units / p.ctas > 0 ? units / p.ctas : 1)) + 2;
     if (p.prefix_len > 0) {
         p.joined = 1;

@@ -73,6 +73,7 @@ struct AttnParams {
     int32_t joined;               // partial results are left and joined
     int32_t stall_for_test;       // one wait that nothing completes (failure-detection tests)
     float scale_log2;             // scale * log2(e)
+    uint64_t limit_ns;            // after which a wait of the kernel has run out
     Divisor by_group, by_kv;      // group, n_kv
 };
 

@@ -110,6 +110,7 @@ bool schedule(AttnParams &p, PrefillPlan &plan, int most)
         }
     p.units = (int)units;
     p.ctas = (int)(units < most ? units : most);
+    p.limit_ns = wait_limit_ns(p, longest, units);
     p.n_split = 0;
     if (better_whole(p, items, longest - p.extra, units))
         p.unsplit = 1;

@@ -62,7 +62,7 @@ using namespace ptx;
 
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFar = 1048576.f;         // scores that are rounded before m is taken off (units of log2)
-constexpr uint64_t kTimeoutNs = 1000000000ull;
+constexpr uint64_t kTimeoutNs = 1000000000ull;       // for copies and MMAs in flight to end
 
 // ---- shapes of a launch --------------------------------------------------------------------
 
@@ -236,7 +236,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
         if (!ok) {
             const uint64_t t0 = globaltimer_ns();
             while (!(ok = mbar_try_wait(bar, parity)) && *abort == 0) {
-                if (globaltimer_ns() - t0 > kTimeoutNs)
+                if (globaltimer_ns() - t0 > p.limit_ns)
                     *abort = 1;
             }
         }

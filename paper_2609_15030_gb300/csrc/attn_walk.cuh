@@ -76,6 +76,15 @@ inline bool better_whole(const AttnParams &p, int64_t items, int longest, int64_
     return (items <= p.ctas ? 0 : share) + longest <= share + 3;
 }
 
+// How long a wait may take.  Most are for a step of one tile (3 us at most, with HBM shared by all), but the
+// warps that search values, and a group of rows without any in a segment, wait for another one's whole run of
+// tiles: the longest item and an even share at most.  (At 0.65 us a tile one CTA's 200 million keys
+// take longer than 1 s.)
+inline uint64_t wait_limit_ns(const AttnParams &p, int longest, int64_t units)
+{
+    return 1000000000ull + 20000ull * (uint64_t)(units / p.ctas + longest);
+}
+
 // one item's key tiles [kt0, kt1) as one CTA has them
 struct Segment {
     int b, rt, kvh, kt0, kt1;

@@ -1,6 +1,6 @@
 // The host side of the attention calls' schedule, for tests/test_attn_schedule.py: no GPU is used.
 //   schedule shares                                              check first_unit and cta_of
-//   schedule decode BATCH HEADS KV_HEADS D MAX_KV PREFIX SMS     print "unsplit joined ctas bytes"
+//   schedule decode BATCH HEADS KV_HEADS D MAX_KV PREFIX SMS [UNSPLIT]  print "unsplit joined ctas bytes limit_ns"
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -45,7 +45,7 @@ int main(int argc, char **argv)
 {
     if (argc == 2 && !std::strcmp(argv[1], "shares"))
         return shares();
-    if (argc == 9 && !std::strcmp(argv[1], "decode")) {
+    if ((argc == 9 || argc == 10) && !std::strcmp(argv[1], "decode")) {
         int a[7];
         for (int i = 0; i < 7; ++i)
             a[i] = std::atoi(argv[2 + i]);
@@ -59,8 +59,10 @@ int main(int argc, char **argv)
         p.by_kv.set(p.n_kv);
         p.max_kv = a[4];
         p.prefix_len = a[5];
+        p.unsplit = argc == 10 ? std::atoi(argv[9]) : 0;
         const int64_t bytes = plan_attn_decode(p, a[3], a[6]);
-        std::printf("%d %d %d %lld\n", p.unsplit, p.joined, p.ctas, (long long)bytes);
+        std::printf("%d %d %d %lld %llu\n", p.unsplit, p.joined, p.ctas, (long long)bytes,
+                    (unsigned long long)p.limit_ns);
         return 0;
     }
     return 2;

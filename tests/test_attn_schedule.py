@@ -31,7 +31,7 @@ def test_every_unit_is_one_ctas(schedule):
 
 
 def decode(schedule, batch, kv_heads, max_kv, d=128, prefix=0, sms=152):
-    unsplit, joined, _, size = schedule("decode", batch, 4 * kv_heads, kv_heads, d, max_kv, prefix, sms)
+    unsplit, joined, _, size, _ = schedule("decode", batch, 4 * kv_heads, kv_heads, d, max_kv, prefix, sms)
     assert joined == (not unsplit) and (size > 0) == bool(joined)
     return bool(unsplit)
 
@@ -47,3 +47,14 @@ def test_decode_steps_of_short_bounds_are_not(schedule):
     for batch, kv_heads in ((38, 8), (64, 4), (1, 2), (384, 8)):
         for max_kv in (0, 1, 128, 300, 384):
             assert decode(schedule, batch, kv_heads, max_kv), (batch, kv_heads, max_kv)
+
+
+@pytest.mark.parametrize("unsplit", [0, 1])
+@pytest.mark.parametrize("batch,max_kv,prefix", [(1, 1 << 20, 0), (1, 200_000_000, 0), (384, 300, 0),
+                                                 (33, 200_000_000, 100), (64, 10, 1 << 30)])
+def test_waits_last_as_long_as_the_work_may(schedule, batch, max_kv, prefix, unsplit):
+    """1 s, and beside it more than the longest run of tiles takes (1.5 us each for two tiles of rows)."""
+    *_, limit = schedule("decode", batch, 4, 1, 64, max_kv, prefix, 152, unsplit)
+    longest = max(max_kv, prefix) // 128
+    assert limit >= 1_000_000_000 + 10 * 1_500 * (longest if unsplit else longest // 304)
+    assert limit < 3_000_000_000 or longest > 50_000
