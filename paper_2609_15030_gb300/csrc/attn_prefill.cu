@@ -73,9 +73,12 @@ attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, const __grid_con
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
     T *const o = static_cast<T *>(p.o) + row * p.o_stride + head * D + col;
 #pragma unroll
+    for (int e = 0; e < E; ++e)
+        a[e] = Elem<T>::in_range(a[e] * inv);
+#pragma unroll
     for (int e = 0; e < E; e += 4)
-        *reinterpret_cast<uint2 *>(o + e) = make_uint2(Elem<T>::pack(a[e] * inv, a[e + 1] * inv),
-                                                       Elem<T>::pack(a[e + 2] * inv, a[e + 3] * inv));
+        *reinterpret_cast<uint2 *>(o + e) = make_uint2(Elem<T>::pack(a[e], a[e + 1]),
+                                                       Elem<T>::pack(a[e + 2], a[e + 3]));
     if (p.lse != nullptr && col == 0)
         p.lse[row * p.n_heads + head] = l == 0.f ? -INFINITY : kLn2 * (m + log2f(l));
 }

@@ -149,6 +149,8 @@ struct Elem<__nv_bfloat16> {
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
         return r;
     }
+    // an output in its range: what the sums give (below 2^128)
+    static __device__ __forceinline__ float in_range(float x) { return x; }
     static constexpr uint32_t idesc(int N, int mn) { return idesc_bf16(128, N, mn); }
     static __device__ __forceinline__ uint32_t plus_zero_times(uint32_t z, uint32_t x)
     {
@@ -165,6 +167,12 @@ struct Elem<__half> {
         uint32_t r;
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
         return r;
+    }
+    // averages of finite values are at most 65504; by the weights' rounding they come out up to 2^-11 above,
+    // which would round to infinity
+    static __device__ __forceinline__ float in_range(float x)
+    {
+        return fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.f), 65504.f) : x;
     }
     static constexpr uint32_t idesc(int N, int mn) { return idesc_f16(128, N, mn); }
     static __device__ __forceinline__ uint32_t plus_zero_times(uint32_t z, uint32_t x)
@@ -950,14 +958,15 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                 for (int c = 0; c < D; c += 32) {
                     float a[32];
                     columns(c, a);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        a[i] = Elem<T>::in_range(a[i] * inv);
                     uint4 v[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int i = 8 * k;
-                        v[k] = make_uint4(Elem<T>::pack(a[i] * inv, a[i + 1] * inv),
-                                          Elem<T>::pack(a[i + 2] * inv, a[i + 3] * inv),
-                                          Elem<T>::pack(a[i + 4] * inv, a[i + 5] * inv),
-                                          Elem<T>::pack(a[i + 6] * inv, a[i + 7] * inv));
+                        v[k] = make_uint4(Elem<T>::pack(a[i], a[i + 1]), Elem<T>::pack(a[i + 2], a[i + 3]),
+                                          Elem<T>::pack(a[i + 4], a[i + 5]), Elem<T>::pack(a[i + 6], a[i + 7]));
                     }
                     swap_chunks(v[0], v[1], lane & 1, 1);
                     swap_chunks(v[2], v[3], lane & 1, 1);
@@ -1114,7 +1123,7 @@ __device__ __forceinline__ void write_row(const AttnParams &p, const Joined<D> &
                                                lane * (D / 32));
 #pragma unroll
     for (int i = 0; i < D / 32; i += 2)
-        o[i / 2] = Elem<T>::pack(x.a[i] * inv, x.a[i + 1] * inv);
+        o[i / 2] = Elem<T>::pack(Elem<T>::in_range(x.a[i] * inv), Elem<T>::in_range(x.a[i + 1] * inv));
     if (p.lse != nullptr && lane == 0)
         p.lse[row * p.n_heads + head] = x.l == 0.f ? -INFINITY : kLn2 * (x.m + log2f(x.l));
 }

@@ -102,3 +102,46 @@ def test_a_row_far_from_zero_leaves_its_neighbours_their_bits(dev):
     assert torch.equal(o[keep], ref[keep])
     assert torch.equal(out.lse[:60].cpu()[keep], clean.lse[:60].cpu()[keep])
     assert torch.isfinite(out.o[11, 128:256].float()).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("call", ["prefill", "unsplit", "decode", "shared"])
+def test_averages_of_the_largest_values_are_finite(dev, call, d):
+    """Columns of 65504, of -65504 and of both: averages lie between them, and what the weights' rounding (2^-11)
+    puts above rounds to the largest number, not to infinity.  Infinities in the values stay."""
+    kv_len = [900, 333, 1, 260]
+    p = Problem(45, 16, 2, d, 16, "fp16", kv_len, 60 if call in ("prefill", "unsplit") else 4,
+                prefix_len=500 if call == "shared" else 0)
+    p.scale = 1.0
+    g = torch.Generator().manual_seed(46)
+    q = torch.zeros(p.rows, 16, d)
+    q[..., 0] = 0.5 + torch.rand(p.rows, 16, generator=g) / 2
+    p.q[:p.rows, :16 * d] = q.reshape(p.rows, -1).half()
+    sign = torch.ones(d)
+    sign[1::3] = -1
+    for b, (k, v) in enumerate(zip([p.kp] + p.K, [p.vp] + p.V)):
+        # one key of 0, a later tile's of up to 6.5 (log2): a weight that is no power of two; the others below 2^-70
+        k.zero_()
+        k[..., 0] = -100
+        k[10:11, :, 0], k[200:201, :, 0] = 0, 4.5
+        v[:] = (65504.0 * sign).half()
+        v[::2, :, 5::7] *= -1
+        ids = p.prefix_table if b == 0 else p.table[b - 1, :-(-k.shape[0] // 16)]
+        for plane, x in enumerate((k, v)):
+            flat = torch.full((ids.numel() * 16, 2, d), math.nan, dtype=x.dtype)
+            flat[:x.shape[0]] = x
+            p.cache[ids.long(), plane] = flat.reshape(-1, 16, 2, d)
+    if call in ("prefill", "unsplit"):
+        pos0, n, cu = [858, 0, 0, 245], [42, 2, 1, 15], [0, 42, 44, 45, 60]
+        out = run_prefill(p, pos0, n, dev, unsplit=call == "unsplit", scale=1.0)
+        rows = list(p.prefill_rows(pos0, n, cu))
+    else:
+        out = run_decode(p, kv_len, 900, dev, shared=call == "shared", scale=1.0)
+        rows = list(p.decode_rows(kv_len))
+    assert torch.isfinite(out.o[:p.rows, :16 * d].float()).all()
+    out.check(rows)
+    p.cache[p.table[0, 2].long(), 1, 4, :, 9] = math.inf       # key 36 of the first request
+    out = run_prefill(p, pos0, n, dev, scale=1.0) if call in ("prefill", "unsplit") else \
+        run_decode(p, kv_len, 900, dev, shared=call == "shared", scale=1.0)
+    o = out.o[0, :16 * d].reshape(16, d).float()
+    assert not torch.isfinite(o[:, 9]).any() and torch.isfinite(o[:, :9]).all()
