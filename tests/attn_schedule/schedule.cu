@@ -1,6 +1,7 @@
 // The host side of the attention calls' schedule, for tests/test_attn_schedule.py: no GPU is used.
 //   schedule shares                                              check first_unit and cta_of
 //   schedule decode BATCH HEADS KV_HEADS D MAX_KV PREFIX SMS [UNSPLIT]  print "unsplit joined ctas bytes limit_ns"
+//   schedule prefill HEADS KV_HEADS D SMS POS0 N [POS0 N ...]    print "unsplit joined groups units n_split"
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -63,6 +64,24 @@ int main(int argc, char **argv)
         const int64_t bytes = plan_attn_decode(p, a[3], a[6]);
         std::printf("%d %d %d %lld %llu\n", p.unsplit, p.joined, p.ctas, (long long)bytes,
                     (unsigned long long)p.limit_ns);
+        return 0;
+    }
+    if (argc >= 8 && argc % 2 == 0 && !std::strcmp(argv[1], "prefill")) {
+        static PrefillPlan plan;
+        AttnParams p;
+        std::memset(&p, 0, sizeof p);
+        p.batch = (argc - 6) / 2;
+        p.n_heads = std::atoi(argv[2]);
+        p.n_kv = std::atoi(argv[3]);
+        p.group = p.n_heads / p.n_kv;
+        p.by_group.set(p.group);
+        p.by_kv.set(p.n_kv);
+        for (int b = 0; b < p.batch; ++b) {
+            plan.req[b].pos0 = std::atoi(argv[6 + 2 * b]);
+            plan.req[b].n = std::atoi(argv[7 + 2 * b]);
+        }
+        plan_attn_prefill(p, plan, std::atoi(argv[4]), std::atoi(argv[5]));
+        std::printf("%d %d %d %d %d\n", p.unsplit, p.joined, p.groups, p.units, p.n_split);
         return 0;
     }
     return 2;

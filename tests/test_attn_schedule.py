@@ -6,6 +6,7 @@ import subprocess
 import pytest
 
 from paper_2609_15030_gb300 import build
+from tests.attn_cases import MANY_SPLIT
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -58,3 +59,17 @@ def test_waits_last_as_long_as_the_work_may(schedule, batch, max_kv, prefix, uns
     longest = max(max_kv, prefix) // 128
     assert limit >= 1_000_000_000 + 10 * 1_500 * (longest if unsplit else longest // 304)
     assert limit < 3_000_000_000 or longest > 50_000
+
+
+def test_the_gpu_tests_reach_both_joins_and_both_counts(schedule):
+    """What tests/test_gpu_attn_bounds.py runs, on 152 SMs: more than 64 split items with one and with two tiles of
+    rows (the join that takes all columns in one block), and more than 2^22 units."""
+    for heads, kv_heads, pos0, n in MANY_SPLIT:
+        lengths = [x for pair in zip(pos0, n) for x in pair]
+        for d in (64, 128):
+            unsplit, joined, groups, _, n_split = schedule("prefill", heads, kv_heads, d, 152, *lengths)
+            assert not unsplit and joined and n_split > 64
+            assert groups == (2 if max(n) * heads // kv_heads > 128 else 1)
+    assert schedule("prefill", 32, 8, 64, 152, 0, 131_072)[3] > 1 << 22
+    _, _, ctas, _, _ = schedule("decode", 384, 8, 8, 64, 180_224, 0, 152)
+    assert ctas == 304 and 384 * 8 * (180_224 // 128 + 1) > 1 << 22

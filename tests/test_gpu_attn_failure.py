@@ -50,3 +50,22 @@ def test_a_wait_that_runs_out_with_heads_of_64(n):
     for r, want, _, bound, _ in rows:
         assert ((o[r, :2 * 64].double().reshape(2, 64) - want).abs() <= bound).all()
     run_prefill(p, [0], [n], dev).check(p.prefill_rows([0], [n], [0, n]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_wait_that_runs_out_in_a_call_with_a_join(d):
+    """The join runs all the same: the status says that the outputs mean nothing, and nothing else is touched."""
+    dev = device()
+    p = Problem(22, 4, 2, d, 16, "bf16", [3000], 20)
+    out = Outputs(p, dev)
+    shape = p.shape(1)
+    size = hs.hs_attn_prefill_workspace_bytes(shape, [2980], [20])
+    assert size > 0
+    ws = workspace(size, dev)
+    hs.hs_test_attn_stalled(shape, p.q.to(dev), p.cache.to(dev), p.table.to(dev), out.o, out.lse, [2980], [20],
+                            [0, 20], ws, size, out.err)
+    torch.cuda.synchronize()
+    assert out.err.item() == hs.HS_DEVERR_TIMEOUT
+    assert (ws[size:] == 0xFF).all()
+    assert torch.isnan(out.o[20:]).all() and torch.isnan(out.lse[20:]).all()
+    run_prefill(p, [2980], [20], dev).check(p.prefill_rows([2980], [20], [0, 20]))
