@@ -109,8 +109,8 @@ hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, i
  * The tensor core adds to a float32 sum and drops what lies below 2^-26 of it: where one CTA walks n keys
  * (`unsplit`, or a row of a long prefill) and a column's values are of one sign, an output is low by up to
  * n 2^-27 of it (8e-4 at 131,072 keys; measured).
- * Scores may lie anywhere in float32's range; each is exact to some 2^-24 of the sum of its products' magnitudes, so
- * that far from zero (10^6 and more) only ones that lie well apart keep their order.
+ * Scores may lie anywhere in float32's range; each is good to some 2^-24 of the sum of its products' magnitudes, so
+ * that of scores of 10^7 and more only ones that lie well apart are told apart.
  * With shp->unsplit a row's result depends on nothing but its query and its keys, so a tail resumed
  * at any position equals the recomputation bit for bit; without it, the keys of one row may be
  * shared out over CTAs by the sizes of the call, and equal calls give equal bits.

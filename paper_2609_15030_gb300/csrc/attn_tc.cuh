@@ -14,8 +14,8 @@
 // operands); l sums them before that rounding.
 // 2^(s_j - m) is one fused multiplication and addition of q . k_j, m a rounded product.  What that rounding
 // takes off is the same factor of all weights of the row and cancels in o; but with m beyond 2^31 it is
-// 2^+-128 and more (NaN, or weights of nothing but 0), and beyond 2^24 fp16 weights overflow.  So with m
-// beyond 2^20 all products are rounded before m is taken off, and the largest gets a weight of 2^0 (fp16: 2^8).
+// 2^+-128 and more (NaN, or weights of nothing but 0), and beyond 2^24 fp16 weights overflow.  So from 2^28 (fp16:
+// 2^23) on all products are rounded before m is taken off, and the largest gets a weight of 2^0 (2^8).
 //
 // Schedule.  The units of all items in order are shared out evenly over the CTAs, each a
 // contiguous run, so that one long request or many ragged ones fill the SMs alike.  An item whose
@@ -61,7 +61,6 @@ namespace attn {
 using namespace ptx;
 
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kFar = 1048576.f;         // scores that are rounded before m is taken off (units of log2)
 constexpr uint64_t kTimeoutNs = 1000000000ull;       // for copies and MMAs in flight to end
 
 // ---- shapes of a launch --------------------------------------------------------------------
@@ -143,6 +142,8 @@ template <>
 struct Elem<__nv_bfloat16> {
     static constexpr uint32_t kExp = 0x7F807F80u, kOne = 0x00800080u;
     static constexpr float kMost = 8.f, kBelow = 0.f;       // log2 of the largest weight, of a new m's
+    static constexpr float kFar = 268435456.f;              // 2^28: from here on scores are rounded before m
+                                                            // is taken off (a half step of 16 adds to kMost)
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         uint32_t r;
@@ -162,6 +163,7 @@ template <>
 struct Elem<__half> {
     static constexpr uint32_t kExp = 0x7C007C00u, kOne = 0x04000400u;
     static constexpr float kMost = 15.f, kBelow = 8.f;
+    static constexpr float kFar = 8388608.f;                // 2^23: two half steps of 1/4 below, and 2^15.5 fits
     static __device__ __forceinline__ uint32_t pack(float lo, float hi)
     {
         uint32_t r;
@@ -755,7 +757,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
             float m = -INFINITY, l = 0.f;       // m in units of log2, of scaled scores
             float limit = -INFINITY;            // m + kMost
             float shift = 0.f;                  // -m, but 0 without a key and far from zero
-            bool far = false;                   // m lies beyond kFar
+            bool far = false;                   // |m| lies beyond kFar
             int valid = keys - info.kt0 * kKeys;   // keys of the row from this tile on
             for (int j = 0; j < tiles; ++j, valid -= kKeys) {
                 go = wait(bar_s, ph_s);
@@ -816,7 +818,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                         to = top - Elem<T>::kBelow;
                         limit = to + Elem<T>::kMost;
                         shift = -to;
-                        far = ok && fabsf(to) > kFar;
+                        far = ok && fabsf(to) > Elem<T>::kFar;
                     }
                     const bool any_far = __any_sync(0xffffffffu, far);
                     if (__builtin_expect(any_far, 0) && far) {  // where 8 or 15 is half a step of float32 or less

@@ -60,8 +60,9 @@ class Far(Problem):
         return (o.reshape(h, d), lse.reshape(h), bound.reshape(h, d), (lse.abs() * 2.0 ** -21 + 2.0 ** -20).reshape(h))
 
 
-SIZES = [("fp16", 4096.0), ("fp16", 30000.0), ("fp16", 60000.0), ("bf16", 4096.0), ("bf16", 3e5), ("bf16", 5e7),
-         ("bf16", 1e15)]
+SIZES = [("fp16", 4096.0), ("fp16", 5000.0), ("fp16", 8000.0), ("fp16", 12000.0), ("fp16", 30000.0),
+         ("fp16", 60000.0), ("bf16", 4096.0), ("bf16", 3e4), ("bf16", 5e4), ("bf16", 1e5), ("bf16", 3e5),
+         ("bf16", 5e7), ("bf16", 1e15)]
 
 
 @pytest.mark.parametrize("d", [64, 128])
