@@ -19,6 +19,8 @@ extern "C" {
 
 /* one more code that a kernel may store into d_err */
 #define HS_DEVERR_LENGTH 5        /* a length read from a device array is < 0 or above the call's bound */
+/* HS_DEVERR_TIMEOUT from an attention call: none of its outputs means anything.  Its waits are bounded by 1 s and
+ * 20 us for each tile of 128 keys that one CTA may have to walk. */
 
 /* Element type of the attention calls' q, o and cache. */
 typedef enum hs_dtype {
@@ -67,8 +69,8 @@ typedef struct hs_attn_shape {
  *   slots      device int64 [n_rows]
  *   cache      device, the layer's cache
  * k, v and the cache must be 16-byte aligned and must not overlap.
- * Errors: HS_ERR_INVALID_ARG, HS_ERR_MISALIGNED, HS_ERR_UNSUPPORTED (head_dim, page_size),
- * HS_ERR_CUDA.
+ * Errors: HS_ERR_INVALID_ARG, HS_ERR_MISALIGNED, HS_ERR_UNSUPPORTED (head_dim, page_size, n_kv_heads > 1024,
+ * 2^31 8-token groups in the cache), HS_ERR_CUDA.
  */
 hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, int64_t kv_stride,
                        const int64_t *slots, int64_t n_rows, void *cache, int32_t *d_err,
@@ -120,8 +122,8 @@ hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, i
  * other requests keep their values.
  * All pointers 16-byte aligned; o and lse must not overlap anything else.
  * Errors: HS_ERR_INVALID_ARG, HS_ERR_MISALIGNED, HS_ERR_UNSUPPORTED (head_dim, page_size,
- * n_heads / n_kv_heads > 128, batch > HS_MAX_BATCH, a stride, position or row times heads near 2^31 or
- * above, 2^31 tiles of 128 keys in all), HS_ERR_CUDA.
+ * n_heads / n_kv_heads > 128, n_kv_heads > 1024, batch > HS_MAX_BATCH, a stride, position, row times heads or
+ * number of 8-token groups in the cache near 2^31 or above, 2^31 tiles of 128 keys in all), HS_ERR_CUDA.
  */
 hs_status hs_attn_prefill(const hs_attn_shape *shp, const void *q, const void *cache,
                           const int32_t *block_table, void *o, float *lse, const int64_t *pos0,

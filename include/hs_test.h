@@ -34,7 +34,9 @@ hs_status hs_test_prefill_stalled(const hs_linattn_shape *shp, const uint16_t *q
 /*
  * hs_test_attn_stalled takes the arguments of hs_attn_prefill.  In every CTA the warp that issues the
  * first rows' products first waits on an mbarrier that nothing completes; when that wait runs out
- * (1 s) the CTA leaves through its abort path, as above, without writing an output of those rows.
+ * (1 s, and 20 us for each tile of the call's longest run) the CTA leaves through its abort path, as above,
+ * without writing an output of those rows.  Where the call joins partial results, the join runs all the same: with
+ * HS_DEVERR_TIMEOUT in d_err the outputs of the rows that it joins mean nothing.
  */
 hs_status hs_test_attn_stalled(const hs_attn_shape *shp, const void *q, const void *cache,
                                const int32_t *block_table, void *o, float *lse, const int64_t *pos0,

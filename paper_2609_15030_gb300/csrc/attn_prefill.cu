@@ -6,8 +6,10 @@ namespace attn {
 namespace {
 
 // Block (x, y, z) takes 32 rows and 8 E columns of the x-th item that is split between CTAs, a lane a row
-// and a warp E columns: 4 where few items are split (of many parts each), all of them in one block
-// where many are (with 4 the 4,832 blocks of nine packed tails' 151 items took 11 us).
+// and a warp E columns: 4 where few items are split (of many parts each), all of them in one block where more
+// than 64 are.  Tails of 200 to 260 tokens behind 3,000 and more keys, 16 heads over 4 of 128, the whole call: 16
+// split items 15.3 us (16.9 in one block each), 64 32.2 (30.2), 80 38.1 (35.9), 137 65.7 (60.9); heads of 64 with
+// 64 items 23.8 (23.1), of 128 with one tile of rows to an item 31.0 (32.0).
 template <typename T, int D, int NG, int E>
 __global__ void __launch_bounds__(kMergeWarps * 32)
 attn_merge_prefill_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ PrefillPlan plan)

@@ -38,10 +38,10 @@
 // and scheduler take 270; the rest are maxima, sums, conversions and the passage through TMEM), and
 // some 250 ns go into the hand-overs, so a pair of tiles takes 1.45 us where the tensor core alone
 // would take 1.07; with a shorter softmax (two threads to a row) registers spilled and it took 2.3.
-// Two 16k-token prompts of 32 heads: 2.87 ms, 1,530 TFLOP/s, at the power limit (a cuBLAS product
-// sustains 1,692 there); one of 8k tokens 338 us, 1,625.  Heads of 64 have half the products to the same
-// softmax: 1.2 us a pair of tiles, 1,070 TFLOP/s.  A decode step is bound by HBM where its contexts are long
-// (four requests at 98k to 131k keys: 269 us, 7.0 TB/s), a short call by latency: 3.5 us until the first
+// Two 16k-token prompts of 32 heads: 2.7 to 3.06 ms, 1,640 to 1,440 TFLOP/s, at the power limit (a cuBLAS
+// product sustains 1,692 there); two of 8k tokens 676 us, 1,626.  Heads of 64 have half the products to the
+// same softmax: 1.2 us a pair of tiles, 1,040 TFLOP/s.  A decode step is bound by HBM where its contexts are long
+// (four requests at 98k to 131k keys: 269 to 275 us, 7.0 to 6.85 TB/s), a short call by latency: 3.5 us until the first
 // scores, 0.7 us of softmax, 1.3 us for sums of 256 rows that go to the workspace, 3 to 4 us for the join.
 // A segment costs what two tiles cost beside its own: its description, queries, and outputs, code that runs
 // once and waits for its instructions.
@@ -651,7 +651,7 @@ attn_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Plan p
                     // Searched are whole atoms of 8 rows, kRows of them at a time, so that a lane's places in
                     // an atom are constants; a product with zero for two values says whether one is not finite.
                     // (Testing exponents took over 10 us a tile of 128 rows: 8k tokens of 32 heads of their own
-                    // 574 us instead of 398.)
+                    // 574 us where this took 398.)
                     for (int a0 = lo >> 3; lo < hi && a0 < (hi + 7) >> 3; a0 += kRows) {
                         uint4 y[8];
     #pragma unroll
