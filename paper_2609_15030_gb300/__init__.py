@@ -1,7 +1,8 @@
 """Python binding of libhs (checkpoint-aligned restore-and-resume, sm_103a).
 
 Argument marshalling only: every function forwards to the C entry point of
-the same name in ``libhs.so`` (declared in ``include/hs.h`` and ``include/hs_attn.h``); all GPU work
+the same name in ``libhs.so`` (declared in ``include/hs.h``, ``include/hs_attn.h`` and ``include/hs_kv8.h``); all GPU
+work
 runs in the library's kernels.  Tensors are accepted wherever the C call
 takes a pointer (their ``data_ptr()`` is passed); plain ints are passed as
 addresses.  A non-OK status raises ``HsError``.
@@ -47,6 +48,16 @@ HS_LINATTN_SINGLE_TOKEN = 3
 HS_BF16 = 0
 HS_FP16 = 1
 
+HS_KV8_GROUP = 16
+HS_ROPE_HALF = 0
+HS_ROPE_INTERLEAVED = 1
+HS_ROPE_PLAIN = 0
+HS_ROPE_LINEAR = 1
+HS_ROPE_BASE = 2
+HS_ROPE_TURNS = 3
+HS_ROPE_INDEX = 4
+HS_ROPE_MAX_PAIRS = 64
+
 EXPORTED = ("hs_status_string", "hs_version", "hs_align_prefix", "hs_restore_kv_pages",
             "hs_save_kv_pages", "hs_restore_kv_page_slices", "hs_save_kv_page_slices",
             "hs_restore_state", "hs_checkpoint_states", "hs_linattn_prefill_from_state",
@@ -55,7 +66,9 @@ EXPORTED = ("hs_status_string", "hs_version", "hs_align_prefix", "hs_restore_kv_
             "hs_linattn_prefill_scan_noalloc", "hs_kv_append", "hs_attn_prefill",
             "hs_attn_prefill_workspace_bytes", "hs_attn_decode", "hs_attn_decode_workspace_bytes",
             "hs_attn_decode_shared", "hs_attn_decode_shared_workspace_bytes",
-            "hs_test_attn_stalled")
+            "hs_test_attn_stalled", "hs_rope_plan", "hs_rope_apply", "hs_kv8_block_bytes",
+            "hs_kv8_append", "hs_kv8_append_rope", "hs_kv8_decode", "hs_kv8_decode_workspace_bytes",
+            "hs_kv8_read")
 
 
 class HsError(RuntimeError):
@@ -75,6 +88,11 @@ class hs_attn_shape(C.Structure):
                 ("head_dim", C.c_int32), ("page_size", C.c_int32), ("dtype", C.c_int32),
                 ("num_blocks", C.c_int64), ("max_pages", C.c_int64), ("q_stride", C.c_int64),
                 ("o_stride", C.c_int64), ("scale", C.c_float), ("unsplit", C.c_int32)]
+
+
+class hs_rope(C.Structure):
+    _fields_ = [("dims", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_double),
+                ("theta", C.c_double * HS_ROPE_MAX_PAIRS)]
 
 
 _lock = threading.Lock()
@@ -124,6 +142,15 @@ def load() -> C.CDLL:
             L.hs_attn_decode_shared.argtypes = [ash, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, i64,
                                                 vp, vp]
             L.hs_attn_decode_shared_workspace_bytes.argtypes = [ash, i64, i64, vp]
+            rp, f64 = C.POINTER(hs_rope), C.c_double
+            L.hs_rope_plan.argtypes = [i32, i32, f64, i32, f64, i64, f64, f64, f64, rp]
+            L.hs_rope_apply.argtypes = [ash, rp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+            L.hs_kv8_block_bytes.argtypes = [ash, vp]
+            L.hs_kv8_append.argtypes = L.hs_kv_append.argtypes
+            L.hs_kv8_append_rope.argtypes = [ash, rp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
+            L.hs_kv8_decode.argtypes = L.hs_attn_decode.argtypes
+            L.hs_kv8_decode_workspace_bytes.argtypes = [ash, i64, vp]
+            L.hs_kv8_read.argtypes = [ash, vp, vp, vp, i64, vp, i64, vp, vp, vp]
             for name in EXPORTED[2:]:
                 getattr(L, name).restype = C.c_int
             _lib = L
@@ -481,3 +508,80 @@ def hs_attn_decode_shared(shape: hs_attn_shape, q, cache, prefix_table, prefix_l
         _ptr(block_table), _ptr(kv_len), int(max_kv_len), _ptr(o), _ptr(lse), _ptr(workspace),
         int(workspace_bytes), _ptr(d_err), _stream(stream))
     _check(rc, "hs_attn_decode_shared")
+
+
+def hs_rope_plan(dims: int, layout: int, base: float, scaling: int = HS_ROPE_PLAIN, factor: float = 1.0,
+                 context: int = 1, low: float = 1.0, high: float = 32.0,
+                 amplitude: float = 1.0) -> hs_rope:
+    """The angles of rotary positions (host only); context, low and high: HS_ROPE_TURNS and
+    HS_ROPE_INDEX alone."""
+    out = hs_rope()
+    rc = (_lib or load()).hs_rope_plan(int(dims), int(layout), float(base), int(scaling), float(factor),
+                                       int(context), float(low), float(high), float(amplitude),
+                                       C.byref(out))
+    _check(rc, "hs_rope_plan")
+    return out
+
+
+def hs_rope_apply(shape: hs_attn_shape, rope: hs_rope, q, k, in_stride: int, pos, n_rows: int, q_out,
+                  q_out_stride: int, k_out, k_out_stride: int, stream=None):
+    """pos: device int64 [n_rows].  q and q_out, or k and k_out, may be None; in place is fine."""
+    rc = (_lib or load()).hs_rope_apply(
+        C.byref(shape), C.byref(rope), _ptr(q), _ptr(k), int(in_stride), _ptr(pos), int(n_rows),
+        _ptr(q_out), int(q_out_stride), _ptr(k_out), int(k_out_stride), _stream(stream))
+    _check(rc, "hs_rope_apply")
+
+
+def hs_kv8_block_bytes(shape: hs_attn_shape) -> int:
+    """Bytes of one block (page) of the 8-bit cache, its scales included."""
+    out = C.c_int64()
+    rc = (_lib or load()).hs_kv8_block_bytes(C.byref(shape), C.addressof(out))
+    _check(rc, "hs_kv8_block_bytes")
+    return out.value
+
+
+def hs_kv8_append(shape: hs_attn_shape, k, v, kv_stride: int, slots, n_rows: int, cache, d_err=None,
+                  stream=None):
+    """slots as in hs_kv_append; the rows of a group of 16 tokens stand one behind the other."""
+    rc = (_lib or load()).hs_kv8_append(
+        C.byref(shape), _ptr(k), _ptr(v), int(kv_stride), _ptr(slots), int(n_rows), _ptr(cache),
+        _ptr(d_err), _stream(stream))
+    _check(rc, "hs_kv8_append")
+
+
+def hs_kv8_append_rope(shape: hs_attn_shape, rope: hs_rope, q, k, v, in_stride: int, pos, slots,
+                       n_rows: int, q_out, q_out_stride: int, cache, d_err=None, stream=None):
+    """hs_rope_apply of q and hs_kv8_append of the turned k, and of v; q and q_out may be None."""
+    rc = (_lib or load()).hs_kv8_append_rope(
+        C.byref(shape), C.byref(rope), _ptr(q), _ptr(k), _ptr(v), int(in_stride), _ptr(pos),
+        _ptr(slots), int(n_rows), _ptr(q_out), int(q_out_stride), _ptr(cache), _ptr(d_err),
+        _stream(stream))
+    _check(rc, "hs_kv8_append_rope")
+
+
+def hs_kv8_decode_workspace_bytes(shape: hs_attn_shape, max_kv_len: int) -> int:
+    out = C.c_int64()
+    rc = (_lib or load()).hs_kv8_decode_workspace_bytes(C.byref(shape), int(max_kv_len),
+                                                        C.addressof(out))
+    _check(rc, "hs_kv8_decode_workspace_bytes")
+    return out.value
+
+
+def hs_kv8_decode(shape: hs_attn_shape, q, cache, block_table, kv_len, max_kv_len: int, o, lse=None,
+                  workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """One decode step over the 8-bit cache; kv_len: device int32 [batch], the token of the step
+    counted in."""
+    rc = (_lib or load()).hs_kv8_decode(
+        C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(kv_len), int(max_kv_len),
+        _ptr(o), _ptr(lse), _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
+    _check(rc, "hs_kv8_decode")
+
+
+def hs_kv8_read(shape: hs_attn_shape, cache, block_table, kv_len, max_kv_len: int, out, out_blocks: int,
+                out_table, d_err=None, stream=None):
+    """The first kv_len[b] tokens of each request read back into 16-bit pages; kv_len: device int32
+    [batch]."""
+    rc = (_lib or load()).hs_kv8_read(
+        C.byref(shape), _ptr(cache), _ptr(block_table), _ptr(kv_len), int(max_kv_len), _ptr(out),
+        int(out_blocks), _ptr(out_table), _ptr(d_err), _stream(stream))
+    _check(rc, "hs_kv8_read")

@@ -19,7 +19,11 @@ inline hs_status cuda_status(cudaError_t e)
     return e == cudaSuccess ? HS_OK : HS_ERR_CUDA;
 }
 
-int page_shift(int32_t page_size)
+}  // namespace
+
+namespace hs {
+
+int attn_page_shift(int32_t page_size)
 {
     for (int s = 4; s <= 8; ++s)
         if (page_size == 1 << s)
@@ -27,14 +31,13 @@ int page_shift(int32_t page_size)
     return -1;
 }
 
-// what every call asks of the cache's part of the shape
-hs_status check_cache(const hs_attn_shape &s)
+hs_status check_attn_cache(const hs_attn_shape &s)
 {
     if (s.n_kv_heads < 1 || s.num_blocks < 0 || s.page_size < 1)
         return HS_ERR_INVALID_ARG;
     if (s.dtype != HS_BF16 && s.dtype != HS_FP16)
         return HS_ERR_INVALID_ARG;
-    if ((s.head_dim != 64 && s.head_dim != 128) || page_shift(s.page_size) < 0)
+    if ((s.head_dim != 64 && s.head_dim != 128) || attn_page_shift(s.page_size) < 0)
         return HS_ERR_UNSUPPORTED;
     // the cache's rows of 64 elements are counted in 32 bits
     if (s.n_kv_heads > 1024 || s.num_blocks > INT32_MAX / (2 * (s.page_size / 8)))
@@ -42,12 +45,12 @@ hs_status check_cache(const hs_attn_shape &s)
     return HS_OK;
 }
 
-hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
+hs_status check_attn_shape(const hs_attn_shape *shp, AttnParams &p)
 {
     if (shp == nullptr)
         return HS_ERR_INVALID_ARG;
     const hs_attn_shape s = *shp;
-    const hs_status st = check_cache(s);
+    const hs_status st = check_attn_cache(s);
     if (st == HS_ERR_INVALID_ARG)
         return st;
     if (s.batch < 0 || s.n_heads < 1 || s.n_heads % s.n_kv_heads != 0 || s.max_pages < 0 ||
@@ -75,13 +78,13 @@ hs_status check_shape(const hs_attn_shape *shp, hs::AttnParams &p)
     p.group = s.n_heads / s.n_kv_heads;
     p.by_group.set(p.group);
     p.by_kv.set(p.n_kv);
-    p.page_shift = page_shift(s.page_size);
+    p.page_shift = attn_page_shift(s.page_size);
     p.unsplit = s.unsplit;
     p.scale_log2 = s.scale * 1.4426950408889634f;
     return HS_OK;
 }
 
-hs_status room(int64_t need, void *workspace, int64_t workspace_bytes, hs::AttnParams &p)
+hs_status attn_workspace(int64_t need, void *workspace, int64_t workspace_bytes, AttnParams &p)
 {
     if (need < 0)
         return HS_ERR_UNSUPPORTED;
@@ -90,6 +93,38 @@ hs_status room(int64_t need, void *workspace, int64_t workspace_bytes, hs::AttnP
     p.part = static_cast<float *>(workspace);
     return HS_OK;
 }
+
+hs_status check_attn_pointers(const AttnParams &p, const void *workspace, int64_t workspace_bytes)
+{
+    if (p.q == nullptr || p.cache == nullptr || p.table == nullptr || p.o == nullptr ||
+        workspace_bytes < 0 || p.num_blocks < 1)
+        return HS_ERR_INVALID_ARG;
+    if (misaligned16(p.q) || misaligned16(p.cache) || misaligned16(p.o) || misaligned16(workspace) ||
+        (reinterpret_cast<uintptr_t>(p.table) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0)
+        return HS_ERR_MISALIGNED;
+    return HS_OK;
+}
+
+hs_status check_attn_decode(const hs_attn_shape *shp, int64_t prefix_len, int64_t max_kv_len,
+                            AttnParams &p)
+{
+    const hs_status st = check_attn_shape(shp, p);
+    if (st != HS_OK)
+        return st;
+    const int64_t room = shp->max_pages > INT32_MAX ? INT64_MAX : shp->max_pages * shp->page_size;
+    if (prefix_len < 0 || max_kv_len < 0 || max_kv_len > room)
+        return HS_ERR_INVALID_ARG;
+    if (prefix_len > INT32_MAX - 8192 || max_kv_len > INT32_MAX - 8192 - prefix_len)
+        return HS_ERR_UNSUPPORTED;
+    p.max_kv = (int32_t)max_kv_len;
+    p.prefix_len = (int32_t)prefix_len;
+    return HS_OK;
+}
+
+}  // namespace hs
+
+namespace {
 
 // the requests' lengths into the plan; *any: whether there is a token
 hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32_t *n_tokens,
@@ -127,41 +162,13 @@ hs_status check_lengths(const hs_attn_shape &s, const int64_t *pos0, const int32
     return HS_OK;
 }
 
-hs_status check_pointers(const hs::AttnParams &p, const void *workspace, int64_t workspace_bytes)
-{
-    if (p.q == nullptr || p.cache == nullptr || p.table == nullptr || p.o == nullptr ||
-        workspace_bytes < 0 || p.num_blocks < 1)
-        return HS_ERR_INVALID_ARG;
-    if (misaligned16(p.q) || misaligned16(p.cache) || misaligned16(p.o) || misaligned16(workspace) ||
-        (reinterpret_cast<uintptr_t>(p.table) & 3u) != 0 ||
-        (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0)
-        return HS_ERR_MISALIGNED;
-    return HS_OK;
-}
-
-hs_status check_decode(const hs_attn_shape *shp, int64_t prefix_len, int64_t max_kv_len,
-                       hs::AttnParams &p)
-{
-    const hs_status st = check_shape(shp, p);
-    if (st != HS_OK)
-        return st;
-    const int64_t room = shp->max_pages > INT32_MAX ? INT64_MAX : shp->max_pages * shp->page_size;
-    if (prefix_len < 0 || max_kv_len < 0 || max_kv_len > room)
-        return HS_ERR_INVALID_ARG;
-    if (prefix_len > INT32_MAX - 8192 || max_kv_len > INT32_MAX - 8192 - prefix_len)
-        return HS_ERR_UNSUPPORTED;
-    p.max_kv = (int32_t)max_kv_len;
-    p.prefix_len = (int32_t)prefix_len;
-    return HS_OK;
-}
-
 hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache,
                  const int32_t *prefix_table, int64_t prefix_len, const int32_t *block_table,
                  const int32_t *kv_len, int64_t max_kv_len, void *o, float *lse, void *workspace,
                  int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream)
 {
     hs::AttnParams p;
-    hs_status st = check_decode(shp, prefix_len, max_kv_len, p);
+    hs_status st = hs::check_attn_decode(shp, prefix_len, max_kv_len, p);
     if (st != HS_OK)
         return st;
     if (p.batch == 0)
@@ -178,13 +185,13 @@ hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache,
     p.o = o;
     p.lse = lse;
     p.d_err = d_err;
-    st = check_pointers(p, workspace, workspace_bytes);
+    st = hs::check_attn_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
     int sms = 0;
     st = hs::device_sm_count(&sms);
     if (st == HS_OK)
-        st = room(hs::plan_attn_decode(p, shp->head_dim, sms), workspace, workspace_bytes, p);
+        st = hs::attn_workspace(hs::plan_attn_decode(p, shp->head_dim, sms), workspace, workspace_bytes, p);
     if (st != HS_OK)
         return st;
     return cuda_status(hs::launch_attn_decode(p, shp->head_dim, shp->dtype, stream));
@@ -200,7 +207,7 @@ hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, i
 {
     if (shp == nullptr || n_rows < 0 || kv_stride < 0)
         return HS_ERR_INVALID_ARG;
-    hs_status st = check_cache(*shp);
+    hs_status st = hs::check_attn_cache(*shp);
     if (st != HS_OK)
         return st;
     const int64_t inner = (int64_t)shp->n_kv_heads * shp->head_dim;
@@ -220,7 +227,7 @@ hs_status hs_kv_append(const hs_attn_shape *shp, const void *k, const void *v, i
     if (st != HS_OK)
         return st;
     return cuda_status(hs::launch_kv_append(k, v, kv_stride != 0 ? kv_stride : inner, slots, n_rows,
-                                            cache, (int32_t)(inner / 8), page_shift(shp->page_size),
+                                            cache, (int32_t)(inner / 8), hs::attn_page_shift(shp->page_size),
                                             shp->num_blocks, d_err, sms, stream));
 }
 
@@ -232,7 +239,7 @@ static hs_status prefill(const hs_attn_shape *shp, const void *q, const void *ca
 {
     hs::AttnParams p;
     hs::PrefillPlan plan;
-    hs_status st = check_shape(shp, p);
+    hs_status st = hs::check_attn_shape(shp, p);
     bool any = false;
     if (st == HS_OK)
         st = check_lengths(*shp, pos0, n_tokens, cu_rows, true, p, plan, &any);
@@ -245,13 +252,13 @@ static hs_status prefill(const hs_attn_shape *shp, const void *q, const void *ca
     p.lse = lse;
     p.d_err = d_err;
     p.stall_for_test = stall_for_test;
-    st = check_pointers(p, workspace, workspace_bytes);
+    st = hs::check_attn_pointers(p, workspace, workspace_bytes);
     if (st != HS_OK)
         return st;
     int sms = 0;
     st = hs::device_sm_count(&sms);
     if (st == HS_OK)
-        st = room(hs::plan_attn_prefill(p, plan, shp->head_dim, sms), workspace, workspace_bytes, p);
+        st = hs::attn_workspace(hs::plan_attn_prefill(p, plan, shp->head_dim, sms), workspace, workspace_bytes, p);
     if (st != HS_OK)
         return st;
     return cuda_status(hs::launch_attn_prefill(p, plan, shp->head_dim, shp->dtype, stream));
@@ -282,7 +289,7 @@ hs_status hs_attn_prefill_workspace_bytes(const hs_attn_shape *shp, const int64_
         return HS_ERR_INVALID_ARG;
     hs::AttnParams p;
     hs::PrefillPlan plan;
-    hs_status st = check_shape(shp, p);
+    hs_status st = hs::check_attn_shape(shp, p);
     bool any = false;
     if (st == HS_OK)
         st = check_lengths(*shp, pos0, n_tokens, nullptr, false, p, plan, &any);
@@ -333,7 +340,7 @@ hs_status hs_attn_decode_shared_workspace_bytes(const hs_attn_shape *shp, int64_
     if (bytes_out == nullptr)
         return HS_ERR_INVALID_ARG;
     hs::AttnParams p;
-    hs_status st = check_decode(shp, prefix_len, max_kv_len, p);
+    hs_status st = hs::check_attn_decode(shp, prefix_len, max_kv_len, p);
     if (st != HS_OK)
         return st;
     *bytes_out = 0;

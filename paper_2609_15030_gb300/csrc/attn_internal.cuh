@@ -97,6 +97,15 @@ struct DecodePlan {
     static constexpr bool kDecode = true;
 };
 
+// Host-side checks that the calls share (attn_api.cu): log2 of a page size (-1: not offered); the cache's part of a
+// shape; all of it, which fills in the parameters; a decode step's bounds; the pointers; the workspace, which becomes p.part.
+int attn_page_shift(int32_t page_size);
+hs_status check_attn_cache(const hs_attn_shape &s);
+hs_status check_attn_shape(const hs_attn_shape *shp, AttnParams &p);
+hs_status check_attn_decode(const hs_attn_shape *shp, int64_t prefix_len, int64_t max_kv_len, AttnParams &p);
+hs_status check_attn_pointers(const AttnParams &p, const void *workspace, int64_t workspace_bytes);
+hs_status attn_workspace(int64_t need, void *workspace, int64_t workspace_bytes, AttnParams &p);
+
 // Fill in the schedule and say how many bytes of workspace it takes; -1: more units than 31 bits count.
 int64_t plan_attn_prefill(AttnParams &p, PrefillPlan &plan, int d, int sm_count);
 int64_t plan_attn_decode(AttnParams &p, int d, int sm_count);
