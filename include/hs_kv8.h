@@ -174,8 +174,9 @@ hs_status hs_kv8_append_rope(const hs_attn_shape *shp, const hs_rope *rope, cons
  * NaN, that request's outputs of the KV head's heads need not be finite; the others keep their values.
  *   block_table  an id outside [0,num_blocks) sets HS_DEVERR_BLOCK_OOB; its page is not read, and the outputs
  *                of that request mean nothing
+ * HS_DEVERR_TIMEOUT from this call: none of its outputs means anything.  Its waits are bounded by 1 s.
  * Errors: as hs_attn_decode (HS_ERR_UNSUPPORTED also for more than 2^31 groups of 16 tokens in all, with every
- * request at max_kv_len).
+ * request at max_kv_len, and for a cache of 2^38 bytes or more).
  */
 hs_status hs_kv8_decode(const hs_attn_shape *shp, const void *q, const void *cache,
                         const int32_t *block_table, const int32_t *kv_len, int64_t max_kv_len, void *o,

@@ -20,6 +20,7 @@
 
 #include "hs.h"
 #include "hs_attn.h"
+#include "hs_kv8.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -42,6 +43,16 @@ hs_status hs_test_attn_stalled(const hs_attn_shape *shp, const void *q, const vo
                                const int32_t *block_table, void *o, float *lse, const int64_t *pos0,
                                const int32_t *n_tokens, const int64_t *cu_rows, void *workspace,
                                int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream);
+
+/*
+ * hs_test_kv8_stalled takes the arguments of hs_kv8_decode.  Every warp that has tiles first waits (1 s) on an mbarrier that
+ * nothing completes; it then waits for its own copies, and leaves without a result.  A join runs all the
+ * same: with HS_DEVERR_TIMEOUT in d_err none of the outputs means anything.
+ */
+hs_status hs_test_kv8_stalled(const hs_attn_shape *shp, const void *q, const void *cache,
+                              const int32_t *block_table, const int32_t *kv_len, int64_t max_kv_len,
+                              void *o, float *lse, void *workspace, int64_t workspace_bytes,
+                              int32_t *d_err, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -68,7 +68,7 @@ EXPORTED = ("hs_status_string", "hs_version", "hs_align_prefix", "hs_restore_kv_
             "hs_attn_decode_shared", "hs_attn_decode_shared_workspace_bytes",
             "hs_test_attn_stalled", "hs_rope_plan", "hs_rope_apply", "hs_kv8_block_bytes",
             "hs_kv8_append", "hs_kv8_append_rope", "hs_kv8_decode", "hs_kv8_decode_workspace_bytes",
-            "hs_kv8_read")
+            "hs_kv8_read", "hs_test_kv8_stalled")
 
 
 class HsError(RuntimeError):
@@ -149,6 +149,7 @@ def load() -> C.CDLL:
             L.hs_kv8_append.argtypes = L.hs_kv_append.argtypes
             L.hs_kv8_append_rope.argtypes = [ash, rp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, vp]
             L.hs_kv8_decode.argtypes = L.hs_attn_decode.argtypes
+            L.hs_test_kv8_stalled.argtypes = L.hs_attn_decode.argtypes
             L.hs_kv8_decode_workspace_bytes.argtypes = [ash, i64, vp]
             L.hs_kv8_read.argtypes = [ash, vp, vp, vp, i64, vp, i64, vp, vp, vp]
             for name in EXPORTED[2:]:
@@ -567,14 +568,28 @@ def hs_kv8_decode_workspace_bytes(shape: hs_attn_shape, max_kv_len: int) -> int:
     return out.value
 
 
+def _kv8_decode_call(name, shape, q, cache, block_table, kv_len, max_kv_len, o, lse, workspace,
+                     workspace_bytes, d_err, stream):
+    rc = getattr(_lib or load(), name)(
+        C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(kv_len), int(max_kv_len),
+        _ptr(o), _ptr(lse), _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
+    _check(rc, name)
+
+
 def hs_kv8_decode(shape: hs_attn_shape, q, cache, block_table, kv_len, max_kv_len: int, o, lse=None,
                   workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
     """One decode step over the 8-bit cache; kv_len: device int32 [batch], the token of the step
     counted in."""
-    rc = (_lib or load()).hs_kv8_decode(
-        C.byref(shape), _ptr(q), _ptr(cache), _ptr(block_table), _ptr(kv_len), int(max_kv_len),
-        _ptr(o), _ptr(lse), _ptr(workspace), int(workspace_bytes), _ptr(d_err), _stream(stream))
-    _check(rc, "hs_kv8_decode")
+    _kv8_decode_call("hs_kv8_decode", shape, q, cache, block_table, kv_len, max_kv_len, o, lse, workspace,
+                     workspace_bytes, d_err, stream)
+
+
+def hs_test_kv8_stalled(shape: hs_attn_shape, q, cache, block_table, kv_len, max_kv_len: int, o, lse=None,
+                        workspace=None, workspace_bytes: int = 0, d_err=None, stream=None):
+    """Failure-detection hook (include/hs_test.h): hs_kv8_decode with one wait per warp that nothing
+    completes; it reports HS_DEVERR_TIMEOUT."""
+    _kv8_decode_call("hs_test_kv8_stalled", shape, q, cache, block_table, kv_len, max_kv_len, o, lse,
+                     workspace, workspace_bytes, d_err, stream)
 
 
 def hs_kv8_read(shape: hs_attn_shape, cache, block_table, kv_len, max_kv_len: int, out, out_blocks: int,

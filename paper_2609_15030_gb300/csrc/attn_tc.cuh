@@ -48,12 +48,12 @@
 #pragma once
 
 #include <cuda.h>
-#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "attn_ptx.cuh"
 #include "attn_walk.cuh"
+#include "tensor_map.cuh"
 
 namespace hs {
 namespace attn {
@@ -1179,24 +1179,6 @@ __device__ __forceinline__ void finish_row(const AttnParams &p, Joined<D> x, int
 }
 
 // ---- launch --------------------------------------------------------------------------------
-
-inline PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
-{
-    // resolved once per process from the driver; a pure function pointer
-    static std::atomic<PFN_cuTensorMapEncodeTiled_v12000> fn{nullptr};
-    PFN_cuTensorMapEncodeTiled_v12000 f = fn.load(std::memory_order_acquire);
-    if (f == nullptr) {
-        void *ptr = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault,
-                                             &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess) {
-            f = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
-            fn.store(f, std::memory_order_release);
-        }
-    }
-    return f;
-}
 
 // The cache of a layer as [8-token group][64-element block of a token's heads][token][64]: a copy's
 // box is one head of a page (or of 128 keys of one), 8-token groups outermost, which in shared

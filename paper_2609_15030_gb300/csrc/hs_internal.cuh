@@ -56,10 +56,11 @@ inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, s
 // with cudaFuncSetAttribute on the first launch on each device (bit `dev` of `done`) instead
 // of on every call; if a launch still fails (the device's context was reset since), the
 // error is cleared, the limit set again and the launch retried once.
+// `limit`: what the kernel's largest launch needs, where launches differ.
 template <typename... KArgs, typename... Args>
-inline cudaError_t launch_pdl_big_smem(void (*kernel)(KArgs...), dim3 grid, dim3 block,
-                                       size_t smem, cudaStream_t stream,
-                                       std::atomic<uint64_t> &done, Args &&...args)
+inline cudaError_t launch_pdl_smem_limit(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                                         size_t limit, cudaStream_t stream,
+                                         std::atomic<uint64_t> &done, Args &&...args)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -67,7 +68,7 @@ inline cudaError_t launch_pdl_big_smem(void (*kernel)(KArgs...), dim3 grid, dim3
         return e;
     const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
     if (bit == 0 || (done.load(std::memory_order_acquire) & bit) == 0) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
         if (e != cudaSuccess)
             return e;
         done.fetch_or(bit, std::memory_order_acq_rel);
@@ -78,11 +79,19 @@ inline cudaError_t launch_pdl_big_smem(void (*kernel)(KArgs...), dim3 grid, dim3
         return e;
     (void)cudaGetLastError();
     done.fetch_and(~bit, std::memory_order_acq_rel);
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)limit);
     if (e != cudaSuccess)
         return e;
     done.fetch_or(bit, std::memory_order_acq_rel);
     return launch_pdl(kernel, grid, block, smem, stream, std::forward<Args>(args)...);
+}
+
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_pdl_big_smem(void (*kernel)(KArgs...), dim3 grid, dim3 block,
+                                       size_t smem, cudaStream_t stream,
+                                       std::atomic<uint64_t> &done, Args &&...args)
+{
+    return launch_pdl_smem_limit(kernel, grid, block, smem, smem, stream, done, std::forward<Args>(args)...);
 }
 
 // First detected device-side problem wins; kernels never clear the word.

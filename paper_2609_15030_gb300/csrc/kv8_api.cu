@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "hs_test.h"
 #include "kv8_internal.cuh"
 
 namespace {
@@ -134,6 +135,46 @@ hs_status append(const hs_attn_shape *shp, const hs_rope *rope, bool with_rope, 
         a.n_heads = s.n_heads;
     }
     return cuda_status(hs::launch_kv8_append(a, with_rope ? &params : nullptr, s.head_dim, s.dtype, sms, stream));
+}
+
+hs_status check_decode(const hs_attn_shape *shp, int64_t max_kv_len, hs::AttnParams &p)
+{
+    const hs_status st = hs::check_attn_decode(shp, 0, max_kv_len, p);
+    // the cache's rows of 128 bytes are counted in 31 bits
+    return st == HS_OK && shp->num_blocks > INT32_MAX / (block_bytes(*shp) / 128) ? HS_ERR_UNSUPPORTED : st;
+}
+
+hs_status decode(const hs_attn_shape *shp, const void *q, const void *cache, const int32_t *block_table,
+                 const int32_t *kv_len, int64_t max_kv_len, void *o, float *lse, void *workspace,
+                 int64_t workspace_bytes, int32_t *d_err, cudaStream_t stream, bool stall_for_test)
+{
+    hs::AttnParams p;
+    hs_status st = check_decode(shp, max_kv_len, p);
+    if (st != HS_OK || p.batch == 0)
+        return st;
+    if (kv_len == nullptr)
+        return HS_ERR_INVALID_ARG;
+    if (misaligned(kv_len, 4))
+        return HS_ERR_MISALIGNED;
+    p.q = q;
+    p.cache = cache;
+    p.table = block_table;
+    p.kv_len = kv_len;
+    p.o = o;
+    p.lse = lse;
+    p.d_err = d_err;
+    p.stall_for_test = stall_for_test;
+    st = hs::check_attn_pointers(p, workspace, workspace_bytes);
+    if (st != HS_OK)
+        return st;
+    int sms = 0;
+    st = hs::device_sm_count(&sms);
+    hs::Kv8Plan plan;
+    if (st == HS_OK)
+        st = hs::attn_workspace(hs::plan_kv8_decode(p, plan, shp->head_dim, sms), workspace, workspace_bytes, p);
+    if (st != HS_OK)
+        return st;
+    return cuda_status(hs::launch_kv8_decode(p, plan, cache_of(*shp, cache), shp->head_dim, shp->dtype, stream));
 }
 
 }  // namespace
@@ -272,31 +313,17 @@ hs_status hs_kv8_decode(const hs_attn_shape *shp, const void *q, const void *cac
                         float *lse, void *workspace, int64_t workspace_bytes, int32_t *d_err,
                         cudaStream_t stream)
 {
-    hs::AttnParams p;
-    hs_status st = hs::check_attn_decode(shp, 0, max_kv_len, p);
-    if (st != HS_OK || p.batch == 0)
-        return st;
-    if (kv_len == nullptr)
-        return HS_ERR_INVALID_ARG;
-    if (misaligned(kv_len, 4))
-        return HS_ERR_MISALIGNED;
-    p.q = q;
-    p.cache = cache;
-    p.table = block_table;
-    p.kv_len = kv_len;
-    p.o = o;
-    p.lse = lse;
-    p.d_err = d_err;
-    st = hs::check_attn_pointers(p, workspace, workspace_bytes);
-    if (st != HS_OK)
-        return st;
-    int sms = 0;
-    st = hs::device_sm_count(&sms);
-    if (st == HS_OK)
-        st = hs::attn_workspace(hs::plan_kv8_decode(p, shp->head_dim, sms), workspace, workspace_bytes, p);
-    if (st != HS_OK)
-        return st;
-    return cuda_status(hs::launch_kv8_decode(p, cache_of(*shp, cache), shp->head_dim, shp->dtype, stream));
+    return decode(shp, q, cache, block_table, kv_len, max_kv_len, o, lse, workspace, workspace_bytes, d_err, stream,
+                  false);
+}
+
+hs_status hs_test_kv8_stalled(const hs_attn_shape *shp, const void *q, const void *cache,
+                              const int32_t *block_table, const int32_t *kv_len, int64_t max_kv_len,
+                              void *o, float *lse, void *workspace, int64_t workspace_bytes,
+                              int32_t *d_err, cudaStream_t stream)
+{
+    return decode(shp, q, cache, block_table, kv_len, max_kv_len, o, lse, workspace, workspace_bytes, d_err, stream,
+                  true);
 }
 
 hs_status hs_kv8_decode_workspace_bytes(const hs_attn_shape *shp, int64_t max_kv_len, int64_t *bytes_out)
@@ -304,7 +331,7 @@ hs_status hs_kv8_decode_workspace_bytes(const hs_attn_shape *shp, int64_t max_kv
     if (bytes_out == nullptr)
         return HS_ERR_INVALID_ARG;
     hs::AttnParams p;
-    hs_status st = hs::check_attn_decode(shp, 0, max_kv_len, p);
+    hs_status st = check_decode(shp, max_kv_len, p);
     if (st != HS_OK)
         return st;
     *bytes_out = 0;
@@ -314,7 +341,8 @@ hs_status hs_kv8_decode_workspace_bytes(const hs_attn_shape *shp, int64_t max_kv
     st = hs::device_sm_count(&sms);
     if (st != HS_OK)
         return st;
-    const int64_t need = hs::plan_kv8_decode(p, shp->head_dim, sms);
+    hs::Kv8Plan plan;
+    const int64_t need = hs::plan_kv8_decode(p, plan, shp->head_dim, sms);
     if (need < 0)
         return HS_ERR_UNSUPPORTED;
     *bytes_out = need;

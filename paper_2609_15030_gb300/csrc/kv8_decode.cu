@@ -11,34 +11,50 @@
 // for each row.
 //
 // Shares.  A tile is a group of 16 tokens.  Every warp has a contiguous run of tiles of its own, shared out
-// evenly over all warps of the GPU from the device lengths, with no hand-over until its end: a warp loads its keys and
-// values into registers (they arrive in the order of the tensor core's operands, whose sums over d
-// and tokens may go in any order), S^T = K Q^T (16 tokens x 8 rows for each instruction), turns the weights'
-// tile by a matrix transpose between lanes, O^T += V^T W^T.  The warps of a block join their parts of an
-// item (request, KV head, 8 or 16 query rows) in shared memory; an item with tiles in several blocks leaves a part
-// for each in the workspace, and a second kernel joins these.  With `unsplit`, and where the bound is short,
+// evenly over all warps of the GPU from the device lengths, with no hand-over until its end.  A warp's lane requests its
+// next tiles by TMA (they land in swizzled rows, so that the operands are read without bank conflicts, in whatever order
+// of d and tokens suits that); per tile S^T = K Q^T (16 tokens x 8 rows to an instruction), the weights' matrix is
+// turned between lanes, O^T += V^T W^T.  The warps of a block join their parts of an
+// item (request, KV head, 8 or 16 query rows), and an item with tiles in several blocks leaves a part
+// for each in the workspace, which a second kernel joins.  With `unsplit`, and where the bound is short,
 // a block takes whole items instead.
 //
 // Few rows share a tile's bytes (the heads of one KV head), so the step is bound by HBM; products of M = 128 rows as in
-// the 16-bit attention would leave most of the tensor core's rows empty and the bytes would have to
+// the 16-bit attention would leave most of the tensor core's rows empty, and the bytes would have to
 // become numbers on a way through shared memory.
 #include "kv8_walk.cuh"
+#include "sm100_ptx.cuh"
+#include "tensor_map.cuh"
 
 namespace hs {
 namespace kv8 {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kWholeTiles = 10;
 
 // floats of a part: per row m and l, then its sums, rows padded against bank conflicts
 template <int D, int R>
 constexpr int kPartFloats = 2 * R + R * (D + 4);
 
+// The kernel's sizes.  A warp takes a step of kTiles tiles at a time; its steps arrive in a ring of its own in shared
+// memory, kStages - 1 ahead.
+template <int D, int NT>
+struct Sizes {
+    static constexpr int R = 8 * NT;
+    static constexpr int kTiles = D == 128 && NT == 1 ? 1 : 2;
+    static constexpr int kWarps = D == 128 ? (NT == 1 ? 12 : 8) : NT == 1 ? 16 : 12;
+    static constexpr int kStages = D == 128 ? (NT == 1 ? 4 : 2) : 3;
+    static constexpr int kThreads = kWarps * 32;
+    static constexpr int kPlaneBytes = kGroup * D, kTileBytes = 2 * kPlaneBytes;
+    static constexpr int kStageBytes = kTiles * kTileBytes, kRingBytes = kStages * kStageBytes;
+    static_assert(kStageBytes % 1024 == 0 && kRingBytes >= (int)sizeof(float) * kPartFloats<D, R>);
+    static constexpr size_t smem(int warps) { return (size_t)warps * kRingBytes + 1024; }
+};
+
 // one of a block's parts
 struct Part {
-    int32_t b, item;              // item: KV head * row tiles + row tile
-    int32_t starts, ends;         // with the item's first and last tile
-    int32_t used;
+    int32_t item;                 // request * items of a request + item; -1: none
+    int16_t starts, ends;         // with the item's first and last tile
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -48,19 +64,22 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-__device__ __forceinline__ uint4 load16(const void *p)
+// 4 bytes to shared memory
+__device__ __forceinline__ void copy4(uint32_t to, const void *from)
 {
-    uint4 x;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
-    return x;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
 }
 
-__device__ __forceinline__ uint2 load8(const void *p)
+__device__ __forceinline__ void commit()
 {
-    uint2 x;
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
-    return x;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
+// until all but the last N groups have arrived
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -80,26 +99,19 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x)
     return y;
 }
 
-// items of a request, and the units of one
-struct Shape {
-    int row_tiles, per_request;
-    __host__ __device__ Shape(const AttnParams &p, int rows)
-        : row_tiles((p.group + rows - 1) / rows), per_request(row_tiles * p.n_kv)
-    {
-    }
-    __host__ __device__ static int units(int len)
-    {
-        return len > 0 ? groups_of(len) : 1;      // an empty row is written by someone
-    }
-};
+// tiles of an item
+__host__ __device__ __forceinline__ int units_of(int len)
+{
+    return len > 0 ? groups_of(len) : 1;          // an empty row is written by someone
+}
 
-// where the results of an item's rows go
+// the rows of an item (KV head * row tiles + row tile) of request b
 template <int R>
 struct Rows {
     int b, head, n;               // head: of the first row
-    __device__ Rows(const AttnParams &p, const Shape &shape, int b_, int item) : b(b_)
+    __device__ __forceinline__ Rows(const AttnParams &p, const Kv8Plan &plan, int b_, int item) : b(b_)
     {
-        const int kvh = item / shape.row_tiles, rt = item - kvh * shape.row_tiles;
+        const int kvh = plan.by_row_tiles.div(item), rt = item - kvh * plan.row_tiles;
         head = kvh * p.group + rt * R;
         n = min(R, p.group - rt * R);
     }
@@ -116,23 +128,32 @@ struct Warp {
     float o[D / 16][NT][4];
     float top;                    // 2^E
 
-    __device__ __forceinline__ void begin(const AttnParams &p, const Rows<R> &rows, int lane)
+    // the queries as they are
+    __device__ __forceinline__ static void load(uint32_t (&x)[NT][C][8], const AttnParams &p, const Rows<R> &rows, int lane)
     {
         const int g = lane >> 2, t = lane & 3;
-        top = 0x1p-100f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const bool on = n * 8 + g < rows.n;
             const T *const row = static_cast<const T *>(p.q) + rows.b * p.q_stride +
-                                 (int64_t)(rows.head + n * 8 + (on ? g : 0)) * D;
-            uint32_t x[C][8];
+                                 (int64_t)(rows.head + n * 8 + g) * D + t * 16 * C;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const uint4 *const at = reinterpret_cast<const uint4 *>(row + c * 64 + t * 16);
-                const uint4 y0 = at[0], y1 = at[1];
-                x[c][0] = y0.x, x[c][1] = y0.y, x[c][2] = y0.z, x[c][3] = y0.w;
-                x[c][4] = y1.x, x[c][5] = y1.y, x[c][6] = y1.z, x[c][7] = y1.w;
-            }
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint4 y = on ? reinterpret_cast<const uint4 *>(row + c * 16)[i] : make_uint4(0, 0, 0, 0);
+                    x[n][c][4 * i] = y.x, x[n][c][4 * i + 1] = y.y, x[n][c][4 * i + 2] = y.z, x[n][c][4 * i + 3] = y.w;
+                }
+        }
+    }
+
+    __device__ __forceinline__ void begin(uint32_t (&raw)[NT][C][8], const AttnParams &p, int lane)
+    {
+        const int t = lane & 3;
+        top = 0x1p-100f;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            uint32_t (&x)[C][8] = raw[n];
             float by = p.scale_log2;
             if constexpr (!std::is_same<T, __half>::value) {
                 float most = 0.f;
@@ -162,7 +183,7 @@ struct Warp {
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    q[c * 4 + i / 2][n][i & 1] = on ? x[c][i] : 0u;
+                    q[c * 4 + i / 2][n][i & 1] = x[c][i];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 factor[n][i] = __shfl_sync(0xffffffffu, by, (2 * t + i) * 4);
@@ -177,7 +198,7 @@ struct Warp {
         }
     }
 
-    // scores of a tile: k[c][i] the 16 bytes [64 c + 16 t, + 16) of token g + 8 i
+    // scores of a tile: k[c][i] the 16 bytes [16 (C t + c), + 16) of tokens token_of(g + 8 i)
     __device__ __forceinline__ void scores(const uint4 (&k)[C][2], float scale, float (&s)[NT][4]) const
     {
         float s2[NT][4];
@@ -210,57 +231,71 @@ struct Warp {
         }
     }
 
-    // scores into weights, as the second product's operand
-    __device__ __forceinline__ void weights(float (&s)[NT][4], float scale, uint32_t (&w)[NT][2])
+    // the scores of N tiles into weights, as the second product's operand; scale: of the tiles' values
+    template <int N>
+    __device__ __forceinline__ void weights(const float (&s)[N][NT][4], const float (&scale)[N], uint32_t (&w)[N][NT][2])
     {
+        float x[NT][2];
         bool more = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-            more = more || fmaxf(s[n][0], s[n][2]) > m[n][0] + 8.f || fmaxf(s[n][1], s[n][3]) > m[n][1] + 8.f;
-        if (__any_sync(0xffffffffu, more)) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                x[n][i] = fmaxf(s[0][n][i], s[0][n][i + 2]);
+#pragma unroll
+                for (int a = 1; a < N; ++a)
+                    x[n][i] = fmaxf(x[n][i], fmaxf(s[a][n][i], s[a][n][i + 2]));
+                more = more || x[n][i] > m[n][i] + 8.f;
+            }
+        float most = scale[0];
+#pragma unroll
+        for (int a = 1; a < N; ++a)
+            most = fmaxf(most, scale[a]);
+        if (__any_sync(0xffffffffu, more || most > top)) {
+            float h0 = 1.f;
+            if (most > top) {
+                // a power of two even where the cache's scale is none
+                const float up = __uint_as_float(__float_as_uint(most) & 0x7f800000u);
+                h0 = top / up;
+                top = up;
+            }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float x = fmaxf(s[n][i], s[n][i + 2]);
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                    if (x > m[n][i]) {
-                        const float h = ex2(m[n][i] - x);
-                        m[n][i] = x;
+                    float y = x[n][i];
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+                    float h = 1.f;
+                    if (y > m[n][i]) {
+                        h = ex2(m[n][i] - y);
+                        m[n][i] = y;
                         l[n][i] *= h;
+                    }
+                    h *= h0;
 #pragma unroll
-                        for (int d = 0; d < D / 16; ++d) {
-                            o[d][n][i] *= h;
-                            o[d][n][i + 2] *= h;
-                        }
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[d][n][i] *= h;
+                        o[d][n][i + 2] *= h;
                     }
                 }
         }
-        if (scale > top) {
-            // a power of two even where the cache's scale is none
-            const float up = __uint_as_float(__float_as_uint(scale) & 0x7f800000u), h = top / up;
-            top = up;
+        const float down = 128.f / top;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d)
+        for (int a = 0; a < N; ++a) {
+            const float by = scale[a] * down;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n) {
+                float y[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        o[d][n][i] *= h;
-        }
-        const float by = scale * (128.f / top);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = ex2(s[n][i] - m[n][i & 1]);
-                l[n][i & 1] += x[i];
+                for (int i = 0; i < 4; ++i) {
+                    y[i] = ex2(s[a][n][i] - m[n][i & 1]);
+                    l[n][i & 1] += y[i];
+                }
+                w[a][n][0] = transposed(narrow<__half>(y[0] * by, y[1] * by));
+                w[a][n][1] = transposed(narrow<__half>(y[2] * by, y[3] * by));
             }
-            w[n][0] = transposed(narrow<__half>(x[0] * by, x[1] * by));
-            w[n][1] = transposed(narrow<__half>(x[2] * by, x[3] * by));
         }
     }
 
@@ -318,7 +353,7 @@ struct Warp {
                 uint32_t x[D / 16];
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j)
-                    x[j] = narrow<T>(within<T>(sum(n, i, 2 * j) * by), within<T>(sum(n, i, 2 * j + 1) * by));
+                    x[j] = narrow_finite<T>(sum(n, i, 2 * j) * by, sum(n, i, 2 * j + 1) * by);
                 uint4 *const to = reinterpret_cast<uint4 *>(static_cast<T *>(p.o) + rows.b * p.o_stride +
                                                             (int64_t)(rows.head + r) * D + g * (D / 8));
 #pragma unroll
@@ -352,411 +387,595 @@ struct Warp {
     }
 };
 
-// the tiles of one request's KV head, as a warp loads them
+// A tile's token that stands in row i of the products (tokens may go in any order): with 64 bytes to a token two of them
+// share a 128-byte row of shared memory, and neighbours in it are neighbours in i.
 template <int D>
-struct Tiles {
-    const Kv8Cache &cache;
-    const int32_t *table;         // the request's row
-    int pages;                    // entries of it
-    int head, lane, num_blocks;
-    int32_t *d_err;
-    int first;                    // page of ids' lane 0
-    int32_t ids;                  // this lane's entry
-
-    __device__ __forceinline__ void fetch(int page)
-    {
-        first = page;
-        ids = page + lane < pages ? __ldg(table + page + lane) : 0;
-        if (ids < 0 || ids >= cache.num_blocks) {
-            report(d_err, HS_DEVERR_BLOCK_OOB);
-            ids = -1;
-        }
-    }
-    // the first byte of a tile's keys, nullptr where its page is none
-    __device__ __forceinline__ const uint8_t *find(int tile, const float **scale)
-    {
-        const int shift = cache.page_shift - 4, page = tile >> shift;
-        if (page - first >= 32)
-            fetch(page);
-        const int id = __shfl_sync(0xffffffffu, ids, page - first);
-        if (id < 0)
-            return nullptr;
-        float *at;
-        const uint8_t *const k = group_at<D>(cache, id, tile & ((1 << shift) - 1), 2 * head, &at);
-        *scale = at;
-        return k;
-    }
-};
-
-template <typename T, int D, int NT>
-__device__ __forceinline__ void walk(const AttnParams &p, const Kv8Cache &cache, Warp<T, D, NT> &w, int b, int len, int kvh,
-                                     const Rows<8 * NT> &rows, int tile, int n, int lane)
+__device__ __forceinline__ int token_of(int i)
 {
-    constexpr int C = D / 64;
-    const int g = lane >> 2, t = lane & 3;
-    Tiles<D> tiles{cache, p.table + (int64_t)b * p.max_pages, ((len - 1) >> cache.page_shift) + 1, kvh, lane, 0, p.d_err, 0, 0};
-    if (n > 0)
-        tiles.fetch(tile >> (cache.page_shift - 4));
-    uint4 k[C][2];
-    uint32_t v[4][D / 32];
-    float k_scale = 0.f, v_scale = 0.f;
-    const uint8_t *at = nullptr;
-    const float *scale_at = nullptr;
-    const int64_t plane = plane_bytes<D>(cache);
-    const int groups = 1 << (cache.page_shift - 4);
-    auto load_k = [&](int i) {
-        at = tiles.find(i, &scale_at);
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                k[c][j] = at != nullptr ? load16(at + (g + 8 * j) * D + c * 64 + t * 16) : make_uint4(0, 0, 0, 0);
-        k_scale = at != nullptr ? __ldg(scale_at) : 0.f;
-    };
-    auto load_v = [&]() {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint8_t *const from = at + plane + (2 * t + (i & 1) + (i >> 1) * 8) * D + g * (D / 8);
-            if constexpr (D == 128) {
-                const uint4 x = at != nullptr ? load16(from) : make_uint4(0, 0, 0, 0);
-                v[i][0] = x.x, v[i][1] = x.y, v[i][2] = x.z, v[i][3] = x.w;
-            } else {
-                const uint2 x = at != nullptr ? load8(from) : make_uint2(0, 0);
-                v[i][0] = x.x, v[i][1] = x.y;
-            }
-        }
-        v_scale = at != nullptr ? __ldg(scale_at + groups) : 0.f;
-    };
-    if (n > 0) {
-        load_k(tile);
-        load_v();
-    }
-    w.begin(p, rows, lane);
-    for (int i = tile; i < tile + n; ++i) {
-        float s[NT][4];
-        uint32_t x[NT][2];
-        w.scores(k, k_scale, s);
-        if (i + 1 < tile + n)
-            load_k(i + 1);
-        const int left = len - i * kGroup;
-        if (left < kGroup) {
-            // behind the last key: no score, and values of zero (a weight of 0 times NaN is NaN)
-#pragma unroll
-            for (int a = 0; a < NT; ++a)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (g + 8 * (c >> 1) >= left)
-                        s[a][c] = -INFINITY;
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-                if (2 * t + (a & 1) + (a >> 1) * 8 >= left)
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c)
-                        v[a][c] = 0;
-        }
-        w.weights(s, v_scale, x);
-        w.sums(v, x);
-        if (i + 1 < tile + n)
-            load_v();
-    }
-    w.end();
+    return D == 128 ? i : ((i & 7) >> 1) * 4 + (i >> 3) * 2 + (i & 1);
 }
 
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
-kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Kv8Cache cache)
-{
-    constexpr int R = 8 * NT, kSlots = 2 * kWarps;
-    extern __shared__ float4 shared[];
-    float *const parts = reinterpret_cast<float *>(shared);
-    __shared__ Lengths all;
-    __shared__ Part part[kSlots];
-    pdl_wait_and_release();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Shape shape(p, R);
-    read_lengths(all, p.kv_len, p.batch, p.max_kv, p.d_err,
-                 [&](int len) { return Shape::units(len) * shape.per_request; });
-    const int units = all.before[p.batch];
+// The loads of a warp's run, ahead of its products.
+template <int D, int NT>
+struct Loader {
+    using S = Sizes<D, NT>;
+    const AttnParams &p;
+    const Kv8Cache &cache;
+    const CUtensorMap &map;
+    const Lengths &all;
+    const Kv8Plan &plan;
+    const uint32_t ring, bars, scales;   // in shared memory
+    const int lane;
+    int left = 0;                 // units of the run not asked for
+    int b, item, tile, len;       // the next one's item
+    int stage = 0;
+    int first = 0, ids = 0;       // the page of lane 0's id
 
-    // the block's run: its share of all units, or one whole item after the other
-    for (int turn = blockIdx.x;; turn += gridDim.x) {
-        int u0, u1, b = 0;
-        if (p.unsplit) {
-            if (turn >= p.batch * shape.per_request)
-                return;
-            b = turn / shape.per_request;
-            if (all.len[b] < 0)
-                continue;
-            const int n = Shape::units(all.len[b]);
-            u0 = all.before[b] + (turn - b * shape.per_request) * n;
-            u1 = u0 + n;
-        } else {
-            u0 = attn::first_unit(units, gridDim.x, blockIdx.x);
-            u1 = attn::first_unit(units, gridDim.x, blockIdx.x + 1);
-        }
-        if (threadIdx.x < kSlots)
-            part[threadIdx.x].used = 0;
-        __syncthreads();
-        int u = u0 + (int)((int64_t)(u1 - u0) * warp / kWarps);
-        const int end = u0 + (int)((int64_t)(u1 - u0) * (warp + 1) / kWarps);
-        if (u < end) {
-            b = request_of(all, p.batch, u, lane);
-            int per = Shape::units(all.len[b]);
-            int item = (u - all.before[b]) / per, tile = (u - all.before[b]) - item * per;
-            int slot = 2 * warp;
-            while (u < end) {
-                const int len = all.len[b], n = min(per - tile, end - u);
-                const Rows<R> rows(p, shape, b, item);
-                Warp<T, D, NT> w;
-                walk<T, D, NT>(p, cache, w, b, len, item / shape.row_tiles, rows, tile, len > 0 ? n : 0, lane);
-                if (n == per) {
-                    w.write(p, rows, lane);
-                } else {
-                    w.leave(parts + slot * kPartFloats<D, R>, lane);
-                    if (lane == 0)
-                        part[slot] = Part{b, item, tile == 0, tile + n == per, 1};
-                    ++slot;
+    __device__ __forceinline__ void begin(int left_, int b_, int item_, int tile_, int len_)
+    {
+        left = left_, b = b_, item = item_, tile = tile_, len = len_;
+        first = -64;
+    }
+    // the next step.  What lies in the ring stays where a page is none (that request's results mean nothing)
+    __device__ __forceinline__ void issue()
+    {
+        if (left > 0) {
+            const int per = units_of(len), n = min(S::kTiles, min(per - tile, left));
+            const int shift = cache.page_shift - 4, head_plane = 2 * plan.by_row_tiles.div(item);
+            const uint32_t bar = bars + 8 * stage, to = ring + stage * S::kStageBytes;
+#pragma unroll 1
+            for (int a = 0; a < S::kTiles; ++a) {
+                int id = -1;
+                const int page = (tile + a) >> shift, in_page = (tile + a) & ((1 << shift) - 1);
+                if (a < n && len > 0) {
+                    if ((unsigned)(page - first) >= 32) {
+                        first = page;
+                        ids = page + lane <= (len - 1) >> cache.page_shift ? __ldg(p.table + b * p.max_pages + page + lane) : 0;
+                        if (ids < 0 || ids >= cache.num_blocks) {
+                            report(p.d_err, HS_DEVERR_BLOCK_OOB);
+                            ids = -1;
+                        }
+                    }
+                    id = __shfl_sync(0xffffffffu, ids, page - first);
                 }
-                u += n;
+                if (id >= 0 && lane < 2) {
+                    float *at;
+                    group_at<D>(cache, id, in_page, head_plane, &at);
+                    copy4(scales + (stage * S::kTiles + a) * 8 + 4 * lane, at + (lane << shift));
+                }
+                if (lane == 0) {
+                    ptx::mbar_arrive_expect_tx(bar, id >= 0 ? S::kTileBytes : 0);
+                    if (id >= 0) {
+                        const int y = id * (int)(cache.block_bytes / 128) +
+                                      ((head_plane << shift) + in_page) * (S::kPlaneBytes / 128);
+                        ptx::tma_load_2d(to + a * S::kTileBytes, &map, 0, y, bar);
+                        ptx::tma_load_2d(to + a * S::kTileBytes + S::kPlaneBytes, &map, 0,
+                                         y + (S::kPlaneBytes / 128 << shift), bar);
+                    }
+                }
+            }
+            stage = stage + 1 == S::kStages ? 0 : stage + 1;
+            left -= n;
+            tile += n;
+            if (tile == per && left > 0) {
                 tile = 0;
-                if (++item == shape.per_request && u < end) {
+                first = -64;
+                if (++item == plan.items) {
                     item = 0;
                     do
                         ++b;
                     while (all.before[b + 1] == all.before[b]);
-                    per = Shape::units(all.len[b]);
+                    len = all.len[b];
                 }
+            }
+        }
+        commit();
+    }
+};
+
+// the products of a step: n tiles from `tile` on, of an item with `len` tokens
+template <typename T, int D, int NT>
+__device__ __forceinline__ void step(Warp<T, D, NT> &w, const uint8_t *at, const float *scales, int tile, int n, int len,
+                                     int lane)
+{
+    using S = Sizes<D, NT>;
+    constexpr int C = D / 64, N = S::kTiles;
+    const int g = lane >> 2, t = lane & 3;
+    float s[N][NT][4], v_scale[N];
+    uint32_t x[N][NT][2];
+    // a 128-byte row's 16-byte chunk c lies at c ^ (row & 7)
+    const int k_row = D == 128 ? g : g & 6, k_chunk = D == 128 ? 2 * t : (g & 1) * 4 + t;
+#pragma unroll
+    for (int a = 0; a < N; ++a) {
+        uint4 k[C][2];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = D == 128 ? k_row + 8 * j : k_row + j;
+                k[c][j] = *reinterpret_cast<const uint4 *>(at + a * S::kTileBytes + row * 128 + (((k_chunk + c) ^ (row & 7)) << 4));
+            }
+        w.scores(k, scales[2 * a], s[a]);
+        v_scale[a] = a < n ? scales[2 * a + 1] : 0.f;
+    }
+    const bool tail = n < N || len - tile * kGroup < N * kGroup;
+    if (tail) {
+#pragma unroll
+        for (int a = 0; a < N; ++a) {
+            const int left = a < n ? len - (tile + a) * kGroup : 0;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (token_of<D>(g + 8 * (c >> 1)) >= left)
+                        s[a][i][c] = -INFINITY;
+        }
+    }
+    w.template weights<N>(s, v_scale, x);
+#pragma unroll
+    for (int a = 0; a < N; ++a) {
+        const uint8_t *const from = at + a * S::kTileBytes + S::kPlaneBytes;
+        uint32_t v[4][D / 32];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (D == 128) {
+                const int row = 2 * t + (j & 1) + (j >> 1) * 8;
+                const uint4 y = *reinterpret_cast<const uint4 *>(from + row * 128 + ((g ^ (row & 7)) << 4));
+                v[j][0] = y.x, v[j][1] = y.y, v[j][2] = y.z, v[j][3] = y.w;
+            } else {
+                const int row = 2 * t + (j >> 1), chunk = (j & 1) * 4 + (g >> 1);
+                const uint2 y = *reinterpret_cast<const uint2 *>(from + row * 128 + ((chunk ^ row) << 4) + (g & 1) * 8);
+                v[j][0] = y.x, v[j][1] = y.y;
+            }
+        }
+        if (tail) {
+            // behind the last key: values of zero (a weight of 0 times NaN is NaN)
+            const int left = a < n ? len - (tile + a) * kGroup : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (token_of<D>(2 * t + (j & 1) + (j >> 1) * 8) >= left)
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c)
+                        v[j][c] = 0;
+        }
+        w.sums(v, x[a]);
+    }
+}
+
+// where an item's result goes that a block has the beginning but not the end of (item < 0: none), for the join
+struct Split {
+    int32_t item, last;                            // index of the item; the last block with a part
+};
+
+__host__ __device__ __forceinline__ int64_t parts_at(int ctas)
+{
+    return (int64_t)(ctas + 1) / 2 * 4;            // parts stay 16-byte aligned
+}
+
+// one row's result, a lane's columns c to c + 3
+template <typename T, int D>
+__device__ __forceinline__ void write_row(const AttnParams &p, int b, int head, int c, float4 o, float m, float l)
+{
+    const float by = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + b * p.o_stride + (int64_t)head * D + c) =
+        make_uint2(narrow_finite<T>(o.x * by, o.y * by), narrow_finite<T>(o.z * by, o.w * by));
+    if (c == 0 && p.lse != nullptr)
+        p.lse[(int64_t)b * p.n_heads + head] = 0.6931471805599453f * (m + log2f(l));
+}
+
+// Parts of a row joined by a warp: lane i has part i's m and l (-infinity and 0: none), row_of(i, i % kAhead) a lane's four
+// columns of its sums, loaded kAhead at a time.
+template <int kAhead, typename RowOf>
+__device__ __forceinline__ float4 join(float &m, float &l, int count, RowOf row_of)
+{
+    float top = m;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1)
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    const float h = m == -INFINITY && l == 0.f ? 0.f : ex2(m - top);
+    m = top;
+    l *= h;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1)
+        l += __shfl_xor_sync(0xffffffffu, l, x);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+        float4 x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            x[k] = row_of(min(i0 + k, count - 1), k);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const float hi = __shfl_sync(0xffffffffu, h, (i0 + k) & 31);
+            if (i0 + k < count)
+                o.x = fmaf(x[k].x, hi, o.x), o.y = fmaf(x[k].y, hi, o.y), o.z = fmaf(x[k].z, hi, o.z),
+                o.w = fmaf(x[k].w, hi, o.w);
+        }
+    }
+    return o;
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(Sizes<D, NT>::kThreads, 1)
+kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Kv8Plan plan,
+                  const __grid_constant__ Kv8Cache cache,
+                  const __grid_constant__ CUtensorMap map)
+{
+    using S = Sizes<D, NT>;
+    constexpr int R = S::R, kPart = kPartFloats<D, R>;
+    extern __shared__ uint8_t shared[];
+    __shared__ Lengths all;
+    __shared__ Part part[2 * S::kWarps];
+    __shared__ int32_t order[2 * S::kWarps], firsts[2 * S::kWarps + 1];
+    __shared__ float scales[S::kWarps][S::kStages][2 * S::kTiles];
+    __shared__ uint64_t bars[S::kWarps][S::kStages + 1];     // the last one is for failure-detection tests
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    uint8_t *const rings = shared + (-(intptr_t)ptx::smem_u32(shared) & 1023), *const ring = rings + warp * S::kRingBytes;
+    if (lane <= S::kStages)
+        ptx::mbar_init(ptx::smem_u32(&bars[warp][lane]), S::kTiles);
+    ptx::fence_mbar_init();
+    __syncwarp();
+    pdl_wait_and_release();
+    Loader<D, NT> loader{p, cache, map, all, plan, ptx::smem_u32(ring), ptx::smem_u32(bars[warp]),
+                         ptx::smem_u32(scales[warp]), lane};
+    int stage = 0, parity = 0;
+    bool lost = false;                                       // a wait has run out
+    if (!p.unsplit)
+        read_lengths(all, p.kv_len, p.batch, p.max_kv, p.d_err,
+                     [&](int len) { return units_of(len) * plan.items; });
+    const Shares shares(p.unsplit ? 0 : all.before[p.batch], plan.by_ctas);
+
+    // the block's run: its share of all units, or one whole item after the other
+    for (int turn = blockIdx.x;; turn += gridDim.x) {
+        int u, end, b, item, tile, len;                      // of the warp's run
+        if (p.unsplit) {
+            if (turn >= p.batch * plan.items)
+                return;
+            b = plan.by_items.div(turn);
+            item = turn - b * plan.items;
+            len = p.kv_len[b];
+            if (len < 0 || len > p.max_kv) {
+                if (threadIdx.x == 0)
+                    report(p.d_err, HS_DEVERR_LENGTH);
+                continue;
+            }
+            const int n = units_of(len);
+            const Shares over(n, plan.by_warps);
+            u = tile = over.begin(warp);
+            end = over.begin(warp + 1);
+        } else {
+            u = end = b = item = tile = len = 0;
+            const int u0 = shares.begin(blockIdx.x);
+            const Shares over(shares.begin(blockIdx.x + 1) - u0, plan.by_warps);
+            u = u0 + over.begin(warp);
+            end = u0 + over.begin(warp + 1);
+            if (u < end) {
+                b = request_of(all, p.batch, u, lane);
+                len = all.len[b];
+                const int per = units_of(len);
+                item = (u - all.before[b]) / per;
+                tile = (u - all.before[b]) - item * per;
+            }
+        }
+        if (lane < 2)
+            part[2 * warp + lane].item = -1;
+        if (u < end && !lost) {
+            uint32_t raw[NT][D / 64][8];
+            Warp<T, D, NT>::load(raw, p, Rows<R>(p, plan, b, item), lane);
+            ptx::fence_proxy_async_smem();                   // the ring held parts
+            loader.begin(end - u, b, item, tile, len);
+            Warp<T, D, NT> w;
+            int from = tile, n = min(units_of(len) - tile, end - u);     // the segment: tiles [from, from + n)
+#pragma unroll 1
+            for (int ahead = 1 - S::kStages;; ++ahead) {
+                if (ahead >= 0) {
+                    lost = !ptx::mbar_wait_bounded(p.stall_for_test ? loader.bars + 8 * S::kStages : loader.bars + 8 * stage,
+                                                   parity, p.limit_ns);
+                    arrived<S::kStages - 2>();
+                    lost = __any_sync(0xffffffffu, lost);    // the scales are there too, and the stage before is free
+                    if (lost)
+                        break;
+                }
+                loader.issue();
+                if (ahead < 0)
+                    continue;
+                if (tile == from)
+                    w.begin(raw, p, lane);
+                if (len > 0)
+                    step(w, ring + stage * S::kStageBytes, scales[warp][stage], tile, min(S::kTiles, from + n - tile), len, lane);
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    parity ^= 1;
+                }
+                tile += S::kTiles;
+                if (tile < from + n)
+                    continue;
+                // the segment's end
+                const int per = units_of(len);
+                const Rows<R> rows(p, plan, b, item);
+                u += n;
+                w.end();
+                if (n == per) {
+                    w.write(p, rows, lane);
+                } else {
+                    // the run's last part goes over the ring, one in front of it to the workspace
+                    const bool last = u == end;
+                    if (last)
+                        arrived<0>();
+                    __syncwarp();
+                    w.leave(last ? reinterpret_cast<float *>(ring)
+                                 : p.part + parts_at(gridDim.x) + (int64_t)(2 * gridDim.x + blockIdx.x * warps + warp) * kPart, lane);
+                    if (lane == 0)
+                        part[2 * warp + last] = Part{b * plan.items + item, from == 0, from + n == per};
+                }
+                if (u == end)
+                    break;
+                if (++item == plan.items) {
+                    item = 0;
+                    do
+                        ++b;
+                    while (all.before[b + 1] == all.before[b]);
+                    len = all.len[b];
+                }
+                from = tile = 0;
+                n = min(units_of(len), end - u);
+                Warp<T, D, NT>::load(raw, p, Rows<R>(p, plan, b, item), lane);
+            }
+            if (lost) {
+                // wait for what is on its way, and leave
+                report(p.d_err, HS_DEVERR_TIMEOUT);
+                while (stage != loader.stage) {
+                    (void)ptx::mbar_wait_bounded(loader.bars + 8 * stage, parity, p.limit_ns);
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        parity ^= 1;
+                    }
+                }
+                arrived<0>();
             }
         }
         __syncthreads();
-        // join the parts of each item, which stand one behind the other
-        for (int s0 = 0; s0 < kSlots;) {
-            if (!part[s0].used) {
-                ++s0;
+
+        // Join the parts of each item.  Those of an item stand one behind the other in the order of slots; every warp finds
+        // the same order, and takes rows of items in turn.
+        const Part mine = lane < 2 * warps ? part[lane] : Part{-1, 0, 0};
+        const unsigned used = __ballot_sync(0xffffffffu, mine.item >= 0);
+        if (mine.item >= 0)
+            order[__popc(used & ((1u << lane) - 1))] = lane;
+        __syncwarp();
+        const int count = __popc(used), slot = lane < count ? order[lane] : 0;
+        const int items = __shfl_sync(0xffffffffu, mine.item, slot);
+        const int in_front = __shfl_up_sync(0xffffffffu, items, 1);
+        const bool begins = lane < count && (lane == 0 || items != in_front);
+        const unsigned begin = __ballot_sync(0xffffffffu, begins);
+        if (begins)
+            firsts[__popc(begin & ((1u << lane) - 1))] = lane;
+        const int chains = __popc(begin);
+        if (lane == 0)
+            firsts[chains] = count;
+        __syncwarp();
+        for (int job = warp; job < chains * R; job += warps) {
+            const int c = job / R, r = job - c * R, i0 = firsts[c], n = firsts[c + 1] - i0;
+            const int own = order[i0 + min(lane, n - 1)];
+            const float *at = own & 1 ? reinterpret_cast<const float *>(rings + (own >> 1) * S::kRingBytes)
+                                      : p.part + parts_at(gridDim.x) +
+                                            (int64_t)(2 * gridDim.x + blockIdx.x * warps + (own >> 1)) * kPart;
+            const Part a = part[own];
+            const int it = a.item, bb = plan.by_items.div(it);
+            const bool starts = __shfl_sync(0xffffffffu, a.starts, 0), ends = __shfl_sync(0xffffffffu, a.ends, n - 1);
+            const Rows<R> rows(p, plan, bb, it - bb * plan.items);
+            if (r >= rows.n || (!(starts && ends) && !p.joined))       // the latter: a wait has run out
+                continue;
+            float m = -INFINITY, l = 0.f;
+            if (lane < n) {
+                m = at[2 * r];
+                l = at[2 * r + 1];
+            }
+            const int col = lane * 4 % D;                   // 64 columns: the second half of the lanes repeats the first
+            at += 2 * R + r * (D + 4);
+            const float4 o = join<4>(m, l, n, [&](int i, int) {
+                return *reinterpret_cast<const float4 *>(
+                    reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, (unsigned long long)at, i)) + col);
+            });
+            if (lane * 4 >= D)
+                continue;
+            if (starts && ends) {
+                write_row<T, D>(p, bb, rows.head + r, col, o, m, l);
                 continue;
             }
-            int s1 = s0, last = s0;
-            for (; s1 < kSlots; ++s1)
-                if (part[s1].used) {
-                    if (part[s1].b != part[s0].b || part[s1].item != part[s0].item)
-                        break;
-                    last = s1;
-                }
-            const Rows<R> rows(p, shape, part[s0].b, part[s0].item);
-            const bool whole = part[s0].starts && part[last].ends;
-            float *const left = p.part + (int64_t)(2 * blockIdx.x + part[s0].starts) * kPartFloats<D, R>;
-            for (int i = threadIdx.x; i < rows.n * (D / 4); i += kThreads) {
-                const int r = i / (D / 4), c = i - r * (D / 4);
-                float m = -INFINITY, l = 0.f;
-                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int s = s0; s < s1; ++s)
-                    if (part[s].used)
-                        m = fmaxf(m, parts[s * kPartFloats<D, R> + 2 * r]);
-                for (int s = s0; s < s1; ++s) {
-                    if (!part[s].used)
-                        continue;
-                    const float *const from = parts + s * kPartFloats<D, R>;
-                    const float h = ex2(from[2 * r] - m);
-                    const float4 x = *reinterpret_cast<const float4 *>(from + 2 * R + r * (D + 4) + 4 * c);
-                    l += from[2 * r + 1] * h;
-                    o.x += x.x * h, o.y += x.y * h, o.z += x.z * h, o.w += x.w * h;
-                }
-                if (whole) {
-                    const float by = 1.f / l;
-                    uint2 y = make_uint2(narrow<T>(within<T>(o.x * by), within<T>(o.y * by)),
-                                         narrow<T>(within<T>(o.z * by), within<T>(o.w * by)));
-                    *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + rows.b * p.o_stride +
-                                               (int64_t)(rows.head + r) * D + 4 * c) = y;
-                    if (c == 0 && p.lse != nullptr)
-                        p.lse[(int64_t)rows.b * p.n_heads + rows.head + r] = 0.6931471805599453f * (m + log2f(l));
-                } else {
-                    *reinterpret_cast<float4 *>(left + 2 * R + r * (D + 4) + 4 * c) = o;
-                    if (c == 0) {
-                        left[2 * r] = m;
-                        left[2 * r + 1] = l;
+            float *const to = p.part + parts_at(gridDim.x) + (int64_t)(2 * blockIdx.x + starts) * kPart;
+            *reinterpret_cast<float4 *>(to + 2 * R + r * (D + 4) + col) = o;
+            if (lane == 0) {
+                to[2 * r] = m;
+                to[2 * r + 1] = l;
+            }
+        }
+        if (!p.unsplit) {
+            if (threadIdx.x == 0) {
+                // the item that goes on in the next block
+                Split x{-1, 0};
+                if (chains > 0) {
+                    const Part a = part[order[firsts[chains - 1]]], z = part[order[count - 1]];
+                    if (a.starts && !z.ends) {
+                        const int bb = plan.by_items.div(a.item), per = units_of(all.len[bb]);
+                        const int last = all.before[bb] + (a.item - bb * plan.items + 1) * per - 1;
+                        x.item = a.item;
+                        x.last = shares.of(last);
                     }
                 }
+                reinterpret_cast<Split *>(p.part)[blockIdx.x] = x;
             }
-            s0 = s1;
-        }
-        if (!p.unsplit)
             return;
+        }
         __syncthreads();
     }
 }
 
-// The parts that several blocks left of an item: a block for each item and kJoinWarps / per_row rows, per_row warps to
-// a row, a lane for D / 32 columns.
+// The parts that several blocks left of an item: the block x in which the item begins, kJoinWarps / per_row rows, per_row
+// warps to a row.
 constexpr int kJoinWarps = 8;
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kJoinWarps * 32)
-kv8_join_kernel(const __grid_constant__ AttnParams p, int per_row)
+kv8_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Kv8Plan plan)
 {
-    constexpr int R = 8 * NT, E = D / 32, kAhead = 8;
-    __shared__ Lengths all;
-    __shared__ float got[kJoinWarps][D + 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Shape shape(p, R);
-    // the lengths may be read before the wait: the kernel in front, which has waited itself, only
-    // reads them
-    read_lengths(all, p.kv_len, p.batch, p.max_kv, nullptr,
-                 [&](int len) { return Shape::units(len) * shape.per_request; });
-    const int b = blockIdx.x / shape.per_request, item = blockIdx.x - b * shape.per_request;
-    const int units = all.before[p.batch], own = Shape::units(all.len[b]);
-    const int u = all.before[b] + item * own;
-    const int c0 = all.len[b] < 0 ? 0 : attn::cta_of(units, p.ctas, u);
-    const int c1 = all.len[b] < 0 ? 0 : attn::cta_of(units, p.ctas, u + own - 1);
+    constexpr int R = 8 * NT, kPart = kPartFloats<D, R>, kAhead = 4;
+    __shared__ float4 sums[kJoinWarps][32];
+    __shared__ float2 pairs[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_row = plan.per_row;
+    const int r = blockIdx.y * (kJoinWarps / per_row) + warp / per_row, first = warp % per_row;
+    const int col = lane * 4 % D;
     pdl_wait_and_release();
-    if (c0 == c1)
+    const Split x = reinterpret_cast<const Split *>(p.part)[blockIdx.x];
+    if (x.item < 0)
         return;
-    const Rows<R> rows(p, shape, b, item);
-    const int some = kJoinWarps / per_row, r = blockIdx.y * some + warp / per_row, first = warp % per_row;
-    const bool on = r < rows.n;
-    float m = -INFINITY, l = 0.f, o[E];
+    const int b = plan.by_items.div(x.item);
+    const Rows<R> rows(p, plan, b, x.item - b * plan.items);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    // up to 32 parts at a time, the sums of the first ones on their way with the pairs
+    for (int c0 = blockIdx.x + first; r < rows.n && c0 <= x.last; c0 += 32 * per_row) {
+        auto at = [&](int i) {
+            const int c = c0 + i * per_row;
+            return p.part + parts_at(plan.ctas) + (int64_t)(c == (int)blockIdx.x ? 2 * c + 1 : 2 * c) * kPart;
+        };
+        auto row = [&](int i) { return *reinterpret_cast<const float4 *>(at(i) + 2 * R + r * (D + 4) + col); };
+        const int count = min(32, (x.last - c0) / per_row + 1);
+        float4 ahead[kAhead];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        o[e] = 0.f;
-    // up to 32 parts at a time: a lane reads one's m and l, all lanes its columns
-    for (int i0 = first; on && i0 < c1 - c0 + 1; i0 += 32 * per_row) {
-        const int c = c0 + i0 + lane * per_row;
-        const bool here = c <= c1 && attn::has_units(units, p.ctas, c);
-        const float *const from = p.part + (int64_t)(c == c0 ? 2 * c + 1 : 2 * c) * kPartFloats<D, R>;
+        for (int i = 0; i < kAhead; ++i)
+            ahead[i] = row(min(i, count - 1));
         float pm = -INFINITY, pl = 0.f;
-        if (here) {
-            pm = from[2 * r];
-            pl = from[2 * r + 1];
+        if (lane < count) {
+            pm = at(lane)[2 * r];
+            pl = at(lane)[2 * r + 1];
         }
-        const unsigned there = __ballot_sync(0xffffffffu, here);
-        float top = pm;
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1)
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        top = fmaxf(top, m);
-        const float h = here ? ex2(pm - top) : 0.f, h0 = m == -INFINITY ? 0.f : ex2(m - top);
-        float sum = pl * h;
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1)
-            sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        l = l * h0 + sum;
+        const float4 y = join<kAhead>(pm, pl, count, [&](int i, int k) { return i < kAhead ? ahead[k] : row(i); });
+        const float top = fmaxf(m, pm), h = m == -INFINITY ? 0.f : ex2(m - top),
+                    hy = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - top);
+        o.x = o.x * h + y.x * hy, o.y = o.y * h + y.y * hy, o.z = o.z * h + y.z * hy, o.w = o.w * h + y.w * hy;
+        l = l * h + pl * hy;
         m = top;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            o[e] *= h0;
-        const int count = 32 - __clz(there);
-        for (int j0 = 0; j0 < count; j0 += kAhead) {
-            float x[kAhead][E];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const uint64_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, (j0 + j) & 31);
-                const float *const y = reinterpret_cast<const float *>(at) + 2 * R + r * (D + 4) + lane * E;
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    x[j][e] = (there >> ((j0 + j) & 31)) & 1 ? y[e] : 0.f;
-            }
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                const float hj = __shfl_sync(0xffffffffu, h, (j0 + j) & 31);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    o[e] = fmaf(x[j][e], hj, o[e]);
-            }
-        }
     }
     if (per_row > 1) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            got[warp][lane * E + e] = o[e];
-        if (lane == 0) {
-            got[warp][D] = m;
-            got[warp][D + 1] = l;
-        }
+        sums[warp][lane] = o;
+        if (lane == 0)
+            pairs[warp] = make_float2(m, l);
         __syncthreads();
         if (first != 0)
             return;
-        for (int x = 1; x < per_row; ++x)
-            m = fmaxf(m, got[warp + x][D]);
-        l = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            o[e] = 0.f;
-        for (int x = 0; x < per_row; ++x) {
-            if (got[warp + x][D] == -INFINITY)
-                continue;
-            const float h = ex2(got[warp + x][D] - m);
-            l += got[warp + x][D + 1] * h;
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                o[e] = fmaf(got[warp + x][lane * E + e], h, o[e]);
-        }
+        const float2 z = lane < per_row ? pairs[warp + lane] : make_float2(-INFINITY, 0.f);
+        m = z.x;
+        l = z.y;
+        o = join<2>(m, l, per_row, [&](int i, int) { return sums[warp + i][lane]; });
     }
-    if (!on)
-        return;
-    const float by = 1.f / l;
-    T *const to = static_cast<T *>(p.o) + rows.b * p.o_stride + (int64_t)(rows.head + r) * D + lane * E;
-#pragma unroll
-    for (int e = 0; e < E; e += 2)
-        reinterpret_cast<uint32_t *>(to)[e / 2] = narrow<T>(within<T>(o[e] * by), within<T>(o[e + 1] * by));
-    if (lane == 0 && p.lse != nullptr)
-        p.lse[(int64_t)rows.b * p.n_heads + rows.head + r] = 0.6931471805599453f * (m + log2f(l));
+    if (r < rows.n && lane * 4 < D)
+        write_row<T, D>(p, b, rows.head + r, col, o, m, l);
+}
+
+// The cache as rows of 128 bytes: a copy takes a group of one head's plane, which lands in swizzled rows (16-byte chunk c
+// of row r at c ^ (r & 7)), so that a warp reads the products' operands without bank conflicts.
+template <int D>
+bool encode(CUtensorMap *m, const Kv8Cache &cache)
+{
+    auto fn = attn::encode_fn();
+    if (fn == nullptr)
+        return false;
+    cuuint64_t dim[2] = {128, (cuuint64_t)(cache.num_blocks * (cache.block_bytes / 128))};
+    cuuint64_t stride[1] = {128};
+    cuuint32_t box[2] = {128, kGroup * D / 128}, one[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, cache.base, dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename T, int D, int NT>
-cudaError_t launch(const AttnParams &p, const Kv8Cache &cache, cudaStream_t s)
+cudaError_t launch(const AttnParams &p, const Kv8Plan &plan, const Kv8Cache &cache, cudaStream_t s)
 {
+    using S = Sizes<D, NT>;
     static std::atomic<uint64_t> done{0};
-    const size_t smem = 2 * kWarps * kPartFloats<D, 8 * NT> * sizeof(float);
-    cudaError_t e = launch_pdl_big_smem(kv8_decode_kernel<T, D, NT>, dim3((unsigned)p.ctas), dim3(kThreads), smem, s,
-                                        done, p, cache);
+    CUtensorMap map;
+    if (!encode<D>(&map, cache))
+        return cudaErrorInvalidValue;
+    const cudaError_t e = launch_pdl_smem_limit(kv8_decode_kernel<T, D, NT>, dim3((unsigned)plan.ctas),
+                                                dim3((unsigned)plan.warps * 32), S::smem(plan.warps), S::smem(S::kWarps),
+                                                s, done, p, plan, cache, map);
     if (e != cudaSuccess || !p.joined)
         return e;
-    int per_row = 1;
-    while (per_row < kJoinWarps && per_row * 8 < p.parts)
-        per_row *= 2;
-    const int rows = p.group < 8 * NT ? p.group : 8 * NT;
-    const dim3 grid((unsigned)(p.batch * Shape(p, 8 * NT).per_request), (unsigned)((rows * per_row + kJoinWarps - 1) / kJoinWarps));
-    return launch_pdl(kv8_join_kernel<T, D, NT>, grid, dim3(kJoinWarps * 32), 0, s, p, per_row);
+    const int rows = p.group < S::R ? p.group : S::R;
+    return launch_pdl(kv8_join_kernel<T, D, NT>,
+                      dim3((unsigned)plan.ctas, (unsigned)((rows * plan.per_row + kJoinWarps - 1) / kJoinWarps)),
+                      dim3(kJoinWarps * 32), 0, s, p, plan);
 }
 
 template <typename T>
-cudaError_t launch(const AttnParams &p, const Kv8Cache &cache, int d, cudaStream_t s)
+cudaError_t launch(const AttnParams &p, const Kv8Plan &plan, const Kv8Cache &cache, int d, cudaStream_t s)
 {
     if (p.group > 8)
-        return d == 128 ? launch<T, 128, 2>(p, cache, s) : launch<T, 64, 2>(p, cache, s);
-    return d == 128 ? launch<T, 128, 1>(p, cache, s) : launch<T, 64, 1>(p, cache, s);
+        return d == 128 ? launch<T, 128, 2>(p, plan, cache, s) : launch<T, 64, 2>(p, plan, cache, s);
+    return d == 128 ? launch<T, 128, 1>(p, plan, cache, s) : launch<T, 64, 1>(p, plan, cache, s);
+}
+
+template <int D, int NT>
+int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
+{
+    using S = Sizes<D, NT>;
+    plan.row_tiles = (p.group + S::R - 1) / S::R;
+    plan.items = plan.row_tiles * p.n_kv;
+    const int64_t items = (int64_t)p.batch * plan.items, longest = units_of(p.max_kv);
+    if (items * longest > INT_MAX)
+        return -1;
+    // whole items: as many warps to each as the SMs have for it, and as it has steps
+    const int64_t rounds = (items + sm_count - 1) / sm_count, steps = (longest + S::kTiles - 1) / S::kTiles;
+    int64_t warps = rounds < S::kWarps ? S::kWarps / rounds : 1;
+    if (warps > steps)
+        warps = steps;
+    if (p.unsplit)
+        warps = S::kWarps;
+    else if (longest <= kWholeTiles * warps)
+        p.unsplit = 1;
+    p.joined = !p.unsplit;
+    if (p.unsplit) {
+        const int64_t most = sm_count * (S::kWarps / warps);
+        plan.ctas = (int)(items < most ? items : most);
+    } else {
+        // a block to each SM, with a warp to each step where there are few
+        const int64_t all = items * steps;
+        plan.ctas = (int)(all < sm_count ? all : sm_count);
+        warps = (all + sm_count - 1) / sm_count;
+        if (warps > S::kWarps)
+            warps = S::kWarps;
+    }
+    plan.warps = (int)warps;
+    // about two parts to a warp of the join
+    const int64_t parts = longest / (items * longest / plan.ctas > 0 ? items * longest / plan.ctas : 1) + 1;
+    plan.per_row = 1;
+    while (plan.per_row < kJoinWarps && plan.per_row * 2 < parts)
+        plan.per_row *= 2;
+    plan.by_row_tiles.set(plan.row_tiles);
+    plan.by_items.set(plan.items);
+    plan.by_warps.set(plan.warps);
+    plan.by_ctas.set(plan.ctas);
+    // two parts of a block, one of each warp
+    return p.unsplit ? 0 : (int64_t)sizeof(float) * (parts_at(plan.ctas) + (2 + warps) * plan.ctas * kPartFloats<D, S::R>);
 }
 
 }  // namespace
 }  // namespace kv8
 
-int64_t plan_kv8_decode(AttnParams &p, int d, int sm_count)
+int64_t plan_kv8_decode(AttnParams &p, Kv8Plan &plan, int d, int sm_count)
 {
-    using namespace kv8;
-    const int rows = p.group > 8 ? 16 : 8;
-    const Shape shape(p, rows);
-    const int64_t items = (int64_t)p.batch * shape.per_request, longest = Shape::units(p.max_kv);
-    if (items * longest > INT_MAX)
-        return -1;
-    int most = sm_count * (rows == 8 ? 2 : 1);
-    if (most > kAttnMaxCtas)
-        most = kAttnMaxCtas;
-    // a tile to a warp
-    int64_t ctas = (items * longest + kWarps - 1) / kWarps;
-    ctas = ctas < most ? ctas : most;
-    if (longest <= 4 * kWarps)
-        p.unsplit = 1;
-    p.joined = !p.unsplit;
-    if (p.unsplit)
-        ctas = items < most ? items : most;
-    p.ctas = (int)ctas;
-    p.parts = (int)(longest / (items * longest / ctas > 0 ? items * longest / ctas : 1)) + 2;
-    const int64_t part = sizeof(float) * (2 * rows + rows * (d + 4));
-    return p.joined ? 2 * ctas * part : 0;
+    p.limit_ns = 1000000000ull;
+    if (p.group > 8)
+        return d == 128 ? kv8::make_plan<128, 2>(p, plan, sm_count) : kv8::make_plan<64, 2>(p, plan, sm_count);
+    return d == 128 ? kv8::make_plan<128, 1>(p, plan, sm_count) : kv8::make_plan<64, 1>(p, plan, sm_count);
 }
 
-cudaError_t launch_kv8_decode(const AttnParams &p, const Kv8Cache &cache, int d, int dtype, cudaStream_t s)
+cudaError_t launch_kv8_decode(const AttnParams &p, const Kv8Plan &plan, const Kv8Cache &cache, int d, int dtype,
+                              cudaStream_t s)
 {
-    return dtype == HS_FP16 ? kv8::launch<__half>(p, cache, d, s) : kv8::launch<__nv_bfloat16>(p, cache, d, s);
+    return dtype == HS_FP16 ? kv8::launch<__half>(p, plan, cache, d, s) : kv8::launch<__nv_bfloat16>(p, plan, cache, d, s);
 }
 
 }  // namespace hs

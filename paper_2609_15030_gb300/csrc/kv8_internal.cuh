@@ -38,6 +38,15 @@ struct Kv8Cache {
     int32_t page_shift;
 };
 
+// how a decode step is shared out
+struct Kv8Plan {
+    int32_t row_tiles;            // of a KV head's query rows
+    int32_t items;                // of a request: row tiles of its KV heads
+    int32_t warps, ctas;          // to a block; blocks
+    int32_t per_row;              // warps that join a row
+    Divisor by_row_tiles, by_items, by_warps, by_ctas;
+};
+
 struct Kv8Append {
     Kv8Cache cache;
     const uint4 *q, *k, *v;       // q: nullptr without positions
@@ -68,8 +77,8 @@ cudaError_t launch_kv8_append(Kv8Append a, const RopeParams *rope, int d, int dt
                               cudaStream_t s);
 cudaError_t launch_kv8_read(const Kv8Read &r, int d, int dtype, int sm_count, cudaStream_t s);
 // Fill in the schedule and say how many bytes of workspace it takes; -1: more units than 31 bits count.
-int64_t plan_kv8_decode(AttnParams &p, int d, int sm_count);
-cudaError_t launch_kv8_decode(const AttnParams &p, const Kv8Cache &cache, int d, int dtype,
+int64_t plan_kv8_decode(AttnParams &p, Kv8Plan &plan, int d, int sm_count);
+cudaError_t launch_kv8_decode(const AttnParams &p, const Kv8Plan &plan, const Kv8Cache &cache, int d, int dtype,
                               cudaStream_t s);
 
 namespace kv8 {
@@ -105,12 +114,16 @@ __device__ __forceinline__ uint32_t narrow(float lo, float hi)
     return x;
 }
 
-// x within the finite values of T; NaN stays
+// the same kept within the finite values of T; NaN stays
 template <typename T>
-__device__ __forceinline__ float within(float x)
+__device__ __forceinline__ uint32_t narrow_finite(float lo, float hi)
 {
-    const float top = std::is_same<T, __half>::value ? 65504.f : 3.3895313892515355e38f;
-    return x != x ? x : fminf(fmaxf(x, -top), top);
+    uint32_t x;
+    if constexpr (std::is_same<T, __half>::value)
+        asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(hi), "f"(lo));
+    return x;
 }
 
 // two E4M3 numbers (the low 16 bits of x) as binary16, exact

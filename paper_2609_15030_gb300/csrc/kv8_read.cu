@@ -68,7 +68,7 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
                     continue;
                 auto pair = [&](uint32_t f16) {
                     const float2 f = widen<__half>(f16);
-                    return narrow<T>(within<T>(f.x * scale[i]), within<T>(f.y * scale[i]));
+                    return narrow_finite<T>(f.x * scale[i], f.y * scale[i]);
                 };
                 const uint4 y = make_uint4(pair(e4m3_to_f16(x[i].x)), pair(e4m3_to_f16_high(x[i].x)),
                                            pair(e4m3_to_f16(x[i].y)), pair(e4m3_to_f16_high(x[i].y)));

@@ -18,34 +18,32 @@ template <typename Units>
 __device__ __forceinline__ void read_lengths(Lengths &all, const int32_t *kv_len, int batch, int max_kv,
                                              int32_t *d_err, Units units)
 {
-    constexpr int kAhead = HS_MAX_BATCH / 32;      // loads that do not wait for one another
+    constexpr int kAhead = 4;                      // loads that do not wait for one another
     if (threadIdx.x < 32) {
         const int lane = threadIdx.x;
-        int n[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            n[i] = i * 32 + lane < batch ? kv_len[i * 32 + lane] : 0;
         int sum = 0;
+#pragma unroll 1
+        for (int b0 = 0; b0 < batch; b0 += 32 * kAhead) {
+            int n[kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int b = i * 32 + lane;
-            if (i * 32 >= batch)
-                break;
-            int x = 0;
-            if (b < batch) {
-                if (n[i] < 0 || n[i] > max_kv) {
-                    if (blockIdx.x == 0)
-                        report(d_err, HS_DEVERR_LENGTH);
-                    n[i] = -1;
-                } else {
-                    x = units(n[i]);
+            for (int i = 0; i < kAhead; ++i)
+                n[i] = b0 + i * 32 + lane < batch ? kv_len[b0 + i * 32 + lane] : -1;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int b = b0 + i * 32 + lane;
+                const bool fine = n[i] >= 0 && n[i] <= max_kv;
+                if (!fine && b < batch && blockIdx.x == 0)
+                    report(d_err, HS_DEVERR_LENGTH);
+                const int x = fine ? units(n[i]) : 0;
+                const int incl = attn::warp_scan(x, lane);
+                if (b < batch) {
+                    all.len[b] = fine ? n[i] : -1;
+                    all.before[b] = sum + incl - x;
                 }
-                all.len[b] = n[i];
+                sum += __shfl_sync(0xffffffffu, incl, 31);
+                if (b0 + i * 32 + 32 >= batch)
+                    break;
             }
-            const int incl = attn::warp_scan(x, lane);
-            if (b < batch)
-                all.before[b] = sum + incl - x;
-            sum += __shfl_sync(0xffffffffu, incl, 31);
         }
         if (lane == 0)
             all.before[batch] = sum;
@@ -66,6 +64,22 @@ __device__ __forceinline__ int request_of(const Lengths &all, int batch, int u, 
     }
     return b;
 }
+
+// Units shared out evenly, the first shares with one more where that does not go up: the first unit of share i, and the
+// share with unit u.
+struct Shares {
+    int each, more;
+    // n units over by.d shares, or over n where these are fewer
+    __device__ __forceinline__ Shares(int n, const Divisor &by) : each(by.div(n)), more(n - each * by.d) {}
+    __device__ __forceinline__ int begin(int i) const
+    {
+        return i * each + min(i, more);
+    }
+    __device__ __forceinline__ int of(int u) const
+    {
+        return u < more * (each + 1) ? u / (each + 1) : more + (u - more * (each + 1)) / each;
+    }
+};
 
 __host__ __device__ __forceinline__ int groups_of(int len)
 {
