@@ -95,7 +95,7 @@ hs_status hs_rope_plan(int32_t dims, int32_t layout, double base, int32_t scalin
  * Arithmetic: sine and cosine, products and sums in float32, rounded once to the element type.
  * Pointers 16-byte aligned (pos: 8).
  * Errors: HS_ERR_INVALID_ARG, HS_ERR_MISALIGNED, HS_ERR_UNSUPPORTED (head_dim, n_kv_heads > 1024,
- * n_heads / n_kv_heads > 128), HS_ERR_CUDA.
+ * n_heads / n_kv_heads > 128, 2^31 rows), HS_ERR_CUDA.
  */
 hs_status hs_rope_apply(const hs_attn_shape *shp, const hs_rope *rope, const void *q, const void *k,
                         int64_t in_stride, const int64_t *pos, int64_t n_rows, void *q_out,
@@ -144,8 +144,8 @@ hs_status hs_kv8_append(const hs_attn_shape *shp, const void *k, const void *v, 
  * hs_kv8_append_rope -- hs_rope_apply of q into q_out and hs_kv8_append of the turned k, and of v, in one
  * launch.
  *
- * k's turned values are quantised as they are (float32, not rounded to the element type in between); a largest
- * magnitude within 2^-20 of a power of two times 448 is decided in float64.  Rows with a negative slot
+ * k's turned values are not rounded to the element type in between: scales and bytes are those of the exactly turned
+ * keys (what float32 leaves open is decided in float64).  Rows with a negative slot
  * are skipped altogether: their row of q_out is not written.  A row whose slot is out of range is turned into q_out.
  *   in_stride  elements between rows of q, k and v, a multiple of 8; 0: each one's own heads * head_dim
  *   q_out      as hs_rope_apply (in place is fine); q and q_out may both be NULL

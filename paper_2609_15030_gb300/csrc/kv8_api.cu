@@ -255,6 +255,8 @@ hs_status hs_rope_apply(const hs_attn_shape *shp, const hs_rope *rope, const voi
         st = check_stride(k_out_stride, k_inner);
     if (st != HS_OK || n_rows == 0)
         return st;
+    if (n_rows > INT32_MAX)
+        return HS_ERR_UNSUPPORTED;
     if (pos == nullptr)
         return HS_ERR_INVALID_ARG;
     if (misaligned(q, 16) || misaligned(k, 16) || misaligned(q_out, 16) || misaligned(k_out, 16) ||

@@ -7,10 +7,18 @@
 // both divisions are exact, so each value is rounded once for each scale that it lives under.
 //
 // The rows of a group stand one behind the other: its first row's place (the row in front has another group)
-// says who owns it.  A block takes a window of rows and the groups that begin in it; a warp takes one (KV
-// head, plane) of these groups one after the other, 16 rows in registers (D / 16 lanes to a row,
-// two 16-byte vectors each), so that M and the bytes come from one read.  Sines and cosines of the
-// block's rows are computed once, in shared memory, for all heads.
+// says who owns it.  Values and keys that are not turned are taken by warps, a (KV head, plane) of a group at a time with its
+// 16 rows in registers, so that M and the bytes come from one read.  Keys that are turned are taken by teams of D threads, a
+// lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
+//
+// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 31.0 us, 5.7 TB/s; with
+// positions and 32 heads of q, 22,647 rows 90 us, 5.7 TB/s; 14,494 rows of 16 + 4 heads 33.8 us, 4.8.  A step of 64 rows
+// with positions takes 5.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
+//
+// Turned values are good to 2^-21 of |x| + |y|: the angle is good to 2^-25 half turns, sines and cosines to 2^-24, and four
+// more roundings follow (sum 2^-21.3).  What lies nearer than that to a border, of two scales or of two E4M3 numbers, is
+// decided by its float64 value, so that the bytes are those of the exactly turned keys.
+#include "attn_ptx.cuh"
 #include "kv8_internal.cuh"
 
 namespace hs {
@@ -18,268 +26,495 @@ namespace {
 
 using namespace kv8;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kWindow = 16;                        // rows of a window at most
-constexpr int kRows = 2 * kWindow - 1;             // rows that a window's groups may reach
+constexpr int kThreads = 128;
+constexpr float kOff = 0x1p-21f;
 
-// The largest magnitude of the turned keys of a lane's rows in float64, for one that lies next to a border between two scales.
-template <typename T, int D, bool kHalf>
-__device__ __noinline__ double largest_exact(const RopeParams &rope, const int64_t *pos, const uint4 *k,
-                                             int64_t stride, int n, int v, int sub)
+// The turned pair (x, y) exactly (float64): what lies next to a border of rounding is decided by it.
+__device__ __noinline__ double2 turned_exactly(uint64_t turns, int64_t pos, double amplitude, float x, float y)
 {
-    double top = 0.0;
-    int a, b;
-    lane_vectors(v, rope.pairs, kHalf, a, b);
-    for (int i = sub; i < n; i += 512 / D) {
-        float x[8], y[8];
-        pairs_of<T>(k[i * stride + a], k[i * stride + b], kHalf, x, y);
-#pragma unroll 1
-        for (int j = 0; j < 8; ++j) {
-            double s = 0.0, c = 1.0;
-            if (v < rope.pairs / 8) {
-                sincospi((double)angle_of(rope.turns[8 * v + j], pos[i]) * 0x1p-63, &s, &c);
-                s *= rope.amplitude;
-                c *= rope.amplitude;
-            }
-            top = fmax(top, fmax(fabs(x[j] * c - y[j] * s), fabs(y[j] * c + x[j] * s)));
-        }
-    }
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1)
-        top = fmax(top, __shfl_xor_sync(0xffffffffu, top, w));
-    return top;
+    double s, c;
+    sincospi((double)angle_of(turns, pos) * 0x1p-63, &s, &c);
+    return make_double2(amplitude * (x * c - y * s), amplitude * (y * c + x * s));
 }
 
-template <typename T, int D, bool kRope, bool kHalf>
-__global__ void __launch_bounds__(kThreads)
-kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ RopeParams rope)
+// a double as a float that E4M3 rounds to the same number: nearest, but never onto a midpoint that it is not
+__device__ __forceinline__ float toward(double x)
 {
-    constexpr int kLanes = D / 16;                 // lanes to a row
-    constexpr int kAtOnce = 32 / kLanes;           // rows of a warp at a time
-    constexpr int kSteps = kGroup / kAtOnce;
-    __shared__ float2 spins[kRope ? kRows : 1][D / 2];
-    pdl_wait_and_release();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int v = lane % kLanes, sub = lane / kLanes;
-    const int64_t r0 = (int64_t)blockIdx.x * p.window;
+    const float f = (float)x;
+    if ((__float_as_uint(f) & 0x7ffff) == 0 && (double)f != x)
+        return __uint_as_float(__float_as_uint(f) + ((double)fabsf(f) < fabs(x) ? 1 : -1));
+    return f;
+}
 
-    // lane l: the slot and group of row r0 - 1 + l; the rows where a group of this window begins
-    const int64_t mine = r0 - 1 + lane;
-    const int64_t slot = mine >= 0 && mine < p.n_rows ? __ldg(p.slots + mine) : -1;
-    const bool far = slot >= p.cache.num_blocks << p.cache.page_shift;
-    if (far && warp == 0 && blockIdx.y == 0 && lane > 0)
-        report(p.d_err, HS_DEVERR_BLOCK_OOB);
-    const int64_t group = slot < 0 || far ? -1 : slot / kGroup;
-    const int64_t before = __shfl_up_sync(0xffffffffu, group, 1);
-    const unsigned begins = __ballot_sync(0xffffffffu, lane >= 1 && lane <= p.window && group >= 0 &&
-                                                           group != before);
-    // rows of the group that begins with lane l's row
-    auto rows_from = [&](int l) {
+// 448 2^e is 1.75 2^(e + 8): the e of the smallest 2^e >= x / 448, for the bits of a float x > 0
+__device__ __forceinline__ int exponent_of(uint32_t bits)
+{
+    return (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+}
+
+// eight pairs as the bytes of a lane's vectors: words 0 and 1 of the first, 2 and 3 of the second
+template <bool kHalf>
+__device__ __forceinline__ void bytes_of(const Pairs &p, uint32_t (&w)[4])
+{
+    float2 x[4], y[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[k] = ptx::unpair(p.x[k]);
+        y[k] = ptx::unpair(p.y[k]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (kHalf) {
+            w[i] = to_e4m3(x[2 * i].x, x[2 * i].y, x[2 * i + 1].x, x[2 * i + 1].y);
+            w[i + 2] = to_e4m3(y[2 * i].x, y[2 * i].y, y[2 * i + 1].x, y[2 * i + 1].y);
+        } else {
+            w[2 * i] = to_e4m3(x[2 * i].x, y[2 * i].x, x[2 * i].y, y[2 * i].y);
+            w[2 * i + 1] = to_e4m3(x[2 * i + 1].x, y[2 * i + 1].x, x[2 * i + 1].y, y[2 * i + 1].y);
+        }
+    }
+}
+
+// where the byte of x (or y) of pair j lies
+template <bool kHalf>
+__device__ __forceinline__ int byte_of(int j, int y)
+{
+    return kHalf ? j + 8 * y : 2 * j + y;
+}
+
+// what a warp needs of the group whose rows it quantises
+struct Group {
+    uint8_t *at;                  // its first token's bytes of the KV head's plane
+    float *scale_at;
+    float old;
+    unsigned tokens;              // that get rows
+    int n, spot;                  // rows; lane i: the token of row i
+};
+
+// Settles the group's scale, rounds what it holds to it where it grows, and gives the scale.
+template <int D>
+__device__ __forceinline__ float settle(const Group &g, int e, int lane)
+{
+    constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes;
+    const float need = power_of_two(e < -126 ? -126 : e);
+    const bool anew = g.tokens & 1;
+    const float scale = anew ? need : fmaxf(g.old, need);
+    if (!anew && need > g.old) {
+        // 16 bytes to a lane
+        const float shrink = g.old / need;
+#pragma unroll 1
+        for (int i = lane / kLanes; i < kGroup; i += kAtOnce) {
+            if ((g.tokens >> i) & 1)
+                continue;
+            uint4 *const w = reinterpret_cast<uint4 *>(g.at + i * D) + lane % kLanes;
+            const uint4 y = *w;
+            auto again = [&](uint32_t u) {
+                const float2 f = widen<__half>(e4m3_to_f16(u)), h = widen<__half>(e4m3_to_f16_high(u));
+                return to_e4m3(f.x * shrink, f.y * shrink, h.x * shrink, h.y * shrink);
+            };
+            *w = make_uint4(again(y.x), again(y.y), again(y.z), again(y.w));
+        }
+    }
+    if (lane == 0)
+        *g.scale_at = scale;
+    return scale;
+}
+
+// Rows of values that are quantised as they are: row i of the group at from + i * stride.
+template <typename T, int D>
+__device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int64_t stride, int lane)
+{
+    constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes, kSteps = kGroup / kAtOnce;
+    constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0x7c00 : 0x7f80;
+    const int v = lane % kLanes, sub = lane / kLanes;
+    uint4 in[kSteps][2];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int i = s * kAtOnce + sub;
+        in[s][0] = in[s][1] = make_uint4(0, 0, 0, 0);
+        if (i < g.n) {
+            in[s][0] = __ldcs(from + i * stride + v);
+            in[s][1] = __ldcs(from + i * stride + v + kLanes);
+        }
+    }
+    // the largest of the magnitudes' bits
+    uint32_t top = 0;
+    auto most = [&](uint32_t x) { asm("max.u16x2 %0, %0, %1;" : "+r"(top) : "r"(x & 0x7fff7fffu)); };
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            most(in[s][h].x), most(in[s][h].y), most(in[s][h].z), most(in[s][h].w);
+        }
+    top = __reduce_max_sync(0xffffffffu, max(top & 0xffff, top >> 16));
+    const bool odd = top >= kInf;                      // a value that is not finite
+    if (odd) {
+        top = 0;
+        auto finite = [&](uint32_t x) { top = (x & 0x7fff) < kInf ? max(top, x & 0x7fff) : top; };
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t u[4] = {in[s][h].x, in[s][h].y, in[s][h].z, in[s][h].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    finite(u[j]), finite(u[j] >> 16);
+            }
+        top = __reduce_max_sync(0xffffffffu, top);
+    }
+    const float by = 1.f / settle<D>(g, exponent_of(__float_as_uint(widen<T>(top).x)), lane);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const int i = s * kAtOnce + sub, token = __shfl_sync(0xffffffffu, g.spot, i);
+        if (i >= g.n)
+            continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t u[4] = {in[s][h].x, in[s][h].y, in[s][h].z, in[s][h].w};
+            uint32_t y[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float2 a = widen<T>(u[2 * j]), b = widen<T>(u[2 * j + 1]);
+                if (odd) {                             // an infinity becomes NaN
+                    a.x += 0.f * a.x, a.y += 0.f * a.y;
+                    b.x += 0.f * b.x, b.y += 0.f * b.y;
+                }
+                y[j] = to_e4m3(a.x * by, a.y * by, b.x * by, b.y * by);
+            }
+            *reinterpret_cast<uint2 *>(g.at + token * D + 8 * (v + h * kLanes)) = make_uint2(y[0], y[1]);
+        }
+    }
+}
+
+// The groups that begin in a window of rows: lane l of each warp has the slot and the group of row `first` + l.
+struct Window {
+    int64_t first, slot, group;
+    unsigned begins;              // lanes whose row begins a group
+    __device__ __forceinline__ Window(const Kv8Append &p, int64_t row, bool complain, int lane) : first(row - 1)
+    {
+        const int64_t mine = first + lane;
+        slot = mine >= 0 && mine < p.n_rows ? __ldg(p.slots + mine) : -1;
+        const bool far = slot >= p.cache.num_blocks << p.cache.page_shift;
+        if (far && complain && lane > 0 && lane <= p.window)
+            report(p.d_err, HS_DEVERR_BLOCK_OOB);
+        group = slot < 0 || far ? -1 : slot / kGroup;
+        const int64_t before = __shfl_up_sync(0xffffffffu, group, 1);
+        begins = __ballot_sync(0xffffffffu, lane >= 1 && lane <= p.window && group >= 0 && group != before);
+    }
+    // rows of the group that begins with lane l's
+    __device__ __forceinline__ int rows(int l) const
+    {
         const unsigned other = ~(__ballot_sync(0xffffffffu, group == __shfl_sync(0xffffffffu, group, l)) >> l);
         const int n = __ffs(other) - 1;
         return n < 0 || n > kGroup ? kGroup : n;
-    };
+    }
+};
 
-    if constexpr (kRope) {
-        int rows = p.window;
-        if (begins != 0) {
-            const int last = 31 - __clz(begins), end = last - 1 + rows_from(last);
-            rows = end > rows ? end : rows;
-        }
-        if (r0 + rows > p.n_rows)
-            rows = (int)(p.n_rows - r0);
-        for (int i = threadIdx.x; i < rows * rope.pairs; i += kThreads) {
-            const int r = i / rope.pairs, j = i - r * rope.pairs;
-            spins[r][j] = spin_of(angle_of(rope.turns[j], __ldg(p.pos + r0 + r)), (float)rope.amplitude);
-        }
-        __syncthreads();
+// Keys that are turned.  A team of D threads takes a group, a lane 16 values of one row, so that a lane keeps its pairs'
+// sines and cosines, and the turned values, while it goes through the heads with the next one's rows on their way.
+template <typename T, int D, bool kHalf>
+struct Team {
+    static constexpr int kLanes = D / 16, kSize = kGroup * kLanes, kCount = kThreads / kSize, kWarps = kSize / 32;
+    const Kv8Append &p;
+    const RopeParams &rope;
+    uint32_t (*const tops)[kWarps];      // [2] in shared memory: the warps' maxima
+    const int team, lane, warp, i, v;    // warp of the team; the lane's row of the group, and its place there
+    int turn = 0;                        // tops that the next maximum goes to
+
+    __device__ __forceinline__ void meet() const
+    {
+        asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(kSize) : "memory");
+    }
+    // the largest x of all lanes
+    __device__ __forceinline__ uint32_t largest(uint32_t x)
+    {
+        x = __reduce_max_sync(0xffffffffu, x);
+        if (lane == 0)
+            tops[turn][warp] = x;
+        meet();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            x = max(x, tops[turn][w]);
+        turn ^= 1;                       // the next one's writers have met again before they come back to these
+        return x;
     }
 
-    // K and V
-    const bool turned = kRope && v < rope.pairs / 8;
-    for (int job = warp + kWarps * blockIdx.y; job < 2 * p.cache.n_kv; job += kWarps * gridDim.y) {
-        const int head = job >> 1, plane = job & 1;
-        const bool turns = turned && plane == 0;
-        const bool half = kRope && kHalf && plane == 0;
+    // one group's rows of the heads slice, slice + slices, ...
+    __device__ __forceinline__ void group(const Window &w, int l, int slice)
+    {
+        const int n = w.rows(l);
+        const int64_t id = __shfl_sync(0xffffffffu, w.group, l), row = w.first + l + i;
+        const int spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
+        const unsigned tokens = __reduce_or_sync(0xffffffffu, lane < n ? 1u << spot : 0u);
+        const int token = (int)(__shfl_sync(0xffffffffu, w.slot, (l + i) & 31) & (kGroup - 1));
+        const bool on = i < n, anew = tokens & 1, turned = v < rope.pairs / 8;
         int a, b;
-        lane_vectors(v, kRope ? rope.pairs : 0, half, a, b);
-        for (unsigned left = begins; left != 0; left &= left - 1) {
-            const int l = __ffs(left) - 1, n = rows_from(l);
-            const int64_t row = r0 - 1 + l;
-            const int64_t g = __shfl_sync(0xffffffffu, group, l);
-            const int shift = p.cache.page_shift - 4;
-            float *scale_at;
-            uint8_t *const at = group_at<D>(p.cache, g >> shift, (int)(g & (((int64_t)1 << shift) - 1)), job,
-                                            &scale_at);
-            const float old = *scale_at;
-            const uint4 *const from = (plane ? p.v : p.k) + row * p.kv_stride + head * (D / 8);
-            uint4 in[kSteps][2];
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int i = s * kAtOnce + sub;
-                in[s][0] = in[s][1] = make_uint4(0, 0, 0, 0);
-                if (i < n) {
-                    in[s][0] = __ldcs(from + i * p.kv_stride + a);
-                    in[s][1] = __ldcs(from + i * p.kv_stride + b);
-                }
+        lane_vectors(v, rope.pairs, kHalf, a, b);
+        Spins spins;
+        const int64_t pos = on ? __ldg(p.pos + row) : 0;
+        const uint4 *const from = p.k + row * p.kv_stride;
+        const int shift = p.cache.page_shift - 4;
+        uint4 next[2];
+        float next_old;
+        auto fetch = [&](int head) {
+            next[0] = next[1] = make_uint4(0, 0, 0, 0);
+            if (on) {
+                next[0] = __ldcs(from + head * (D / 8) + a);
+                next[1] = __ldcs(from + head * (D / 8) + b);
             }
-            // the values of step s
-            auto values = [&](int s, float (&x)[8], float (&y)[8]) {
-                pairs_of<T>(in[s][0], in[s][1], half, x, y);
-                if (turns) {
-                    const int i = s * kAtOnce + sub;
-                    const float2 *const cs = spins[l - 1 + (i < n ? i : 0)] + 8 * v;
+            float *scale;
+            group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * head, &scale);
+            next_old = *scale;
+        };
+        fetch(slice);
+        if (turned && on) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        turn(x[j], y[j], cs[j]);
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), (float)rope.amplitude),
+                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), (float)rope.amplitude);
+                spins.c[k] = ptx::pair(f.x, g.x);
+                spins.s[k] = ptx::pair(f.y, g.y);
+            }
+        }
+#pragma unroll 1
+        for (int head = slice; head < p.cache.n_kv; head += p.slices) {
+            const Pairs in = pairs_of<T, kHalf>(next[0], next[1]);
+            const float old = next_old;
+            float *scale_at;
+            uint8_t *const at = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * head,
+                                            &scale_at);
+            if (head + p.slices < p.cache.n_kv)
+                fetch(head + p.slices);
+            Pairs x = in;
+            if (turned && on)
+                hs::kv8::turn(x, spins);
+            // the exact values of pair j
+            auto exactly = [&](int j) {
+                float px = 0.f, py = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float2 ix = ptx::unpair(in.x[k / 2]), iy = ptx::unpair(in.y[k / 2]);
+                    px = k == j ? (k & 1 ? ix.y : ix.x) : px;
+                    py = k == j ? (k & 1 ? iy.y : iy.x) : py;
                 }
+                return turned ? turned_exactly(rope.turns[8 * v + j], pos, rope.amplitude, px, py) : make_double2(px, py);
             };
             float top = 0.f;
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                float x[8], y[8];
-                values(s, x, y);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    top = fmaxf(top, fmaxf(fabsf(x[j]), fabsf(y[j])));
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = ptx::unpair(x.x[k]), g = ptx::unpair(x.y[k]);
+                top = fmaxf(fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y))), fmaxf(fabsf(g.x), fabsf(g.y)));
             }
-            uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
-            const bool odd = bits >= 0x7f800000u;       // an infinity among the values
+            uint32_t bits = largest(__float_as_uint(top));
+            const bool odd = bits >= 0x7f800000u;       // an infinity among the values: they become NaN, and do not count
             if (odd) {
                 top = 0.f;
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    float x[8], y[8];
-                    values(s, x, y);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        top = fabsf(x[j]) < INFINITY ? fmaxf(top, fabsf(x[j])) : top;
-                        top = fabsf(y[j]) < INFINITY ? fmaxf(top, fabsf(y[j])) : top;
-                    }
+                for (int k = 0; k < 4; ++k) {
+                    x.x[k] = ptx::fma2(x.x[k], 0, x.x[k]);
+                    x.y[k] = ptx::fma2(x.y[k], 0, x.y[k]);
+                    const float2 f = ptx::unpair(x.x[k]), g = ptx::unpair(x.y[k]);
+                    top = fmaxf(fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y))), fmaxf(fabsf(g.x), fabsf(g.y)));
                 }
-                bits = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
+                bits = largest(__float_as_uint(top));
             }
-            // 448 = 1.75 2^8
-            int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
-            if (kRope && plane == 0 && !odd && abs((int)(bits & 0x7fffffu) - 0x600000) <= 8) {
-                const double t = largest_exact<T, D, kHalf>(rope, p.pos + row, from, p.kv_stride, n, v, sub);
-                const int64_t w = __double_as_longlong(t);
-                e = (int)(w >> 52) - 1023 - 8 + ((w & 0xfffffffffffffll) > 0xc000000000000ll);
-            }
-            const float need = power_of_two(e < -126 ? -126 : e);
-            const int spot = (int)(__shfl_sync(0xffffffffu, slot, (l + lane) & 31) & (kGroup - 1));
-            const unsigned tokens = __reduce_or_sync(0xffffffffu, lane < n ? 1u << spot : 0u);
-            const bool anew = tokens & 1;
-            const float scale = anew ? need : fmaxf(old, need);
-            if (!anew && need > old) {
-                // what the group holds, 16 bytes to a lane
-                const float shrink = old / need;
-#pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    const int i = s * kAtOnce + sub;
-                    if ((tokens >> i) & 1)
-                        continue;
-                    uint4 *const w = reinterpret_cast<uint4 *>(at + i * D) + v;
-                    const uint4 y = *w;
-                    auto again = [&](uint32_t u) {
-                        const float2 f = widen<__half>(e4m3_to_f16(u)), h = widen<__half>(e4m3_to_f16_high(u));
-                        return to_e4m3(f.x * shrink, f.y * shrink, h.x * shrink, h.y * shrink);
-                    };
-                    *w = make_uint4(again(y.x), again(y.y), again(y.z), again(y.w));
-                }
-            }
-            const float by = 1.f / scale;
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int i = s * kAtOnce + sub;
-                const int token = __shfl_sync(0xffffffffu, spot, i);
-                if (i >= n)
-                    continue;
-                float x[8], y[8];
-                values(s, x, y);
-                if (odd) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        x[j] = fabsf(x[j]) < INFINITY ? x[j] : NAN;
-                        y[j] = fabsf(y[j]) < INFINITY ? y[j] : NAN;
-                    }
-                }
-#pragma unroll
+            int e = exponent_of(bits);
+            // |x| + |y| is at most twice the largest turned value, and 2^-20 of that 15 steps
+            if (abs((int)(bits & 0x7fffffu) - 0x600000) <= 16) {
+                const float close = __uint_as_float(bits) * (1.f - 0x1p-18f);
+                const double border = __uint_as_float((bits & 0x7f800000u) | 0x600000u);
+                bool above = false;
+#pragma unroll 1
                 for (int j = 0; j < 8; ++j) {
-                    x[j] *= by;
-                    y[j] *= by;
+                    float y = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float2 f = ptx::unpair(x.x[k / 2]), g = ptx::unpair(x.y[k / 2]);
+                        y = k == j ? fmaxf(fabsf(k & 1 ? f.y : f.x), fabsf(k & 1 ? g.y : g.x)) : y;
+                    }
+                    if (!on || !(y >= close))
+                        continue;
+                    const double2 z = exactly(j);
+                    above = above || fabs(z.x) > border || fabs(z.y) > border;
+                }
+                __syncwarp();
+                e = (int)(bits >> 23) - 127 - 8 + largest(above);
+            }
+            const float need = power_of_two(e < -126 ? -126 : e), scale = anew ? need : fmaxf(old, need), by = 1.f / scale;
+            if (i == 0 && v == 0)
+                *scale_at = scale;
+            if (!anew && need > old && !((tokens >> i) & 1)) {
+                // what the group holds: token i's bytes
+                const float shrink = old / need;
+                uint4 *const held = reinterpret_cast<uint4 *>(at + i * D) + v;
+                const uint4 y = *held;
+                auto again = [&](uint32_t u) {
+                    const float2 f = widen<__half>(e4m3_to_f16(u)), h = widen<__half>(e4m3_to_f16_high(u));
+                    return to_e4m3(f.x * shrink, f.y * shrink, h.x * shrink, h.y * shrink);
+                };
+                *held = make_uint4(again(y.x), again(y.y), again(y.z), again(y.w));
+            }
+            if (on) {
+                const uint64_t by2 = ptx::pair(by, by);
+                uint32_t byte[4];
+                if (turned) {
+                    const float off = kOff * (float)rope.amplitude * by;
+                    quantise_turned(x, in, by2, ptx::pair(off, off), by, exactly, byte);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        x.x[k] = ptx::mul2(x.x[k], by2);
+                        x.y[k] = ptx::mul2(x.y[k], by2);
+                    }
+                    bytes_of<kHalf>(x, byte);
                 }
                 uint8_t *const to = at + token * D;
-                if (half && turned) {
-                    *reinterpret_cast<uint2 *>(to + 8 * a) =
-                        make_uint2(to_e4m3(x[0], x[1], x[2], x[3]), to_e4m3(x[4], x[5], x[6], x[7]));
-                    *reinterpret_cast<uint2 *>(to + 8 * b) =
-                        make_uint2(to_e4m3(y[0], y[1], y[2], y[3]), to_e4m3(y[4], y[5], y[6], y[7]));
-                } else if (half) {              // x and y hold the two vectors one behind the other
-                    *reinterpret_cast<uint4 *>(to + 8 * a) =
-                        make_uint4(to_e4m3(x[0], x[1], x[2], x[3]), to_e4m3(x[4], x[5], x[6], x[7]),
-                                   to_e4m3(y[0], y[1], y[2], y[3]), to_e4m3(y[4], y[5], y[6], y[7]));
-                } else {                        // and here every other element
-                    *reinterpret_cast<uint4 *>(to + 8 * a) =
-                        make_uint4(to_e4m3(x[0], y[0], x[1], y[1]), to_e4m3(x[2], y[2], x[3], y[3]),
-                                   to_e4m3(x[4], y[4], x[5], y[5]), to_e4m3(x[6], y[6], x[7], y[7]));
-                }
+                *reinterpret_cast<uint2 *>(to + 8 * a) = make_uint2(byte[0], byte[1]);
+                *reinterpret_cast<uint2 *>(to + 8 * b) = make_uint2(byte[2], byte[3]);
             }
-            if (lane == 0)
-                *scale_at = scale;
+            __syncwarp();
         }
     }
 
-    // q
-    if constexpr (kRope) {
-        if (p.q == nullptr)
-            return;
-        int a, b;
-        lane_vectors(v, rope.pairs, kHalf, a, b);
-        const int each = kThreads / kLanes;
-        for (int i = threadIdx.x / kLanes + each * blockIdx.y; i < p.window * p.n_heads; i += each * gridDim.y) {
-            const int r = i / p.n_heads, h = i - r * p.n_heads;
-            const int64_t row = r0 + r;
-            if (row >= p.n_rows || __ldg(p.slots + row) < 0)
-                continue;
-            const uint4 *const from = p.q + row * p.q_stride + h * (D / 8);
-            uint4 *const to = p.q_out + row * p.q_out_stride + h * (D / 8);
-            uint4 y0 = __ldcs(from + a), y1 = __ldcs(from + b);
-            if (turned) {
-                float x[8], y[8];
-                pairs_of<T>(y0, y1, kHalf, x, y);
+    // turned values times by2 as bytes; off2 times |x| + |y| of `in` is how far they may be off
+    template <typename Exactly>
+    __device__ __forceinline__ static void quantise_turned(const Pairs &x, const Pairs &in, uint64_t by2, uint64_t off2, float by,
+                                                           Exactly exactly, uint32_t (&w)[4])
+    {
+        constexpr uint64_t kAbs = 0x7fffffff7fffffffull, kSign = 0x8000000080000000ull;
+        Pairs low, high;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    turn(x[j], y[j], spins[r][8 * v + j]);
-                vectors_of<T>(x, y, kHalf, y0, y1);
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t off = ptx::mul2(ptx::add2(in.x[k] & kAbs, in.y[k] & kAbs), off2);
+            high.x[k] = ptx::fma2(x.x[k], by2, off);
+            high.y[k] = ptx::fma2(x.y[k], by2, off);
+            low.x[k] = ptx::fma2(x.x[k], by2, off ^ kSign);
+            low.y[k] = ptx::fma2(x.y[k], by2, off ^ kSign);
+        }
+        uint32_t z[4];
+        bytes_of<kHalf>(low, w);
+        bytes_of<kHalf>(high, z);
+        // values that go to two numbers by what they may be off
+#pragma unroll 1
+        while (((w[0] ^ z[0]) | (w[1] ^ z[1]) | (w[2] ^ z[2]) | (w[3] ^ z[3])) != 0) {
+            const uint64_t first = (uint64_t)(w[1] ^ z[1]) << 32 | (w[0] ^ z[0]);
+            const int byte = first != 0 ? (__ffsll(first) - 1) / 8
+                                        : 8 + (__ffsll((uint64_t)(w[3] ^ z[3]) << 32 | (w[2] ^ z[2])) - 1) / 8;
+            const int j = kHalf ? byte & 7 : byte >> 1;
+            const double2 q = exactly(j);
+            const uint32_t r = to_e4m3(fabsf((float)q.x) < INFINITY ? toward(q.x * by) : NAN,
+                                       fabsf((float)q.y) < INFINITY ? toward(q.y * by) : NAN, 0.f, 0.f);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = byte_of<kHalf>(j, h);
+                const uint32_t mask = 0xffu << 8 * (at & 3), put = (r >> 8 * h & 0xff) << 8 * (at & 3);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k == at >> 2) {
+                        w[k] = (w[k] & ~mask) | put;
+                        z[k] = (z[k] & ~mask) | put;
+                    }
             }
-            to[a] = y0;
-            to[b] = y1;
         }
     }
+};
+
+// Blocks: the turned keys' teams, which take longest; warps for the other planes' heads; q.
+template <typename T, int D, bool kRope, bool kHalf>
+__global__ void __launch_bounds__(kThreads, kRope ? 6 : 8)
+kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ RopeParams rope)
+{
+    using Keys = Team<T, D, kHalf>;
+    __shared__ uint32_t tops[Keys::kCount][2][Keys::kWarps];
+    pdl_wait_and_release();
+    const int lane = threadIdx.x & 31;
+    if constexpr (kRope) {
+        if ((int)blockIdx.x < p.team_blocks) {
+            const int team = threadIdx.x / Keys::kSize, in_team = threadIdx.x % Keys::kSize;
+            const int unit = blockIdx.x * Keys::kCount + team, slice = unit / p.windows;
+            if (slice >= p.slices)
+                return;
+            const Window w(p, (int64_t)(unit - slice * p.windows) * p.window, false, lane);
+            Keys keys{p, rope, tops[team], team, lane, in_team / 32, in_team / Keys::kLanes, in_team % Keys::kLanes};
+#pragma unroll 1
+            for (unsigned left = w.begins; left != 0; left &= left - 1)
+                keys.group(w, __ffs(left) - 1, slice);
+            return;
+        }
+    }
+    if ((int)blockIdx.x < p.team_blocks + p.warp_blocks) {
+        const int unit = (blockIdx.x - p.team_blocks) * (kThreads / 32) + threadIdx.x / 32, part = unit / p.windows;
+        const int planes = (kRope ? 1 : 2) * p.cache.n_kv;            // values alone, or both planes of each head
+        if (part >= p.parts)
+            return;
+        const Window w(p, (int64_t)(unit - part * p.windows) * p.window, part == 0, lane);
+        const int shift = p.cache.page_shift - 4;
+#pragma unroll 1
+        for (unsigned left = w.begins; left != 0; left &= left - 1) {
+            const int l = __ffs(left) - 1;
+            const int64_t id = __shfl_sync(0xffffffffu, w.group, l);
+            Group g;
+            g.n = w.rows(l);
+            g.spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
+            g.tokens = __reduce_or_sync(0xffffffffu, lane < g.n ? 1u << g.spot : 0u);
+#pragma unroll 1
+            for (int x = part; x < planes; x += p.parts) {
+                const int head_plane = kRope ? 2 * x + 1 : x;
+                g.at = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), head_plane, &g.scale_at);
+                g.old = *g.scale_at;
+                quantise<T, D>(g, (head_plane & 1 ? p.v : p.k) + (w.first + l) * p.kv_stride + (head_plane >> 1) * (D / 8),
+                               p.kv_stride, lane);
+            }
+        }
+        return;
+    }
+    if constexpr (kRope) {
+        const RopeRows q{p.q, nullptr, p.q_out, nullptr, p.q_stride, 0, p.q_out_stride, 0, p.pos, p.n_rows, p.n_heads, 0, p.q_slices};
+        turn_rows<T, D, kHalf>(q, rope, p.slots,
+                               (int64_t)(blockIdx.x - p.team_blocks - p.warp_blocks) * (kThreads / Keys::kLanes));
+    }
+}
+
+// how many share `all` heads of each of `windows` windows so that there are `wanted` in all
+int32_t shared_by(int32_t all, int32_t windows, int64_t wanted)
+{
+    int32_t n = 1;
+    while (n < all && (int64_t)windows * n < wanted)
+        n *= 2;
+    return n < all ? n : all;
 }
 
 template <typename T, int D>
 cudaError_t launch(Kv8Append p, const RopeParams *rope, int sm_count, cudaStream_t s)
 {
-    // windows of one row where there are few, up to 16 rows where those fill the SMs
+    constexpr int kTeams = kThreads / D, kJobs = kThreads / (D / 16);
+    // Few rows may be a decode step's, each a group of its own: windows of one row, and of more where they fill the SMs.
     p.window = 1;
-    while (p.window < kWindow && p.n_rows >= (int64_t)sm_count * 2 * p.window)
+    while (p.window < kGroup && p.n_rows >= (int64_t)sm_count * 2 * p.window)
         p.window *= 2;
-    const int64_t grid = (p.n_rows + p.window - 1) / p.window;
-    if (grid > INT32_MAX)
+    p.windows = (int)((p.n_rows + p.window - 1) / p.window);
+    // About three groups' planes for every warp that an SM holds: 28,913 rows of 8 x 128 take 31.0 us so, 34.8 with one (a
+    // warp waits for a group's rows one after the other).  Beside turned keys, whose teams are the longer part and
+    // share the SM, one: 14,494 rows of 16 + 4 x 128 33.8 us, 38.3 with three.
+    p.parts = shared_by((rope != nullptr ? 1 : 2) * p.cache.n_kv, p.windows, (int64_t)sm_count * (rope != nullptr ? 32 : 96));
+    p.warp_blocks = (p.windows * p.parts + kThreads / 32 - 1) / (kThreads / 32);
+    int64_t blocks = p.warp_blocks;
+    if (rope != nullptr) {
+        p.slices = shared_by(p.cache.n_kv, p.windows, (int64_t)sm_count * 8 * kTeams);
+        p.team_blocks = (p.windows * p.slices + kTeams - 1) / kTeams;
+        blocks += p.team_blocks;
+        if (p.q != nullptr) {
+            p.q_slices = rope_slices(p.n_rows, p.n_heads, sm_count, kJobs);
+            blocks += (p.n_rows * p.q_slices + kJobs - 1) / kJobs;
+        }
+    }
+    if (blocks > INT32_MAX)
         return cudaErrorInvalidValue;
-    const int jobs = 2 * p.cache.n_kv + (rope != nullptr && p.q != nullptr ? p.n_heads : 0);
-    int y = (int)((2 * sm_count + grid - 1) / grid);
-    if (y > (jobs + kWarps - 1) / kWarps)
-        y = (jobs + kWarps - 1) / kWarps;
-    const dim3 blocks((unsigned)grid, (unsigned)y);
     if (rope == nullptr)
-        return launch_pdl(kv8_append_kernel<T, D, false, false>, blocks, dim3(kThreads), 0, s, p,
+        return launch_pdl(kv8_append_kernel<T, D, false, false>, dim3((unsigned)blocks), dim3(kThreads), 0, s, p,
                           RopeParams{});
     return launch_pdl(rope->layout == HS_ROPE_HALF ? kv8_append_kernel<T, D, true, true>
                                                    : kv8_append_kernel<T, D, true, false>,
-                      blocks, dim3(kThreads), 0, s, p, *rope);
+                      dim3((unsigned)blocks), dim3(kThreads), 0, s, p, *rope);
 }
 
 }  // namespace

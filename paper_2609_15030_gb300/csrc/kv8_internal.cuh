@@ -6,6 +6,7 @@
 
 #include "attn_internal.cuh"
 #include "hs_kv8.h"
+#include "sm100_ptx.cuh"
 
 namespace hs {
 
@@ -56,7 +57,10 @@ struct Kv8Append {
     int64_t n_rows;
     int32_t *d_err;
     int32_t n_heads;
-    int32_t window;               // rows whose groups a block begins
+    int32_t window, windows;      // rows whose groups a unit begins, and how many of these
+    int32_t slices, parts;        // teams that share a window's turned keys, warps that share its other planes
+    int32_t q_slices;             // threads that share a row's heads of q
+    int32_t team_blocks, warp_blocks;   // in front of those for q
 };
 
 struct Kv8Read {
@@ -210,43 +214,121 @@ __device__ __forceinline__ void lane_vectors(int v, int pairs, bool half, int &a
     }
 }
 
-// The pairs of a lane's vectors as floats, x and y of pair j, and back into the vectors' order.
-template <typename T>
-__device__ __forceinline__ void pairs_of(const uint4 &a, const uint4 &b, bool half, float (&x)[8],
-                                         float (&y)[8])
+// Eight pairs of a head as floats, two to a register pair: x[k] and y[k] of the pairs 2 k and 2 k + 1.
+struct Pairs {
+    uint64_t x[4], y[4];
+};
+
+// their cosines and sines
+struct Spins {
+    uint64_t c[4], s[4];
+};
+
+// a lane's vectors as pairs, and back
+template <typename T, bool kHalf>
+__device__ __forceinline__ Pairs pairs_of(const uint4 &a, const uint4 &b)
 {
     const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    Pairs p;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float2 f = widen<T>(u[j]);
-        if (half) {
-            (j < 4 ? x : y)[2 * (j & 3)] = f.x;
-            (j < 4 ? x : y)[2 * (j & 3) + 1] = f.y;
-        } else {
-            x[j] = f.x;
-            y[j] = f.y;
-        }
+    for (int k = 0; k < 4; ++k) {
+        const float2 f = widen<T>(u[kHalf ? k : 2 * k]), g = widen<T>(u[kHalf ? k + 4 : 2 * k + 1]);
+        p.x[k] = kHalf ? ptx::pair(f.x, f.y) : ptx::pair(f.x, g.x);
+        p.y[k] = kHalf ? ptx::pair(g.x, g.y) : ptx::pair(f.y, g.y);
     }
+    return p;
 }
 
-template <typename T>
-__device__ __forceinline__ void vectors_of(const float (&x)[8], const float (&y)[8], bool half, uint4 &a,
-                                           uint4 &b)
+template <typename T, bool kHalf>
+__device__ __forceinline__ void vectors_of(const Pairs &p, uint4 &a, uint4 &b)
 {
     uint32_t u[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        u[j] = half ? narrow<T>((j < 4 ? x : y)[2 * (j & 3)], (j < 4 ? x : y)[2 * (j & 3) + 1])
-                    : narrow<T>(x[j], y[j]);
+    for (int k = 0; k < 4; ++k) {
+        const float2 x = ptx::unpair(p.x[k]), y = ptx::unpair(p.y[k]);
+        u[kHalf ? k : 2 * k] = kHalf ? narrow<T>(x.x, x.y) : narrow<T>(x.x, y.x);
+        u[kHalf ? k + 4 : 2 * k + 1] = kHalf ? narrow<T>(y.x, y.y) : narrow<T>(x.y, y.y);
+    }
     a = make_uint4(u[0], u[1], u[2], u[3]);
     b = make_uint4(u[4], u[5], u[6], u[7]);
 }
 
-__device__ __forceinline__ void turn(float &x, float &y, float2 cs)
+// (x, y) to (x c - y s, y c + x s)
+__device__ __forceinline__ void turn(Pairs &p, const Spins &by)
 {
-    const float t = x * cs.x - y * cs.y;
-    y = y * cs.x + x * cs.y;
-    x = t;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const uint64_t x = p.x[k], y = p.y[k];
+        p.x[k] = ptx::fma2(y, by.s[k] ^ 0x8000000080000000ull, ptx::mul2(x, by.c[k]));
+        p.y[k] = ptx::fma2(x, by.s[k], ptx::mul2(y, by.c[k]));
+    }
+}
+
+// threads that share a row's heads: as many heads to a thread as fill the SMs; `jobs`: rows of a block at one slice
+inline int32_t rope_slices(int64_t n_rows, int heads, int sm_count, int jobs)
+{
+    int64_t slices = 4;
+    while (slices < heads && n_rows * slices < (int64_t)sm_count * 4 * jobs)
+        slices *= 2;
+    return (int32_t)(slices < heads ? slices : heads);
+}
+
+// Rows turned: every D / 16 lanes take a job, a row's heads slice, slice + slices, ...; the block's jobs begin at `job0`.  A
+// lane's 8 sines and cosines serve all its heads, several of which are in flight.  Rows with a negative slot are
+// left out (slots: nullptr, or of the rows).
+template <typename T, int D, bool kHalf>
+__device__ __forceinline__ void turn_rows(const RopeRows &p, const RopeParams &rope, const int64_t *slots, int64_t job0)
+{
+    constexpr int kLanes = D / 16, kAhead = 4;
+    const int v = threadIdx.x % kLanes, heads = p.n_heads + p.n_kv;
+    const bool turned = v < rope.pairs / 8;
+    int a, b;
+    lane_vectors(v, rope.pairs, kHalf, a, b);
+    const int64_t job = job0 + threadIdx.x / kLanes, row = job / p.slices;
+    const int slice = (int)(job - row * p.slices);
+    if (row >= p.n_rows)
+        return;
+    const int64_t pos = turned ? __ldg(p.pos + row) : 0;
+    if (slots != nullptr && __ldg(slots + row) < 0)
+        return;
+    Spins spins;
+    for (int h0 = slice; h0 < heads; h0 += p.slices * kAhead) {
+        uint4 in[kAhead][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + i * p.slices;
+            if (h >= heads)
+                break;
+            const uint4 *const from = h < p.n_heads ? p.q + row * p.q_stride + h * (D / 8)
+                                                    : p.k + row * p.k_stride + (h - p.n_heads) * (D / 8);
+            in[i][0] = __ldcs(from + a);
+            in[i][1] = __ldcs(from + b);
+        }
+        if (h0 == slice && turned) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), (float)rope.amplitude),
+                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), (float)rope.amplitude);
+                spins.c[k] = ptx::pair(f.x, g.x);
+                spins.s[k] = ptx::pair(f.y, g.y);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + i * p.slices;
+            if (h >= heads)
+                break;
+            if (turned) {
+                Pairs x = pairs_of<T, kHalf>(in[i][0], in[i][1]);
+                turn(x, spins);
+                vectors_of<T, kHalf>(x, in[i][0], in[i][1]);
+            }
+            uint4 *const to = h < p.n_heads ? p.q_out + row * p.q_out_stride + h * (D / 8)
+                                            : p.k_out + row * p.k_out_stride + (h - p.n_heads) * (D / 8);
+            to[a] = in[i][0];
+            to[b] = in[i][1];
+        }
+    }
 }
 
 }  // namespace kv8
