@@ -2,8 +2,11 @@
 // recomputed suffix attends to, Section 2.2 of the paper).
 //
 // Bytes in, twice as many out: bound by HBM.  Units of 16 tokens (a group, all heads, both planes) are shared
-// out evenly over the blocks, whatever the requests' lengths.  A thread takes 8 bytes of a token to 16, of
-// eight (KV head, plane) at a time: a warp reads 256 contiguous bytes and writes two rows of 256.
+// out evenly over the blocks, whatever the requests' lengths.  A thread takes 16 bytes of a token to 32, of up to
+// eight (KV head, plane) at a time.  459,413 tokens of 8 heads of 128 (2.82 GB) take 434 us, 6.5 TB/s; with 8 bytes to
+// 16 and as many loads in flight 461.  Groups of fewer heads have fewer loads for a thread (16 requests of 3,000 tokens of 4
+// heads: 26 us, 5.5 TB/s); taking several groups at a time, each vector with its own table entries, cost more than it
+// brought (35 us).
 #include "kv8_walk.cuh"
 
 namespace hs {
@@ -13,13 +16,12 @@ using namespace kv8;
 
 constexpr int kThreads = 256;
 
-template <typename T, int D>
+template <typename T, int D, int kAhead>
 __global__ void __launch_bounds__(kThreads)
 kv8_read_kernel(const __grid_constant__ Kv8Read p)
 {
-    constexpr int kVecs = D / 8;                          // 8-byte vectors of a token
+    constexpr int kVecs = D / 16;                         // 16-byte vectors of a token
     constexpr int kPieces = kThreads / (kGroup * kVecs);  // (KV head, plane) pairs of a block at a time
-    constexpr int kAhead = 8;
     __shared__ Lengths all;
     pdl_wait_and_release();
     const int lane = threadIdx.x & 31;
@@ -47,9 +49,9 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
         const bool on = g * kGroup + token < all.len[b];
         const int in_page = g & ((1 << shift) - 1);
         uint4 *const out = p.out + (((int64_t)to * 2 << p.cache.page_shift) + in_page * kGroup + token) *
-                                       p.cache.n_kv * kVecs + vec;
+                                       p.cache.n_kv * (2 * kVecs) + 2 * vec;
         for (int i0 = piece; i0 < 2 * p.cache.n_kv; i0 += kPieces * kAhead) {
-            uint2 x[kAhead];
+            uint4 x[kAhead];
             float scale[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
@@ -58,7 +60,7 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
                     continue;
                 float *at_scale;
                 const uint8_t *const at = group_at<D>(p.cache, from, in_page, head_plane, &at_scale);
-                x[i] = __ldcs(reinterpret_cast<const uint2 *>(at + token * D) + vec);
+                x[i] = __ldcs(reinterpret_cast<const uint4 *>(at + token * D) + vec);
                 scale[i] = __ldg(at_scale);
             }
 #pragma unroll
@@ -70,10 +72,14 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
                     const float2 f = widen<__half>(f16);
                     return narrow_finite<T>(f.x * scale[i], f.y * scale[i]);
                 };
-                const uint4 y = make_uint4(pair(e4m3_to_f16(x[i].x)), pair(e4m3_to_f16_high(x[i].x)),
-                                           pair(e4m3_to_f16(x[i].y)), pair(e4m3_to_f16_high(x[i].y)));
-                const int64_t plane = ((int64_t)(head_plane & 1) << p.cache.page_shift) * p.cache.n_kv * kVecs;
-                __stcs(out + plane + (head_plane >> 1) * kVecs, y);
+                const int64_t plane = ((int64_t)(head_plane & 1) << p.cache.page_shift) * p.cache.n_kv * (2 * kVecs);
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
+                                 out + plane + (head_plane >> 1) * (2 * kVecs)),
+                             "r"(pair(e4m3_to_f16(x[i].x))), "r"(pair(e4m3_to_f16_high(x[i].x))),
+                             "r"(pair(e4m3_to_f16(x[i].y))), "r"(pair(e4m3_to_f16_high(x[i].y))),
+                             "r"(pair(e4m3_to_f16(x[i].z))), "r"(pair(e4m3_to_f16_high(x[i].z))),
+                             "r"(pair(e4m3_to_f16(x[i].w))), "r"(pair(e4m3_to_f16_high(x[i].w)))
+                             : "memory");
             }
         }
     }
@@ -83,8 +89,10 @@ template <typename T, int D>
 cudaError_t launch(const Kv8Read &p, int sm_count, cudaStream_t s)
 {
     const int64_t units = (int64_t)p.batch * groups_of(p.max_kv), most = (int64_t)sm_count * 8;
-    return launch_pdl(kv8_read_kernel<T, D>, dim3((unsigned)(units < most ? units : most)), dim3(kThreads), 0, s,
-                      p);
+    // as many vectors of a thread in flight as a group has for it
+    const int pieces = 2 * p.cache.n_kv * kGroup * (D / 16) / kThreads;
+    return launch_pdl(pieces > 4 ? kv8_read_kernel<T, D, 8> : pieces > 2 ? kv8_read_kernel<T, D, 4> : kv8_read_kernel<T, D, 2>,
+                      dim3((unsigned)(units < most ? units : most)), dim3(kThreads), 0, s, p);
 }
 
 }  // namespace
