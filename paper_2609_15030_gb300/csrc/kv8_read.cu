@@ -16,6 +16,19 @@ using namespace kv8;
 
 constexpr int kThreads = 256;
 
+// 32 bytes, in one store where the address is a multiple of that
+__device__ __forceinline__ void store(uint4 *to, bool wide, uint4 a, uint4 b)
+{
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(a.x), "r"(a.y), "r"(a.z),
+                     "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                     : "memory");
+    } else {
+        to[0] = a;
+        to[1] = b;
+    }
+}
+
 template <typename T, int D, int kAhead>
 __global__ void __launch_bounds__(kThreads)
 kv8_read_kernel(const __grid_constant__ Kv8Read p)
@@ -35,6 +48,7 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
     const int piece = threadIdx.x / (kGroup * kVecs), token = threadIdx.x / kVecs % kGroup,
               vec = threadIdx.x % kVecs;
     const int shift = p.cache.page_shift - 4;
+    const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31) == 0;     // rows of a head are multiples of 32 bytes
     for (; u < end; ++u) {
         while (all.before[b + 1] <= u)
             ++b;
@@ -73,13 +87,11 @@ kv8_read_kernel(const __grid_constant__ Kv8Read p)
                     return narrow_finite<T>(f.x * scale[i], f.y * scale[i]);
                 };
                 const int64_t plane = ((int64_t)(head_plane & 1) << p.cache.page_shift) * p.cache.n_kv * (2 * kVecs);
-                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(
-                                 out + plane + (head_plane >> 1) * (2 * kVecs)),
-                             "r"(pair(e4m3_to_f16(x[i].x))), "r"(pair(e4m3_to_f16_high(x[i].x))),
-                             "r"(pair(e4m3_to_f16(x[i].y))), "r"(pair(e4m3_to_f16_high(x[i].y))),
-                             "r"(pair(e4m3_to_f16(x[i].z))), "r"(pair(e4m3_to_f16_high(x[i].z))),
-                             "r"(pair(e4m3_to_f16(x[i].w))), "r"(pair(e4m3_to_f16_high(x[i].w)))
-                             : "memory");
+                store(out + plane + (head_plane >> 1) * (2 * kVecs), wide,
+                      make_uint4(pair(e4m3_to_f16(x[i].x)), pair(e4m3_to_f16_high(x[i].x)), pair(e4m3_to_f16(x[i].y)),
+                                 pair(e4m3_to_f16_high(x[i].y))),
+                      make_uint4(pair(e4m3_to_f16(x[i].z)), pair(e4m3_to_f16_high(x[i].z)), pair(e4m3_to_f16(x[i].w)),
+                                 pair(e4m3_to_f16_high(x[i].w))));
             }
         }
     }

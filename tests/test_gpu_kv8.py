@@ -296,15 +296,17 @@ READ = [(4, 128, 16, "bf16", [300, 0, 1, 16, 17, 999]), (2, 64, 32, "fp16", [31,
         (1, 64, 256, "bf16", [700, 255, 256, 257]), (3, 128, 64, "bf16", [5] * 50), (5, 64, 16, "fp16", [90, 1] * 120)]
 
 
+@pytest.mark.parametrize("shift", [0, 8])       # elements: a cache at a multiple of 16 bytes, not of 32
 @pytest.mark.parametrize("kv_heads,d,page,dtype,lens", READ)
-def test_read(dev, kv_heads, d, page, dtype, lens):
+def test_read(dev, kv_heads, d, page, dtype, lens, shift):
     c, table = filled(1, lens, kv_heads, page, d, width=-(-max(lens) // page) + 2)
     blocks = c.blocks + 5
     g = torch.Generator().manual_seed(9)
     to = torch.randperm(blocks, generator=g).int()
     out_table = torch.where(table >= 0, to[table.clamp(min=0).long()], -1).int()
-    out = torch.full((blocks, 2, page, kv_heads, d), math.nan, dtype=DT[dtype], device=dev)
-    want = out.cpu()
+    room = torch.full((blocks * 2 * page * kv_heads * d + 16,), math.nan, dtype=DT[dtype], device=dev)
+    out = room[shift:shift - 16].view(blocks, 2, page, kv_heads, d)
+    want = out.cpu().contiguous()
     vals = c.values()
     for b, n in enumerate(lens):
         for j in range(n):
@@ -319,6 +321,7 @@ def test_read(dev, kv_heads, d, page, dtype, lens):
         assert err.item() == 0
         assert torch.equal(out.cpu().nan_to_num(7.0), want.nan_to_num(7.0))
         assert torch.equal(torch.isnan(out.cpu()), torch.isnan(want))
+        assert torch.isnan(room[:shift]).all() and torch.isnan(room[shift - 16:]).all()
 
 
 def test_read_of_every_byte_and_the_largest_values(dev):
