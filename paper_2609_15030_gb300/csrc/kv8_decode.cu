@@ -21,16 +21,23 @@
 //
 // Few rows share a tile's bytes (the heads of one KV head), so the step is bound by HBM; products of M = 128 rows as in
 // the 16-bit attention would leave most of the tensor core's rows empty, and the bytes would have to
-// become numbers on a way through shared memory.
+// become numbers on a way through shared memory.  Four requests of 98k to 131k keys (943 MB) take 146 us, 6.5 TB/s, where
+// the 16-bit step takes 269 to 279; 64 of 4,096 keys of 8 heads 91 us, 5.9 TB/s; 32 ragged ones 33 us, of which HBM
+// accounts for 22 (3.5 us until the first tiles are there, 2 to 5 for the ends and the join's launch, 2 for the join); one
+// of 4,600 keys 9.0 us, latency.  16 rows to a KV head (155 us for 799 MB, 5.1 TB/s) and heads of 64 (58 us for 268 MB) are bound by
+// instructions: 650 a tile and warp, 100 of them conversions, with 2 to 4 warps to a scheduler.
+//
+// What was tried: loads into registers (two blocks of 8 warps to an SM: 154 us for the long ones, 67 for heads of 64, 82 for 16
+// rows where the ring takes 63; no room for more than one tile ahead); the ring by asynchronous copies of 16 bytes (205 us: they and
+// the reads share one queue); prefetches into L2 (1 to 4 tiles ahead: no gain); two tiles to a step (148 us, but 11.3 us
+// for one request: code that runs once waits for its instructions).
+#include "attn_ptx.cuh"
 #include "kv8_walk.cuh"
-#include "sm100_ptx.cuh"
 #include "tensor_map.cuh"
 
 namespace hs {
 namespace kv8 {
 namespace {
-
-constexpr int kWholeTiles = 10;
 
 // floats of a part: per row m and l, then its sums, rows padded against bank conflicts
 template <int D, int R>
@@ -43,12 +50,16 @@ struct Sizes {
     static constexpr int R = 8 * NT;
     static constexpr int kTiles = D == 128 && NT == 1 ? 1 : 2;
     static constexpr int kWarps = D == 128 ? (NT == 1 ? 12 : 8) : NT == 1 ? 16 : 12;
-    static constexpr int kStages = D == 128 ? (NT == 1 ? 4 : 2) : 3;
+    static constexpr int kStages = D == 128 ? (NT == 1 ? 3 : 2) : NT == 1 ? 2 : 3;
     static constexpr int kThreads = kWarps * 32;
     static constexpr int kPlaneBytes = kGroup * D, kTileBytes = 2 * kPlaneBytes;
     static constexpr int kStageBytes = kTiles * kTileBytes, kRingBytes = kStages * kStageBytes;
     static_assert(kStageBytes % 1024 == 0 && kRingBytes >= (int)sizeof(float) * kPartFloats<D, R>);
-    static constexpr size_t smem(int warps) { return (size_t)warps * kRingBytes + 1024; }
+    // beside the rings a part for each warp
+    static constexpr size_t smem(int warps)
+    {
+        return (size_t)warps * (kRingBytes + sizeof(float) * kPartFloats<D, R>) + 1024;
+    }
 };
 
 // one of a block's parts
@@ -612,9 +623,12 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
     __shared__ uint64_t bars[S::kWarps][S::kStages + 1];     // the last one is for failure-detection tests
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     uint8_t *const rings = shared + (-(intptr_t)ptx::smem_u32(shared) & 1023), *const ring = rings + warp * S::kRingBytes;
+    float *const heads = reinterpret_cast<float *>(rings + warps * S::kRingBytes);
     if (lane <= S::kStages)
         ptx::mbar_init(ptx::smem_u32(&bars[warp][lane]), S::kTiles);
     ptx::fence_mbar_init();
+    if (threadIdx.x == 0)
+        ptx::prefetch_tensormap(&map);
     __syncwarp();
     pdl_wait_and_release();
     Loader<D, NT> loader{p, cache, map, all, plan, ptx::smem_u32(ring), ptx::smem_u32(bars[warp]),
@@ -699,13 +713,12 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
                 if (n == per) {
                     w.write(p, rows, lane);
                 } else {
-                    // the run's last part goes over the ring, one in front of it to the workspace
+                    // the run's last part goes over the ring, one in front of it behind the rings
                     const bool last = u == end;
                     if (last)
                         arrived<0>();
                     __syncwarp();
-                    w.leave(last ? reinterpret_cast<float *>(ring)
-                                 : p.part + parts_at(gridDim.x) + (int64_t)(2 * gridDim.x + blockIdx.x * warps + warp) * kPart, lane);
+                    w.leave(last ? reinterpret_cast<float *>(ring) : heads + warp * kPart, lane);
                     if (lane == 0)
                         part[2 * warp + last] = Part{b * plan.items + item, from == 0, from + n == per};
                 }
@@ -755,12 +768,12 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
         if (lane == 0)
             firsts[chains] = count;
         __syncwarp();
-        for (int job = warp; job < chains * R; job += warps) {
-            const int c = job / R, r = job - c * R, i0 = firsts[c], n = firsts[c + 1] - i0;
+        const int live = min(R, p.group);                   // rows of an item at most
+        for (int job = warp; job < chains * live; job += warps) {
+            const int c = job / live, r = job - c * live, i0 = firsts[c], n = firsts[c + 1] - i0;
             const int own = order[i0 + min(lane, n - 1)];
             const float *at = own & 1 ? reinterpret_cast<const float *>(rings + (own >> 1) * S::kRingBytes)
-                                      : p.part + parts_at(gridDim.x) +
-                                            (int64_t)(2 * gridDim.x + blockIdx.x * warps + (own >> 1)) * kPart;
+                                      : heads + (own >> 1) * kPart;
             const Part a = part[own];
             const int it = a.item, bb = plan.by_items.div(it);
             const bool starts = __shfl_sync(0xffffffffu, a.starts, 0), ends = __shfl_sync(0xffffffffu, a.ends, n - 1);
@@ -775,8 +788,8 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
             const int col = lane * 4 % D;                   // 64 columns: the second half of the lanes repeats the first
             at += 2 * R + r * (D + 4);
             const float4 o = join<4>(m, l, n, [&](int i, int) {
-                return *reinterpret_cast<const float4 *>(
-                    reinterpret_cast<const float *>(__shfl_sync(0xffffffffu, (unsigned long long)at, i)) + col);
+                const int from = __shfl_sync(0xffffffffu, (int)(at - heads), i);
+                return *reinterpret_cast<const float4 *>(heads + from + col);
             });
             if (lane * 4 >= D)
                 continue;
@@ -926,14 +939,18 @@ int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
     const int64_t items = (int64_t)p.batch * plan.items, longest = units_of(p.max_kv);
     if (items * longest > INT_MAX)
         return -1;
-    // whole items: as many warps to each as the SMs have for it, and as it has steps
+    // Whole items: as many warps to each as the SMs have for it, and as it has steps.  They save the join and the walk over
+    // lengths, 2 to 5 us, and cost what the longest item takes its warps above an even share.  128 short requests of 2 heads
+    // 7.0 us instead of 12.8 split, 300 of 8 heads of up to 150 keys 22.2 instead of 27.4, 32 of 4 heads of up to 2,000 keys
+    // 16.7 instead of 19.1; but with one warp to an item 128 of 8 heads of up to 400 keys (25 tiles) 27.7 instead of 23.9, and
+    // where half of the SMs would have none, one request of 4 heads of 1,500 keys (8 tiles to a warp) 12.0 instead of 9.4.
     const int64_t rounds = (items + sm_count - 1) / sm_count, steps = (longest + S::kTiles - 1) / S::kTiles;
     int64_t warps = rounds < S::kWarps ? S::kWarps / rounds : 1;
     if (warps > steps)
         warps = steps;
     if (p.unsplit)
         warps = S::kWarps;
-    else if (longest <= kWholeTiles * warps)
+    else if (longest <= (items * 2 >= sm_count ? 12 : 4) * warps)
         p.unsplit = 1;
     p.joined = !p.unsplit;
     if (p.unsplit) {
@@ -957,8 +974,8 @@ int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
     plan.by_items.set(plan.items);
     plan.by_warps.set(plan.warps);
     plan.by_ctas.set(plan.ctas);
-    // two parts of a block, one of each warp
-    return p.unsplit ? 0 : (int64_t)sizeof(float) * (parts_at(plan.ctas) + (2 + warps) * plan.ctas * kPartFloats<D, S::R>);
+    // two parts of a block
+    return p.unsplit ? 0 : (int64_t)sizeof(float) * (parts_at(plan.ctas) + (int64_t)2 * plan.ctas * kPartFloats<D, S::R>);
 }
 
 }  // namespace
