@@ -7,7 +7,7 @@
 // Bytes to numbers.  E4M3 lies within binary16, so keys and values become binary16 without loss on their way
 // from the load to the tensor core.  A key's scale is a factor of its scores; a value's one goes into its
 // weight, w_j = 2^(s_j - m) 2^(7 - E) scale_j with 2^E the largest scale so far, so that weights are at most 2^15 and one is
-// rounded to nothing only below 2^-32 of the largest.  A bf16 q is scaled to binary16 by a power of two
+// rounded to nothing only below 2^-32 of the largest (for fp16 outputs a weight is two numbers).  A bf16 q is scaled to binary16 by a power of two
 // for each row.
 //
 // Shares.  A tile is a group of 16 tokens.  Every warp has a contiguous run of tiles of its own, shared out
@@ -133,6 +133,9 @@ struct Rows {
 template <typename T, int D, int NT>
 struct Warp {
     static constexpr int R = 8 * NT, C = D / 64;
+    // Numbers to a weight.  One binary16 would cost an fp16 output as much as its own rounding (3.1e-4 of it, 2-norm, instead
+    // of 2.1e-4, which the output's alone makes); the second product takes 2 to 3 % of the time, 10 % with 16 rows.
+    static constexpr int H = std::is_same<T, __half>::value ? 2 : 1;
     uint32_t q[C * 4][NT][2];
     float factor[NT][2];          // of scores, beside the keys' scale
     float m[NT][2], l[NT][2];
@@ -244,7 +247,7 @@ struct Warp {
 
     // the scores of N tiles into weights, as the second product's operand; scale: of the tiles' values
     template <int N>
-    __device__ __forceinline__ void weights(const float (&s)[N][NT][4], const float (&scale)[N], uint32_t (&w)[N][NT][2])
+    __device__ __forceinline__ void weights(const float (&s)[N][NT][4], const float (&scale)[N], uint32_t (&w)[N][NT][H][2])
     {
         float x[NT][2];
         bool more = false;
@@ -304,15 +307,23 @@ struct Warp {
                     y[i] = ex2(s[a][n][i] - m[n][i & 1]);
                     l[n][i & 1] += y[i];
                 }
-                w[a][n][0] = transposed(narrow<__half>(y[0] * by, y[1] * by));
-                w[a][n][1] = transposed(narrow<__half>(y[2] * by, y[3] * by));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float y0 = y[2 * i] * by, y1 = y[2 * i + 1] * by;
+                    const uint32_t z = narrow<__half>(y0, y1);
+                    w[a][n][0][i] = transposed(z);
+                    if constexpr (H == 2) {
+                        const float2 f = widen<__half>(z);
+                        w[a][n][1][i] = transposed(narrow<__half>(y0 - f.x, y1 - f.y));
+                    }
+                }
             }
         }
     }
 
     // sums of a tile: v[i] the bytes [g D/8, + D/8) of the tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
     template <int N>
-    __device__ __forceinline__ void sums(const uint32_t (&v)[4][N], const uint32_t (&w)[NT][2])
+    __device__ __forceinline__ void sums(const uint32_t (&v)[4][N], const uint32_t (&w)[NT][H][2])
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -324,10 +335,12 @@ struct Warp {
             const uint32_t b0 = e4m3_to_f16(x1), b1 = e4m3_to_f16_high(x1), b2 = e4m3_to_f16(y1),
                            b3 = e4m3_to_f16_high(y1);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                mma(o[2 * i][n], a0, a1, a2, a3, w[n][0], w[n][1]);
-                mma(o[2 * i + 1][n], b0, b1, b2, b3, w[n][0], w[n][1]);
-            }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    mma(o[2 * i][n], a0, a1, a2, a3, w[n][h][0], w[n][h][1]);
+                    mma(o[2 * i + 1][n], b0, b1, b2, b3, w[n][h][0], w[n][h][1]);
+                }
         }
     }
 
@@ -493,7 +506,7 @@ __device__ __forceinline__ void step(Warp<T, D, NT> &w, const uint8_t *at, const
     constexpr int C = D / 64, N = S::kTiles;
     const int g = lane >> 2, t = lane & 3;
     float s[N][NT][4], v_scale[N];
-    uint32_t x[N][NT][2];
+    uint32_t x[N][NT][Warp<T, D, NT>::H][2];
     // a 128-byte row's 16-byte chunk c lies at c ^ (row & 7)
     const int k_row = D == 128 ? g : g & 6, k_chunk = D == 128 ? 2 * t : (g & 1) * 4 + t;
 #pragma unroll

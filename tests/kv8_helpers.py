@@ -177,9 +177,10 @@ def attended(q, k, v, scale, dtype):
     lost = q.abs().amax(dim=2)[..., None] * k.abs().sum(dim=2)[:, None] * scale * 2.0 ** -39
     ds = ((d + 6) * 2.0 ** -23 * size + lost).amax(dim=2) + 2.0 ** -20 * (1 + s.abs().amax(dim=2))
     total = n * 2.0 ** -23
-    # a weight rounded to binary16: 2^-11 of it, or 2^-32 of the largest, times the largest scale (a value is at most
-    # 448 of its own, and 1 / l is at most the largest weight's share)
+    # a weight is one binary16 number (2^-11 of it), for fp16 two (2^-22 of it, and a step of the sum), or 2^-32 of the
+    # largest off, times the largest scale (a value is at most 448 of its own, and 1 / l is at most the largest weight's share)
+    weight = 2.0 ** -11 if dtype == "bf16" else 2.0 ** -21
     mag = torch.einsum("agn,and->agd", w, v.abs())
     small = 2.0 ** -32 * n * 448.0 * v.abs().amax(dim=(1, 2))[:, None, None]
-    do = (2.0 ** -11 + 2 * ds[..., None] + 2 * total) * mag + U[dtype] * o.abs() * (1 + 2.0 ** -7) + small + TINY[dtype]
+    do = (weight + 2 * ds[..., None] + 2 * total) * mag + U[dtype] * o.abs() * (1 + 2.0 ** -7) + small + TINY[dtype]
     return o, lse, do, ds + total

@@ -626,3 +626,80 @@ def test_a_resumed_request(dev, heads, kv_heads, d, page, dtype, layout):
             want, _, bound, _ = attended(x, k, v, d ** -0.5, dtype)
             assert ((o1[0].double().cpu().reshape(want.shape) - want).abs() <= bound).all()
     assert err.item() == 0
+
+
+def test_pages_beyond_4_gib(dev):
+    """The same keys in the last blocks of a large cache and in a small one: bytes, what is read back and answers."""
+    heads, hk, d, page, n = 4, 2, 128, 256, 600
+    g = torch.Generator().manual_seed(40)
+    x = torch.randn(n, (heads + 2 * hk) * d, generator=g).bfloat16().to(dev)
+    w = x.shape[1]
+    rope, pos, got = hs.hs_rope_plan(d, hs.HS_ROPE_HALF, **PLAIN), torch.arange(n, device=dev), []
+    size = hs.hs_kv8_block_bytes(shape_of(1, heads, hk, d, page, 1, 3, "bf16"))
+    many = (5 << 30) // size
+    for blocks, ids in ((4, [2, 0, 3]), (many, [many - 1, many - 7, many - 2])):
+        shape = shape_of(1, heads, hk, d, page, blocks, 3, "bf16", q_stride=w)
+        cache = torch.zeros(blocks, size, dtype=torch.uint8, device=dev)
+        table = torch.tensor([ids], dtype=torch.int32, device=dev)
+        slots = table[0, pos // page].long() * page + pos % page
+        err, q = fresh_err(dev), x.clone()
+        hs.hs_kv8_append_rope(shape, rope, q, q[:, heads * d:], q[:, (heads + hk) * d:], w, pos, slots, n, q, w, cache, err)
+        out = torch.zeros(3, 2, page, hk, d, dtype=torch.bfloat16, device=dev)
+        lens = torch.tensor([n], dtype=torch.int32, device=dev)
+        hs.hs_kv8_read(shape, cache, table, lens, n, out, 3, torch.tensor([[0, 1, 2]], dtype=torch.int32, device=dev), err)
+        need = hs.hs_kv8_decode_workspace_bytes(shape, n)
+        ws, o = torch.empty(max(need, 16), dtype=torch.uint8, device=dev), torch.empty(1, heads * d, dtype=torch.bfloat16, device=dev)
+        hs.hs_kv8_decode(shape, q[n - 1:], cache, table, lens, n, o, None, ws, need, err)
+        torch.cuda.synchronize()
+        assert err.item() == 0
+        got.append((cache[torch.tensor(ids, device=dev)].cpu(), out.cpu(), o.cpu(), q.cpu()))
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("heads,d,dtype", [(2, 64, "bf16"), (1, 128, "fp16")])
+def test_decode_of_a_long_context(dev, heads, d, dtype):
+    lens = [200_003, 17]
+    c, table = filled(41, lens, 1, 256, d)
+    q = rows_of(42, 2, heads * d, 0, DT[dtype], dev)
+    for unsplit in (False, True):
+        o, z, err = decoded(dev, c, table, q, heads, dtype, lens, 200_003, unsplit=unsplit)
+        assert err == 0
+        near(c, table, q, heads, dtype, lens, o, z, d ** -0.5)
+
+
+def test_decode_without_a_key(dev):
+    c, table = filled(43, [0, 0, 0], 2, 16, 128)
+    q = rows_of(44, 3, 4 * 128, 0, torch.bfloat16, dev)
+    for bound in (0, 16):
+        o, z, err = decoded(dev, c, table, q, 4, "bf16", [0, 0, 0], bound)
+        assert err == 0 and (o == 0).all() and (z == -math.inf).all()
+
+
+def test_calls_on_two_streams_at_once(dev):
+    """Each with its own workspace and cache: the bits of the calls one by one."""
+    cases = []
+    for seed, lens, heads, hk in ((50, [3000, 5, 900], 8, 2), (51, [2500] * 4, 16, 1)):
+        c, table = filled(seed, lens, hk, 16, 128)
+        shape = shape_of(len(lens), heads, hk, 128, 16, c.blocks, table.shape[1], "bf16")
+        bound = table.shape[1] * 16
+        size = hs.hs_kv8_decode_workspace_bytes(shape, bound)
+        q = rows_of(seed, len(lens), heads * 128, 0, torch.bfloat16, dev)
+        cases.append(dict(shape=shape, q=q.to(dev), cache=c.image().to(dev), table=table.to(dev), size=size, bound=bound,
+                          lens=torch.tensor(lens, dtype=torch.int32, device=dev),
+                          ws=torch.empty(size, dtype=torch.uint8, device=dev),
+                          o=[torch.zeros(len(lens), heads * 128, dtype=torch.bfloat16, device=dev) for _ in range(13)]))
+
+    def run(x, i, stream=None):
+        hs.hs_kv8_decode(x["shape"], x["q"], x["cache"], x["table"], x["lens"], x["bound"], x["o"][i], None, x["ws"], x["size"],
+                         None, stream)
+    for x in cases:
+        run(x, 0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for i in range(1, 13):
+        for x, s in zip(cases, streams):
+            run(x, i, s)
+    torch.cuda.synchronize()
+    for x in cases:
+        assert all(torch.equal(y, x["o"][0]) for y in x["o"][1:])

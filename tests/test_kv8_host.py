@@ -228,6 +228,14 @@ def test_read_arguments(kw, code):
     refused(read, kw, code)
 
 
+def test_caches_beyond_31_bits_of_rows():
+    """65 rows of 128 bytes to a block: the decode step counts them in 31 bits, the other calls do not."""
+    big = (1 << 31) // 65 + 1
+    refused(decode, dict(sh=shape(num_blocks=big)), UNS)
+    refused(decode, dict(sh=shape(num_blocks=big - 1), q=None), INV)
+    refused(append, dict(sh=shape(num_blocks=big), k=None), INV)
+
+
 def test_empty_calls_touch_nothing():
     apply(n_rows=0, pos=None)
     apply(n_rows=0, q=None, q_out=None, k=None, k_out=None)
