@@ -970,12 +970,11 @@ int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
         const int64_t most = sm_count * (S::kWarps / warps);
         plan.ctas = (int)(items < most ? items : most);
     } else {
-        // a block to each SM, with a warp to each step where there are few
-        const int64_t all = items * steps;
+        // A block to each SM, fewer where they would not be full: a step to a warp.  One request of one KV head and 8,000 keys
+        // 9.3 us in 16 blocks of 16 warps, 12.4 in 152 of two, whose many parts are joined.
+        const int64_t all = (items * steps + S::kWarps - 1) / S::kWarps;
         plan.ctas = (int)(all < sm_count ? all : sm_count);
-        warps = (all + sm_count - 1) / sm_count;
-        if (warps > S::kWarps)
-            warps = S::kWarps;
+        warps = S::kWarps;
     }
     plan.warps = (int)warps;
     // about two parts to a warp of the join
