@@ -17,6 +17,7 @@
  *   hs_restore_kv_page_slices / hs_save_kv_page_slices: the same for one tensor-parallel
  *                                      rank's heads of every page.
  * The attention of the full-attention layers over the restored pages is in hs_attn.h.
+ * Rotary positions and an 8-bit cache for them are in hs_kv8.h.
  *
  * Conventions shared by every call
  *   - Every call returns hs_status.  HS_OK means the arguments passed host-side
