@@ -43,7 +43,7 @@ typedef enum hs_rope_scaling {
 typedef struct hs_rope {
     int32_t dims;       /* the first dims elements of a head are turned; a multiple of 16, at most head_dim */
     int32_t layout;     /* hs_rope_layout */
-    double amplitude;   /* factor of the turned elements, > 0 and finite (1: lengths are kept) */
+    double amplitude;   /* factor of the turned elements, 2^-64 to 2^64 (1: lengths are kept) */
     double theta[HS_ROPE_MAX_PAIRS]; /* angle of pair i for each position, in radians; finite */
 } hs_rope;
 
@@ -67,7 +67,7 @@ typedef struct hs_rope {
  *   factor     >= 1 and finite (HS_ROPE_PLAIN ignores it)
  *   context    tokens that the unscaled positions were trained for, >= 1 (TURNS and INDEX alone)
  *   low, high  turns, 0 < low < high, finite (TURNS and INDEX alone)
- *   amplitude  > 0 and finite
+ *   amplitude  2^-64 to 2^64
  * Errors: HS_ERR_INVALID_ARG, HS_ERR_UNSUPPORTED (dims).
  */
 hs_status hs_rope_plan(int32_t dims, int32_t layout, double base, int32_t scaling, double factor,
@@ -145,7 +145,7 @@ hs_status hs_kv8_append(const hs_attn_shape *shp, const void *k, const void *v, 
  * launch.
  *
  * k's turned values are not rounded to the element type in between: scales and bytes are those of the exactly turned
- * keys (what float32 leaves open is decided in float64).  Rows with a negative slot
+ * keys (what float32 leaves open is decided with twice its bits).  Rows with a negative slot
  * are skipped altogether: their row of q_out is not written.  A row whose slot is out of range is turned into q_out.
  *   in_stride  elements between rows of q, k and v, a multiple of 8; 0: each one's own heads * head_dim
  *   q_out      as hs_rope_apply (in place is fine); q and q_out may both be NULL

@@ -26,15 +26,22 @@ inline bool positive(double x)
     return x > 0.0 && std::isfinite(x);
 }
 
+// products of values, scales and these stay finite and normal in 32 bits
+inline bool usable_amplitude(double x)
+{
+    return x >= 0x1p-64 && x <= 0x1p64;
+}
+
 hs_status check_rope(const hs_rope *rope, int32_t head_dim, hs::RopeParams &p)
 {
     if (rope == nullptr || (rope->layout != HS_ROPE_HALF && rope->layout != HS_ROPE_INTERLEAVED) ||
-        rope->dims < 1 || rope->dims > head_dim || !positive(rope->amplitude))
+        rope->dims < 1 || rope->dims > head_dim || !usable_amplitude(rope->amplitude))
         return HS_ERR_INVALID_ARG;
     if (rope->dims % 16 != 0)
         return HS_ERR_UNSUPPORTED;
     std::memset(&p, 0, sizeof p);
-    p.amplitude = rope->amplitude;
+    p.gain = (float)rope->amplitude;
+    p.gain_low = (float)(rope->amplitude - p.gain);
     p.pairs = rope->dims / 2;
     p.layout = rope->layout;
     for (int i = 0; i < p.pairs; ++i) {
@@ -187,7 +194,7 @@ hs_status hs_rope_plan(int32_t dims, int32_t layout, double base, int32_t scalin
     const bool by_turns = scaling == HS_ROPE_TURNS || scaling == HS_ROPE_INDEX;
     if (out == nullptr || dims < 1 || (layout != HS_ROPE_HALF && layout != HS_ROPE_INTERLEAVED) ||
         scaling < HS_ROPE_PLAIN || scaling > HS_ROPE_INDEX || !positive(base) || base <= 1.0 ||
-        !positive(amplitude) || (scaling != HS_ROPE_PLAIN && !(positive(factor) && factor >= 1.0)) ||
+        !usable_amplitude(amplitude) || (scaling != HS_ROPE_PLAIN && !(positive(factor) && factor >= 1.0)) ||
         (by_turns && (context < 1 || !positive(low) || !positive(high) || low >= high)))
         return HS_ERR_INVALID_ARG;
     if (dims % 16 != 0 || dims > 2 * HS_ROPE_MAX_PAIRS)

@@ -12,12 +12,12 @@
 // lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
 //
 // Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 31.0 us, 5.7 TB/s; with
-// positions and 32 heads of q, 22,647 rows 90 us, 5.7 TB/s; 14,494 rows of 16 + 4 heads 33.8 us, 4.8.  A step of 64 rows
-// with positions takes 5.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
+// positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.9 us, 5.3.  A step of 64 rows
+// with positions takes 4.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
 //
 // Turned values are good to 2^-21 of |x| + |y|: the angle is good to 2^-25 half turns, sines and cosines to 2^-24, and four
 // more roundings follow (sum 2^-21.3).  What lies nearer than that to a border, of two scales or of two E4M3 numbers, is
-// decided by its float64 value, so that the bytes are those of the exactly turned keys.
+// decided by its value in twice as many bits, so that the bytes are those of the exactly turned keys.
 #include "attn_ptx.cuh"
 #include "kv8_internal.cuh"
 
@@ -29,21 +29,73 @@ using namespace kv8;
 constexpr int kThreads = 128;
 constexpr float kOff = 0x1p-21f;
 
-// The turned pair (x, y) exactly (float64): what lies next to a border of rounding is decided by it.
-__device__ __noinline__ double2 turned_exactly(uint64_t turns, int64_t pos, double amplitude, float x, float y)
+// The upper half of a product of 64 bits, to 2 units: what the lower halves carry is left out.
+__device__ __forceinline__ uint64_t upper(uint64_t a, uint64_t b)
 {
-    double s, c;
-    sincospi((double)angle_of(turns, pos) * 0x1p-63, &s, &c);
-    return make_double2(amplitude * (x * c - y * s), amplitude * (y * c + x * s));
+    const uint32_t ah = a >> 32, bh = b >> 32;
+    return (uint64_t)ah * bh + __umulhi(ah, (uint32_t)b) + __umulhi((uint32_t)a, bh);
 }
 
-// a double as a float that E4M3 rounds to the same number: nearest, but never onto a midpoint that it is not
-__device__ __forceinline__ float toward(double x)
+// A number as high + low, to 2^-47 of it.
+struct Two {
+    float high, low;
+};
+
+// magnitude 2^-63, with a sign
+__device__ __forceinline__ Two two_of(uint64_t magnitude, bool negative)
 {
-    const float f = (float)x;
-    if ((__float_as_uint(f) & 0x7ffff) == 0 && (double)f != x)
-        return __uint_as_float(__float_as_uint(f) + ((double)fabsf(f) < fabs(x) ? 1 : -1));
-    return f;
+    const float sign = negative ? -1.f : 1.f;
+    return {(float)(uint32_t)(magnitude >> 39) * (0x1p-24f * sign),
+            (float)((uint32_t)(magnitude >> 15) & 0xffffffu) * (0x1p-48f * sign)};
+}
+
+// Element `second` of the pair (x, y) times `by` turned, to 2^-45 of |x| + |y|: what lies next to a border of rounding is
+// decided by it.  The angle's sine and cosine are Taylor's series of at most an eighth of a turn in integers of 64 bits
+// (to 2^-54), which need neither tables nor the float64 units: with those a step of 64 rows took 5.1 us, not 4.1.
+__device__ __noinline__ Two turned_closely(int64_t angle, Two gain, float x, float y, float by, bool second)
+{
+    // angle = quarter 2^62 + r, -2^61 <= r <= 2^61
+    const uint64_t a = (uint64_t)angle, quarter = (a + (1ull << 61)) >> 62, r = a - (quarter << 62);
+    const bool below = (int64_t)r < 0;
+    // of 2^64: the angle in radians, and its square
+    const uint64_t t = 2 * upper((below ? -r : r) << 2, 0xc90fdaa22168c235ull), u = upper(t, t);
+    uint64_t s = 0xd73f9f, c = 0xd73fa;                // 1 / 15!, 1 / 16!
+    s = 0xb092309dull - upper(u, s);                   // 1 / 13!
+    c = 0xc9cba54ull - upper(u, c);                    // 1 / 14!
+    s = 0x6b99159fd5ull - upper(u, s);                 // and so on
+    c = 0x8f76c77fcull - upper(u, c);
+    s = 0x2e3bc74aad8eull - upper(u, s);
+    c = 0x49f93edde28ull - upper(u, c);
+    s = 0xd00d00d00d00dull - upper(u, s);
+    c = 0x1a01a01a01a02ull - upper(u, c);
+    s = 0x222222222222222ull - upper(u, s);
+    c = 0x5b05b05b05b05bull - upper(u, c);
+    s = 0x2aaaaaaaaaaaaaabull - upper(u, s);
+    c = 0xaaaaaaaaaaaaaabull - upper(u, c);
+    c = 0x8000000000000000ull - upper(u, c);
+    s = (t - upper(t, upper(u, s))) >> 1;              // of 2^63
+    c = (1ull << 63) - (upper(u, c) >> 1);
+    // cos, sin of quarters 0 to 3: (c, s), (-s, c), (-c, -s), (s, -c)
+    const bool odd = quarter & 1, high = quarter & 2;
+    const Two cosine = two_of(odd ? s : c, odd ? below == high : high),
+              sine = two_of(odd ? c : s, odd ? high : below != high);
+    // p cos + q sin, the products' and the sum's errors added behind
+    const float p = by * (second ? y : x), q = by * (second ? x : -y);
+    const float f = p * cosine.high, g = q * sine.high, h = f + g, k = h - f;
+    const float l = ((f - (h - k)) + (g - k)) + (fmaf(p, cosine.high, -f) + fmaf(q, sine.high, -g)) +
+                    (p * cosine.low + q * sine.low);
+    const float m = h * gain.high, n = fmaf(h, gain.high, -m) + (h * gain.low + l * gain.high);
+    const float sum = n == 0.f ? m : m + n;            // a zero keeps its sign
+    return {sum, n - (sum - m)};
+}
+
+// a float that E4M3 rounds to the same number as x: nearest, but never onto a midpoint that it is not
+__device__ __forceinline__ float toward(Two x)
+{
+    const uint32_t bits = __float_as_uint(x.high);
+    if ((bits & 0x7ffff) == 0 && x.low != 0.f)
+        return __uint_as_float(bits + ((x.low > 0.f) == (x.high > 0.f) ? 1 : -1));
+    return x.high;
 }
 
 // 448 2^e is 1.75 2^(e + 8): the e of the smallest 2^e >= x / 448, for the bits of a float x > 0
@@ -74,11 +126,10 @@ __device__ __forceinline__ void bytes_of(const Pairs &p, uint32_t (&w)[4])
     }
 }
 
-// where the byte of x (or y) of pair j lies
-template <bool kHalf>
-__device__ __forceinline__ int byte_of(int j, int y)
+// 2^-e of 2^e, -126 <= e <= 126
+__device__ __forceinline__ float inverse(float power)
 {
-    return kHalf ? j + 8 * y : 2 * j + y;
+    return __uint_as_float(0x7f000000u - __float_as_uint(power));
 }
 
 // what a warp needs of the group whose rows it quantises
@@ -161,7 +212,7 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
             }
         top = __reduce_max_sync(0xffffffffu, top);
     }
-    const float by = 1.f / settle<D>(g, exponent_of(__float_as_uint(widen<T>(top).x)), lane);
+    const float by = inverse(settle<D>(g, exponent_of(__float_as_uint(widen<T>(top).x)), lane));
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         const int i = s * kAtOnce + sub, token = __shfl_sync(0xffffffffu, g.spot, i);
@@ -251,26 +302,30 @@ struct Team {
         lane_vectors(v, rope.pairs, kHalf, a, b);
         Spins spins;
         const int64_t pos = on ? __ldg(p.pos + row) : 0;
-        const uint4 *const from = p.k + row * p.kv_stride;
+        // the next head's rows, bytes and scale
+        const uint4 *from = p.k + row * p.kv_stride + slice * (D / 8);
         const int shift = p.cache.page_shift - 4;
+        float *scale_next;
+        uint8_t *at_next = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * slice, &scale_next);
+        const int64_t at_step = 2 * p.slices * plane_bytes<D>(p.cache);
+        const int scale_step = 2 * p.slices << shift;
         uint4 next[2];
         float next_old;
-        auto fetch = [&](int head) {
+        auto fetch = [&]() {
             next[0] = next[1] = make_uint4(0, 0, 0, 0);
             if (on) {
-                next[0] = __ldcs(from + head * (D / 8) + a);
-                next[1] = __ldcs(from + head * (D / 8) + b);
+                next[0] = __ldcs(from + a);
+                next[1] = __ldcs(from + b);
             }
-            float *scale;
-            group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * head, &scale);
-            next_old = *scale;
+            next_old = *scale_next;
+            from += p.slices * (D / 8);
         };
-        fetch(slice);
+        fetch();
         if (turned && on) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), (float)rope.amplitude),
-                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), (float)rope.amplitude);
+                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), rope.gain),
+                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), rope.gain);
                 spins.c[k] = ptx::pair(f.x, g.x);
                 spins.s[k] = ptx::pair(f.y, g.y);
             }
@@ -279,24 +334,29 @@ struct Team {
         for (int head = slice; head < p.cache.n_kv; head += p.slices) {
             const Pairs in = pairs_of<T, kHalf>(next[0], next[1]);
             const float old = next_old;
-            float *scale_at;
-            uint8_t *const at = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * head,
-                                            &scale_at);
+            float *const scale_at = scale_next;
+            uint8_t *const at = at_next;
+            scale_next += scale_step;
+            at_next += at_step;
             if (head + p.slices < p.cache.n_kv)
-                fetch(head + p.slices);
+                fetch();
             Pairs x = in;
             if (turned && on)
                 hs::kv8::turn(x, spins);
-            // the exact values of pair j
-            auto exactly = [&](int j) {
-                float px = 0.f, py = 0.f;
+            // element `second` of pair j times f, closely
+            auto closely = [&](int j, bool second, float f) {
+                auto of = [&](const uint64_t (&z)[4]) {
+                    float one[4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float2 ix = ptx::unpair(in.x[k / 2]), iy = ptx::unpair(in.y[k / 2]);
-                    px = k == j ? (k & 1 ? ix.y : ix.x) : px;
-                    py = k == j ? (k & 1 ? iy.y : iy.x) : py;
-                }
-                return turned ? turned_exactly(rope.turns[8 * v + j], pos, rope.amplitude, px, py) : make_double2(px, py);
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 w = ptx::unpair(z[k]);
+                        one[k] = j & 1 ? w.y : w.x;
+                    }
+                    const float low = j & 2 ? one[1] : one[0], high = j & 2 ? one[3] : one[2];
+                    return j & 4 ? high : low;
+                };
+                return turned_closely(angle_of(rope.turns[8 * v + j], pos), Two{rope.gain, rope.gain_low}, of(in.x), of(in.y), f,
+                                      second);
             };
             float top = 0.f;
 #pragma unroll
@@ -320,26 +380,28 @@ struct Team {
             int e = exponent_of(bits);
             // |x| + |y| is at most twice the largest turned value, and 2^-20 of that 15 steps
             if (abs((int)(bits & 0x7fffffu) - 0x600000) <= 16) {
-                const float close = __uint_as_float(bits) * (1.f - 0x1p-18f);
-                const double border = __uint_as_float((bits & 0x7f800000u) | 0x600000u);
+                e = (int)(bits >> 23) - 127 - 8;
+                const float close = __uint_as_float(bits) * (1.f - 0x1p-18f), by = inverse(power_of_two(e < -126 ? -126 : e));
                 bool above = false;
 #pragma unroll 1
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 16; ++j) {
                     float y = 0.f;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float2 f = ptx::unpair(x.x[k / 2]), g = ptx::unpair(x.y[k / 2]);
-                        y = k == j ? fmaxf(fabsf(k & 1 ? f.y : f.x), fabsf(k & 1 ? g.y : g.x)) : y;
+                        const float2 f = ptx::unpair(k < 4 ? x.x[k % 4] : x.y[k % 4]);
+                        y = k == j >> 1 ? fabsf(j & 1 ? f.y : f.x) : y;
                     }
                     if (!on || !(y >= close))
                         continue;
-                    const double2 z = exactly(j);
-                    above = above || fabs(z.x) > border || fabs(z.y) > border;
+                    // elements that are not turned are what they are
+                    const Two z = turned ? closely(j & 7, j >> 3, by) : Two{y * by, 0.f};
+                    above = above || (fabsf(z.high) - 448.f) + (z.high > 0.f ? z.low : -z.low) > 0.f;
                 }
                 __syncwarp();
-                e = (int)(bits >> 23) - 127 - 8 + largest(above);
+                e += largest(above);
             }
-            const float need = power_of_two(e < -126 ? -126 : e), scale = anew ? need : fmaxf(old, need), by = 1.f / scale;
+            const float need = power_of_two(e < -126 ? -126 : e), scale = anew ? need : fmaxf(old, need),
+                        by = inverse(scale);
             if (i == 0 && v == 0)
                 *scale_at = scale;
             if (!anew && need > old && !((tokens >> i) & 1)) {
@@ -357,8 +419,8 @@ struct Team {
                 const uint64_t by2 = ptx::pair(by, by);
                 uint32_t byte[4];
                 if (turned) {
-                    const float off = kOff * (float)rope.amplitude * by;
-                    quantise_turned(x, in, by2, ptx::pair(off, off), by, exactly, byte);
+                    const float off = kOff * rope.gain * by;
+                    quantise_turned(x, in, by2, ptx::pair(off, off), by, top == 0.f, closely, byte);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -375,10 +437,10 @@ struct Team {
         }
     }
 
-    // turned values times by2 as bytes; off2 times |x| + |y| of `in` is how far they may be off
-    template <typename Exactly>
+    // turned values times by2 as bytes; off2 times |x| + |y| of `in` is how far they may be off; zeros: all are
+    template <typename Closely>
     __device__ __forceinline__ static void quantise_turned(const Pairs &x, const Pairs &in, uint64_t by2, uint64_t off2, float by,
-                                                           Exactly exactly, uint32_t (&w)[4])
+                                                           bool zeros, Closely closely, uint32_t (&w)[4])
     {
         constexpr uint64_t kAbs = 0x7fffffff7fffffffull, kSign = 0x8000000080000000ull;
         Pairs low, high;
@@ -393,34 +455,29 @@ struct Team {
         uint32_t z[4];
         bytes_of<kHalf>(low, w);
         bytes_of<kHalf>(high, z);
-        // values that go to two numbers by what they may be off
+        // values that go to two numbers by what they may be off; not -0, to -0 and 0
 #pragma unroll 1
-        while (((w[0] ^ z[0]) | (w[1] ^ z[1]) | (w[2] ^ z[2]) | (w[3] ^ z[3])) != 0) {
+        while (!zeros && ((w[0] ^ z[0]) | (w[1] ^ z[1]) | (w[2] ^ z[2]) | (w[3] ^ z[3])) != 0) {
             const uint64_t first = (uint64_t)(w[1] ^ z[1]) << 32 | (w[0] ^ z[0]);
             const int byte = first != 0 ? (__ffsll(first) - 1) / 8
                                         : 8 + (__ffsll((uint64_t)(w[3] ^ z[3]) << 32 | (w[2] ^ z[2])) - 1) / 8;
-            const int j = kHalf ? byte & 7 : byte >> 1;
-            const double2 q = exactly(j);
-            const uint32_t r = to_e4m3(fabsf((float)q.x) < INFINITY ? toward(q.x * by) : NAN,
-                                       fabsf((float)q.y) < INFINITY ? toward(q.y * by) : NAN, 0.f, 0.f);
+            const Two q = closely(kHalf ? byte & 7 : byte >> 1, kHalf ? byte >> 3 : byte & 1, by);
+            const uint32_t mask = 0xffu << 8 * (byte & 3), put = to_e4m3(toward(q), 0.f, 0.f, 0.f) << 8 * (byte & 3);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = byte_of<kHalf>(j, h);
-                const uint32_t mask = 0xffu << 8 * (at & 3), put = (r >> 8 * h & 0xff) << 8 * (at & 3);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (k == at >> 2) {
-                        w[k] = (w[k] & ~mask) | put;
-                        z[k] = (z[k] & ~mask) | put;
-                    }
-            }
+            for (int k = 0; k < 4; ++k)
+                if (k == byte >> 2) {
+                    w[k] = (w[k] & ~mask) | put;
+                    z[k] = (z[k] & ~mask) | put;
+                }
         }
     }
 };
 
-// Blocks: the turned keys' teams, which take longest; warps for the other planes' heads; q.
+// Blocks: the turned keys' teams, which take longest; warps for the other planes' heads; q.  With positions 24 warps share an
+// SM (80 registers, a few of them spilled) where four meet for a head, 14,494 rows of 4 x 128 32.7 us, 36.4 with 16 warps;
+// 16 where two do, 12,000 rows of 16 x 64 35.3 us, 40.4 with 24.
 template <typename T, int D, bool kRope, bool kHalf>
-__global__ void __launch_bounds__(kThreads, kRope ? 6 : 8)
+__global__ void __launch_bounds__(kThreads, kRope ? (D == 64 ? 4 : 6) : 8)
 kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ RopeParams rope)
 {
     using Keys = Team<T, D, kHalf>;
@@ -494,12 +551,16 @@ cudaError_t launch(Kv8Append p, const RopeParams *rope, int sm_count, cudaStream
     p.windows = (int)((p.n_rows + p.window - 1) / p.window);
     // About three groups' planes for every warp that an SM holds: 28,913 rows of 8 x 128 take 31.0 us so, 34.8 with one (a
     // warp waits for a group's rows one after the other).  Beside turned keys, whose teams are the longer part and
-    // share the SM, one: 14,494 rows of 16 + 4 x 128 33.8 us, 38.3 with three.
+    // share the SM, one: 14,494 rows of 16 + 4 x 128 30.9 us, the same with two; 28,000 of 32 + 8 x 128 106.7, 107.7.
     p.parts = shared_by((rope != nullptr ? 1 : 2) * p.cache.n_kv, p.windows, (int64_t)sm_count * (rope != nullptr ? 32 : 96));
     p.warp_blocks = (p.windows * p.parts + kThreads / 32 - 1) / (kThreads / 32);
     int64_t blocks = p.warp_blocks;
     if (rope != nullptr) {
-        p.slices = shared_by(p.cache.n_kv, p.windows, (int64_t)sm_count * 8 * kTeams);
+        // Teams of up to 8 heads, so that sines and cosines are worth it (14,494 rows of 4 heads 30.9 us, 32.7 with 2 to
+        // a team) and the last wave stays short (12,000 rows of 16 heads 51.7 us, 59.4 with all in a team); of
+        // fewer where there are not four to an SM (1,000 rows of 8 heads 8.6 us so, 10.4 with two).
+        const int64_t teams = (int64_t)sm_count * 4 * kTeams, eights = (int64_t)p.windows * ((p.cache.n_kv + 7) / 8);
+        p.slices = shared_by(p.cache.n_kv, p.windows, teams > eights ? teams : eights);
         p.team_blocks = (p.windows * p.slices + kTeams - 1) / kTeams;
         blocks += p.team_blocks;
         if (p.q != nullptr) {

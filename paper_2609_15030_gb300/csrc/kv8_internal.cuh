@@ -14,7 +14,7 @@ namespace hs {
 // position, so that a position's angle is an integer product modulo 2^64, without loss at any position.
 struct RopeParams {
     uint64_t turns[HS_ROPE_MAX_PAIRS];
-    double amplitude;
+    float gain, gain_low;         // the amplitude as a sum of two numbers
     int32_t pairs;                // dims / 2
     int32_t layout;
 };
@@ -307,8 +307,8 @@ __device__ __forceinline__ void turn_rows(const RopeRows &p, const RopeParams &r
         if (h0 == slice && turned) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), (float)rope.amplitude),
-                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), (float)rope.amplitude);
+                const float2 f = spin_of(angle_of(rope.turns[8 * v + 2 * k], pos), rope.gain),
+                             g = spin_of(angle_of(rope.turns[8 * v + 2 * k + 1], pos), rope.gain);
                 spins.c[k] = ptx::pair(f.x, g.x);
                 spins.s[k] = ptx::pair(f.y, g.y);
             }

@@ -290,6 +290,52 @@ def test_a_turned_key_at_a_border(dev):
             assert scales[i].item() == want, i
 
 
+def at_nothing(dev, y, rope, x, slots, pos):
+    w, n = y.hk * y.d, len(slots)
+    xd = x.to(dev)
+    hs.hs_kv8_append_rope(y.shape, rope, None, xd, xd[:, w:], x.shape[1], torch.tensor(pos, device=dev),
+                          torch.tensor(slots, device=dev), n, None, 0, y.cache, y.err)
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("amplitude", [0, -64, 64])          # powers of two: the bytes are those of 1
+@pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
+def test_keys_at_position_zero_are_rounded_as_they_are(dev, layout, amplitude, d, dtype):
+    """Position 0 turns by nothing, so that keys that lie halfway between two bytes stay there: one in 16 of bf16."""
+    rope = hs.hs_rope_plan(d, layout, 10000.0, hs.HS_ROPE_PLAIN, 1.0, 1, 1.0, 2.0, 2.0 ** amplitude)
+    y, n, w = Layer(dev, 2, d, 16, dtype, 6), 61, 2 * d
+    x = rows_of(5, n, 2 * w, 0, DT[dtype], dev)[:n]
+    slots = list(range(16, 16 + n))
+    at_nothing(dev, y, rope, x, slots, [0] * n)
+    z = x.double().reshape(n, 2, 2, d)
+    z[:, 0] *= 2.0 ** amplitude
+    y.ref.append(z, slots)
+    y.check()
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+def test_zeros_turned(dev, layout):
+    """Rows of zeros among others, groups of zeros, pairs of zeros: zeros, of either sign."""
+    rope = hs.hs_rope_plan(128, layout, 10000.0)
+    y, n, w = Layer(dev, 1, 128, 32, "bf16", 8), 200, 128
+    x = rows_of(6, n, 2 * w, 0, torch.bfloat16, dev)[:n]
+    x[3], x[32:64], x[70:75, :w] = 0.0, 0.0, -0.0
+    x[100:, 7:9], x[100:, 64 + 7:64 + 9] = 0.0, -0.0
+    slots, pos = list(range(n)), list(range(1000, 1000 + n))
+    at_nothing(dev, y, rope, x, slots, pos)
+    z = x.double().reshape(n, 2, 1, 128)
+    z[:, 0] = turned(rope, z[:, 0], pos)[0]
+    y.ref.append(z, slots)
+    unsigned = y.ref.bytes.clone()
+    got = y.cache.cpu()
+    m = unsigned[0].numel()
+    flat = got[:, :m]
+    got[:, :m] = torch.where(flat == 128, torch.zeros_like(flat), flat)
+    y.ref.bytes = torch.where(unsigned == 128, torch.zeros_like(unsigned), unsigned)
+    y.cache = got
+    y.check()
+
+
 # ---- reading back ------------------------------------------------------------------------
 
 READ = [(4, 128, 16, "bf16", [300, 0, 1, 16, 17, 999]), (2, 64, 32, "fp16", [31, 33]), (8, 128, 32, "fp16", [2000]),

@@ -265,3 +265,15 @@ def test_the_tests_own_rounding():
         mid = (a + c) / 2
         for x, want in ((mid, b + b % 2), (mid + (c - a) / 64, b + 1), (mid - (c - a) / 64, b)):
             assert to_e4m3(VALUES.new_tensor([x])).item() == want, (b, x)
+
+
+@pytest.mark.parametrize("amplitude", [2.0 ** -65, 2.0 ** 65, 1e-300, 1e300, math.inf])
+@pytest.mark.parametrize("call", [apply, append_rope])
+def test_amplitudes_that_float32_does_not_hold(call, amplitude):
+    with pytest.raises(hs.HsError) as e:
+        plan(amplitude=amplitude)
+    assert e.value.status == INV
+    with pytest.raises(hs.HsError) as e:
+        call(rope=bent(amplitude=amplitude))
+    assert e.value.status == INV
+    assert plan(amplitude=2.0 ** -64).amplitude == 2.0 ** -64 and plan(amplitude=2.0 ** 64).amplitude == 2.0 ** 64
