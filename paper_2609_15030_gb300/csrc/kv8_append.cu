@@ -11,7 +11,7 @@
 // 16 rows in registers, so that M and the bytes come from one read.  Keys that are turned are taken by teams of D threads, a
 // lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
 //
-// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 31.0 us, 5.7 TB/s; with
+// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 31.3 us, 5.7 TB/s; with
 // positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.9 us, 5.3.  A step of 64 rows
 // with positions takes 4.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
 //
@@ -236,29 +236,54 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
     }
 }
 
-// The groups that begin in a window of rows: lane l of each warp has the slot and the group of row `first` + l.
+// The groups that begin in a window of 16 rows: lane l of each warp has the slot of row `first` + l, -1 if it is left out.
 struct Window {
-    int64_t first, slot, group;
+    int64_t first, slot;
     unsigned begins;              // lanes whose row begins a group
     __device__ __forceinline__ Window(const Kv8Append &p, int64_t row, bool complain, int lane) : first(row - 1)
     {
         const int64_t mine = first + lane;
         slot = mine >= 0 && mine < p.n_rows ? __ldg(p.slots + mine) : -1;
-        const bool far = slot >= p.cache.num_blocks << p.cache.page_shift;
-        if (far && complain && lane > 0 && lane <= p.window)
-            report(p.d_err, HS_DEVERR_BLOCK_OOB);
-        group = slot < 0 || far ? -1 : slot / kGroup;
-        const int64_t before = __shfl_up_sync(0xffffffffu, group, 1);
-        begins = __ballot_sync(0xffffffffu, lane >= 1 && lane <= p.window && group >= 0 && group != before);
+        if (slot >= p.cache.num_blocks << p.cache.page_shift) {
+            if (complain && lane > 0 && lane <= kGroup)
+                report(p.d_err, HS_DEVERR_BLOCK_OOB);
+            slot = -1;
+        }
+        slot = slot < 0 ? -1 : slot;
+        const int64_t before = __shfl_up_sync(0xffffffffu, group(), 1);
+        begins = __ballot_sync(0xffffffffu, lane >= 1 && lane <= kGroup && slot >= 0 && group() != before);
     }
+    __device__ __forceinline__ int64_t group() const { return slot >> 4; }
     // rows of the group that begins with lane l's
     __device__ __forceinline__ int rows(int l) const
     {
-        const unsigned other = ~(__ballot_sync(0xffffffffu, group == __shfl_sync(0xffffffffu, group, l)) >> l);
+        const unsigned other = ~(__ballot_sync(0xffffffffu, group() == __shfl_sync(0xffffffffu, group(), l)) >> l);
         const int n = __ffs(other) - 1;
         return n < 0 || n > kGroup ? kGroup : n;
     }
 };
+
+// Who shares a window takes a run of its (group, plane) pairs, the planes of a group one after the other: of a prompt's window
+// one group's, of a step's up to 16 groups'.  f(lane whose row begins the group, its planes `from` up to `to`).  Windows of
+// fewer rows, of which most begin nothing in a prompt, took 4.5 us for 1,000 rows of 8 x 128, not 3.9.
+template <typename F>
+__device__ __forceinline__ void share(unsigned begins, int planes, int part, int parts_log, F f)
+{
+    const int all = __popc(begins) * planes;
+    int from = part * all >> parts_log, to = (part + 1) * all >> parts_log;
+    if (from == to)
+        return;
+    // the groups in front of the run's first
+    const int lane = threadIdx.x & 31, rank = __popc(begins & ((1u << lane) - 1));
+    const unsigned left = __ballot_sync(0xffffffffu, (begins >> lane & 1) && (rank + 1) * planes > from);
+    const int skipped = (__popc(begins) - __popc(left)) * planes;
+    begins = left;
+    from -= skipped;
+    to -= skipped;
+#pragma unroll 1
+    for (; to > 0; begins &= begins - 1, from = 0, to -= planes)
+        f(__ffs(begins) - 1, from, to < planes ? to : planes);
+}
 
 // Keys that are turned.  A team of D threads takes a group, a lane 16 values of one row, so that a lane keeps its pairs'
 // sines and cosines, and the turned values, while it goes through the heads with the next one's rows on their way.
@@ -289,11 +314,11 @@ struct Team {
         return x;
     }
 
-    // one group's rows of the heads slice, slice + slices, ...
-    __device__ __forceinline__ void group(const Window &w, int l, int slice)
+    // one group's rows of the heads first to end - 1
+    __device__ __forceinline__ void group(const Window &w, int l, int first, int end)
     {
         const int n = w.rows(l);
-        const int64_t id = __shfl_sync(0xffffffffu, w.group, l), row = w.first + l + i;
+        const int64_t id = __shfl_sync(0xffffffffu, w.slot, l) >> 4, row = w.first + l + i;
         const int spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
         const unsigned tokens = __reduce_or_sync(0xffffffffu, lane < n ? 1u << spot : 0u);
         const int token = (int)(__shfl_sync(0xffffffffu, w.slot, (l + i) & 31) & (kGroup - 1));
@@ -303,12 +328,12 @@ struct Team {
         Spins spins;
         const int64_t pos = on ? __ldg(p.pos + row) : 0;
         // the next head's rows, bytes and scale
-        const uint4 *from = p.k + row * p.kv_stride + slice * (D / 8);
+        const uint4 *from = p.k + row * p.kv_stride + first * (D / 8);
         const int shift = p.cache.page_shift - 4;
         float *scale_next;
-        uint8_t *at_next = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * slice, &scale_next);
-        const int64_t at_step = 2 * p.slices * plane_bytes<D>(p.cache);
-        const int scale_step = 2 * p.slices << shift;
+        uint8_t *at_next = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), 2 * first, &scale_next);
+        const int64_t at_step = 2 * plane_bytes<D>(p.cache);
+        const int scale_step = 2 << shift;
         uint4 next[2];
         float next_old;
         auto fetch = [&]() {
@@ -318,7 +343,7 @@ struct Team {
                 next[1] = __ldcs(from + b);
             }
             next_old = *scale_next;
-            from += p.slices * (D / 8);
+            from += D / 8;
         };
         fetch();
         if (turned && on) {
@@ -331,14 +356,14 @@ struct Team {
             }
         }
 #pragma unroll 1
-        for (int head = slice; head < p.cache.n_kv; head += p.slices) {
+        for (int head = first; head < end; ++head) {
             const Pairs in = pairs_of<T, kHalf>(next[0], next[1]);
             const float old = next_old;
             float *const scale_at = scale_next;
             uint8_t *const at = at_next;
             scale_next += scale_step;
             at_next += at_step;
-            if (head + p.slices < p.cache.n_kv)
+            if (head + 1 < end)
                 fetch();
             Pairs x = in;
             if (turned && on)
@@ -488,40 +513,36 @@ kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ R
         if ((int)blockIdx.x < p.team_blocks) {
             const int team = threadIdx.x / Keys::kSize, in_team = threadIdx.x % Keys::kSize;
             const int unit = blockIdx.x * Keys::kCount + team, slice = unit / p.windows;
-            if (slice >= p.slices)
+            if (slice >> p.slices_log)
                 return;
-            const Window w(p, (int64_t)(unit - slice * p.windows) * p.window, false, lane);
+            const Window w(p, (int64_t)(unit - slice * p.windows) * kGroup, false, lane);
             Keys keys{p, rope, tops[team], team, lane, in_team / 32, in_team / Keys::kLanes, in_team % Keys::kLanes};
-#pragma unroll 1
-            for (unsigned left = w.begins; left != 0; left &= left - 1)
-                keys.group(w, __ffs(left) - 1, slice);
+            share(w.begins, p.cache.n_kv, slice, p.slices_log, [&](int l, int from, int to) { keys.group(w, l, from, to); });
             return;
         }
     }
     if ((int)blockIdx.x < p.team_blocks + p.warp_blocks) {
         const int unit = (blockIdx.x - p.team_blocks) * (kThreads / 32) + threadIdx.x / 32, part = unit / p.windows;
         const int planes = (kRope ? 1 : 2) * p.cache.n_kv;            // values alone, or both planes of each head
-        if (part >= p.parts)
+        if (part >> p.parts_log)
             return;
-        const Window w(p, (int64_t)(unit - part * p.windows) * p.window, part == 0, lane);
+        const Window w(p, (int64_t)(unit - part * p.windows) * kGroup, part == 0, lane);
         const int shift = p.cache.page_shift - 4;
-#pragma unroll 1
-        for (unsigned left = w.begins; left != 0; left &= left - 1) {
-            const int l = __ffs(left) - 1;
-            const int64_t id = __shfl_sync(0xffffffffu, w.group, l);
+        share(w.begins, planes, part, p.parts_log, [&](int l, int from, int to) {
+            const int64_t id = __shfl_sync(0xffffffffu, w.slot, l) >> 4;
             Group g;
             g.n = w.rows(l);
             g.spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
             g.tokens = __reduce_or_sync(0xffffffffu, lane < g.n ? 1u << g.spot : 0u);
 #pragma unroll 1
-            for (int x = part; x < planes; x += p.parts) {
+            for (int x = from; x < to; ++x) {
                 const int head_plane = kRope ? 2 * x + 1 : x;
                 g.at = group_at<D>(p.cache, id >> shift, (int)(id & (((int64_t)1 << shift) - 1)), head_plane, &g.scale_at);
                 g.old = *g.scale_at;
                 quantise<T, D>(g, (head_plane & 1 ? p.v : p.k) + (w.first + l) * p.kv_stride + (head_plane >> 1) * (D / 8),
                                p.kv_stride, lane);
             }
-        }
+        });
         return;
     }
     if constexpr (kRope) {
@@ -531,37 +552,41 @@ kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ R
     }
 }
 
-// how many share `all` heads of each of `windows` windows so that there are `wanted` in all
+// the logarithm of how many share up to `all` jobs of each of `windows` windows so that there are `wanted` in all
 int32_t shared_by(int32_t all, int32_t windows, int64_t wanted)
 {
-    int32_t n = 1;
-    while (n < all && (int64_t)windows * n < wanted)
-        n *= 2;
-    return n < all ? n : all;
+    int32_t log = 0;
+    while (1 << log < all && (int64_t)windows << log < wanted)
+        ++log;
+    return log;
 }
 
 template <typename T, int D>
 cudaError_t launch(Kv8Append p, const RopeParams *rope, int sm_count, cudaStream_t s)
 {
     constexpr int kTeams = kThreads / D, kJobs = kThreads / (D / 16);
-    // Few rows may be a decode step's, each a group of its own: windows of one row, and of more where they fill the SMs.
-    p.window = 1;
-    while (p.window < kGroup && p.n_rows >= (int64_t)sm_count * 2 * p.window)
-        p.window *= 2;
-    p.windows = (int)((p.n_rows + p.window - 1) / p.window);
-    // About three groups' planes for every warp that an SM holds: 28,913 rows of 8 x 128 take 31.0 us so, 34.8 with one (a
-    // warp waits for a group's rows one after the other).  Beside turned keys, whose teams are the longer part and
-    // share the SM, one: 14,494 rows of 16 + 4 x 128 30.9 us, the same with two; 28,000 of 32 + 8 x 128 106.7, 107.7.
-    p.parts = shared_by((rope != nullptr ? 1 : 2) * p.cache.n_kv, p.windows, (int64_t)sm_count * (rope != nullptr ? 32 : 96));
-    p.warp_blocks = (p.windows * p.parts + kThreads / 32 - 1) / (kThreads / 32);
+    constexpr int64_t most = INT32_MAX / 4;
+    p.windows = (int)((p.n_rows + kGroup - 1) / kGroup);
+    // 24 warps for each SM (256 rows of 8 x 128, each a group, 4.1 us), or more: one for each plane of a prompt's group
+    // (28,913 rows 31.3 us; 34.8 with fewer, which wait for one group's rows after another).  Beside turned keys, whose teams
+    // are the longer part and share the SM, four (256 rows 6.9 us, 7.3 with eight), or one for each two heads
+    // (12,000 rows of 16 + 16 x 128 52 us, 63 with eight).
+    const int planes = (rope != nullptr ? 1 : 2) * p.cache.n_kv;
+    int64_t warps = (int64_t)sm_count * (rope != nullptr ? 4 : 24);
+    const int64_t prompt = (int64_t)p.windows * (rope != nullptr ? (planes + 1) / 2 : planes);
+    warps = prompt > warps ? prompt : warps;
+    p.parts_log = shared_by(kGroup * planes, p.windows, warps < most ? warps : most);
+    p.warp_blocks = ((p.windows << p.parts_log) + kThreads / 32 - 1) / (kThreads / 32);
     int64_t blocks = p.warp_blocks;
     if (rope != nullptr) {
         // Teams of up to 8 heads, so that sines and cosines are worth it (14,494 rows of 4 heads 30.9 us, 32.7 with 2 to
         // a team) and the last wave stays short (12,000 rows of 16 heads 51.7 us, 59.4 with all in a team); of
-        // fewer where there are not four to an SM (1,000 rows of 8 heads 8.6 us so, 10.4 with two).
-        const int64_t teams = (int64_t)sm_count * 4 * kTeams, eights = (int64_t)p.windows * ((p.cache.n_kv + 7) / 8);
-        p.slices = shared_by(p.cache.n_kv, p.windows, teams > eights ? teams : eights);
-        p.team_blocks = (p.windows * p.slices + kTeams - 1) / kTeams;
+        // fewer where there are not two to an SM (2,000 rows of 8 heads 10.6 us so, 12.0 with four, 12.3 with one).
+        const int64_t eights = (int64_t)p.windows * ((p.cache.n_kv + 7) / 8);
+        int64_t teams = (int64_t)sm_count * 2 * kTeams;
+        teams = eights > teams ? eights : teams;
+        p.slices_log = shared_by(kGroup * p.cache.n_kv, p.windows, teams < most ? teams : most);
+        p.team_blocks = ((p.windows << p.slices_log) + kTeams - 1) / kTeams;
         blocks += p.team_blocks;
         if (p.q != nullptr) {
             p.q_slices = rope_slices(p.n_rows, p.n_heads, sm_count, kJobs);

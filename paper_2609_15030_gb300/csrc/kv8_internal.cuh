@@ -57,8 +57,8 @@ struct Kv8Append {
     int64_t n_rows;
     int32_t *d_err;
     int32_t n_heads;
-    int32_t window, windows;      // rows whose groups a unit begins, and how many of these
-    int32_t slices, parts;        // teams that share a window's turned keys, warps that share its other planes
+    int32_t windows;              // of 16 rows
+    int32_t slices_log, parts_log;   // logarithms: teams that share a window's turned keys, warps for its other planes
     int32_t q_slices;             // threads that share a row's heads of q
     int32_t team_blocks, warp_blocks;   // in front of those for q
 };

@@ -290,7 +290,7 @@ def test_a_turned_key_at_a_border(dev):
             assert scales[i].item() == want, i
 
 
-def at_nothing(dev, y, rope, x, slots, pos):
+def append_keys(dev, y, rope, x, slots, pos):
     w, n = y.hk * y.d, len(slots)
     xd = x.to(dev)
     hs.hs_kv8_append_rope(y.shape, rope, None, xd, xd[:, w:], x.shape[1], torch.tensor(pos, device=dev),
@@ -306,7 +306,7 @@ def test_keys_at_position_zero_are_rounded_as_they_are(dev, layout, amplitude, d
     y, n, w = Layer(dev, 2, d, 16, dtype, 6), 61, 2 * d
     x = rows_of(5, n, 2 * w, 0, DT[dtype], dev)[:n]
     slots = list(range(16, 16 + n))
-    at_nothing(dev, y, rope, x, slots, [0] * n)
+    append_keys(dev, y, rope, x, slots, [0] * n)
     z = x.double().reshape(n, 2, 2, d)
     z[:, 0] *= 2.0 ** amplitude
     y.ref.append(z, slots)
@@ -322,7 +322,7 @@ def test_zeros_turned(dev, layout):
     x[3], x[32:64], x[70:75, :w] = 0.0, 0.0, -0.0
     x[100:, 7:9], x[100:, 64 + 7:64 + 9] = 0.0, -0.0
     slots, pos = list(range(n)), list(range(1000, 1000 + n))
-    at_nothing(dev, y, rope, x, slots, pos)
+    append_keys(dev, y, rope, x, slots, pos)
     z = x.double().reshape(n, 2, 1, 128)
     z[:, 0] = turned(rope, z[:, 0], pos)[0]
     y.ref.append(z, slots)
@@ -333,6 +333,37 @@ def test_zeros_turned(dev, layout):
     got[:, :m] = torch.where(flat == 128, torch.zeros_like(flat), flat)
     y.ref.bytes = torch.where(unsigned == 128, torch.zeros_like(unsigned), unsigned)
     y.cache = got
+    y.check()
+
+
+@pytest.mark.parametrize("times", [1, 30])
+@pytest.mark.parametrize("kv_heads,d,dtype,dims", [(3, 64, "bf16", 64), (1, 128, "fp16", 32), (9, 128, "bf16", 128),
+                                                   (24, 64, "fp16", 16)])
+def test_steps_beside_prompts(dev, kv_heads, d, dtype, dims, times):
+    """Single tokens, short runs and prompts in one call: windows of rows that begin 16 groups, some and none."""
+    g = torch.Generator().manual_seed(kv_heads)
+    runs = [1] * 20 + [2, 3, 40, 1, 17, 5, 1, 1, 33, 16, 16, 1] * times + [1] * 17
+    slots, at = [], 0
+    for n in runs:
+        at = -(-at // G) * G
+        first = at + int(torch.randint(0, G, (1,), generator=g))
+        slots += list(range(first, first + n))
+        at = first + n
+        if n == 5:
+            slots.append(-1)
+    n, w = len(slots), kv_heads * d
+    y = Layer(dev, kv_heads, d, 32, dtype, -(-at // 32) + 1)
+    held = sorted({s // G * G for s in slots if s >= 0})
+    y.append(8, [b + i for b in held for i in range(G)], loud=0.5)
+    y.append(9, slots)
+    y.check()
+    rope = hs.hs_rope_plan(dims, 0, 10000.0)
+    x = rows_of(10, n, 2 * w, 0, DT[dtype], dev, loud=3.0)[:n]
+    pos = torch.randint(0, 70000, (n,), generator=g).tolist()
+    append_keys(dev, y, rope, x, slots, pos)
+    z = x.double().reshape(n, 2, kv_heads, d)
+    z[:, 0] = turned(rope, z[:, 0], pos)[0]
+    y.ref.append(z, slots)
     y.check()
 
 
