@@ -43,7 +43,7 @@ typedef enum hs_rope_scaling {
 typedef struct hs_rope {
     int32_t dims;       /* the first dims elements of a head are turned; a multiple of 16, at most head_dim */
     int32_t layout;     /* hs_rope_layout */
-    double amplitude;   /* factor of the turned elements, 2^-64 to 2^64 (1: lengths are kept) */
+    double amplitude;   /* factor of the turned elements, 2^-20 to 2^20 (1: lengths are kept) */
     double theta[HS_ROPE_MAX_PAIRS]; /* angle of pair i for each position, in radians; finite */
 } hs_rope;
 
@@ -67,7 +67,7 @@ typedef struct hs_rope {
  *   factor     >= 1 and finite (HS_ROPE_PLAIN ignores it)
  *   context    tokens that the unscaled positions were trained for, >= 1 (TURNS and INDEX alone)
  *   low, high  turns, 0 < low < high, finite (TURNS and INDEX alone)
- *   amplitude  2^-64 to 2^64
+ *   amplitude  2^-20 to 2^20
  * Errors: HS_ERR_INVALID_ARG, HS_ERR_UNSUPPORTED (dims).
  */
 hs_status hs_rope_plan(int32_t dims, int32_t layout, double base, int32_t scaling, double factor,

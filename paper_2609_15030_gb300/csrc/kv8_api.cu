@@ -26,10 +26,10 @@ inline bool positive(double x)
     return x > 0.0 && std::isfinite(x);
 }
 
-// products of values, scales and these stay finite and normal in 32 bits
+// its products with 2^-21 and a scale's inverse, 2^126 at most, have to be finite in 32 bits
 inline bool usable_amplitude(double x)
 {
-    return x >= 0x1p-64 && x <= 0x1p64;
+    return x >= 0x1p-20 && x <= 0x1p20;
 }
 
 hs_status check_rope(const hs_rope *rope, int32_t head_dim, hs::RopeParams &p)

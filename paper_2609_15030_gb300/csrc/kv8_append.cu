@@ -380,8 +380,8 @@ struct Team {
                     const float low = j & 2 ? one[1] : one[0], high = j & 2 ? one[3] : one[2];
                     return j & 4 ? high : low;
                 };
-                return turned_closely(angle_of(rope.turns[8 * v + j], pos), Two{rope.gain, rope.gain_low}, of(in.x), of(in.y), f,
-                                      second);
+                return turned_closely(angle_of(rope.turns[8 * v + j], pos), Two{rope.gain, rope.gain_low}, of(in.x),
+                                      of(in.y), f, second);
             };
             float top = 0.f;
 #pragma unroll
@@ -406,7 +406,8 @@ struct Team {
             // |x| + |y| is at most twice the largest turned value, and 2^-20 of that 15 steps
             if (abs((int)(bits & 0x7fffffu) - 0x600000) <= 16) {
                 e = (int)(bits >> 23) - 127 - 8;
-                const float close = __uint_as_float(bits) * (1.f - 0x1p-18f), by = inverse(power_of_two(e < -126 ? -126 : e));
+                const float close = __uint_as_float(bits) * (1.f - 0x1p-18f);
+                const float by = inverse(power_of_two(e < -126 ? -126 : e));
                 bool above = false;
 #pragma unroll 1
                 for (int j = 0; j < 16; ++j) {
@@ -444,8 +445,9 @@ struct Team {
                 const uint64_t by2 = ptx::pair(by, by);
                 uint32_t byte[4];
                 if (turned) {
-                    const float off = kOff * rope.gain * by;
-                    quantise_turned(x, in, by2, ptx::pair(off, off), by, top == 0.f, closely, byte);
+                    // and two roundings to multiples of 2^-149, where those count
+                    const float off = kOff * rope.gain * by, least = by >= 0x1p100f ? by * 0x1p-148f : 0.f;
+                    quantise_turned(x, in, by2, ptx::pair(off, off), ptx::pair(least, least), by, top == 0.f, closely, byte);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -462,16 +464,18 @@ struct Team {
         }
     }
 
-    // turned values times by2 as bytes; off2 times |x| + |y| of `in` is how far they may be off; zeros: all are
+    // turned values times by2 as bytes; off2 times |x| + |y| of `in`, and least2, is how far
+    // they may be off; zeros: all are
     template <typename Closely>
-    __device__ __forceinline__ static void quantise_turned(const Pairs &x, const Pairs &in, uint64_t by2, uint64_t off2, float by,
-                                                           bool zeros, Closely closely, uint32_t (&w)[4])
+    __device__ __forceinline__ static void quantise_turned(const Pairs &x, const Pairs &in, uint64_t by2, uint64_t off2,
+                                                           uint64_t least2, float by, bool zeros, Closely closely,
+                                                           uint32_t (&w)[4])
     {
         constexpr uint64_t kAbs = 0x7fffffff7fffffffull, kSign = 0x8000000080000000ull;
         Pairs low, high;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint64_t off = ptx::mul2(ptx::add2(in.x[k] & kAbs, in.y[k] & kAbs), off2);
+            const uint64_t off = ptx::fma2(ptx::add2(in.x[k] & kAbs, in.y[k] & kAbs), off2, least2);
             high.x[k] = ptx::fma2(x.x[k], by2, off);
             high.y[k] = ptx::fma2(x.y[k], by2, off);
             low.x[k] = ptx::fma2(x.x[k], by2, off ^ kSign);

@@ -298,7 +298,7 @@ def append_keys(dev, y, rope, x, slots, pos):
 
 
 @pytest.mark.parametrize("layout", [0, 1])
-@pytest.mark.parametrize("amplitude", [0, -64, 64])          # powers of two: the bytes are those of 1
+@pytest.mark.parametrize("amplitude", [0, -20, 20])          # powers of two: the bytes are those of 1
 @pytest.mark.parametrize("d,dtype", [(64, "fp16"), (128, "bf16")])
 def test_keys_at_position_zero_are_rounded_as_they_are(dev, layout, amplitude, d, dtype):
     """Position 0 turns by nothing, so that keys that lie halfway between two bytes stay there: one in 16 of bf16."""
@@ -332,6 +332,30 @@ def test_zeros_turned(dev, layout):
     flat = got[:, :m]
     got[:, :m] = torch.where(flat == 128, torch.zeros_like(flat), flat)
     y.ref.bytes = torch.where(unsigned == 128, torch.zeros_like(unsigned), unsigned)
+    y.cache = got
+    y.check()
+
+
+@pytest.mark.parametrize("amplitude", [2.0 ** -20, 2.0 ** 20])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_smallest_and_largest_values_at_the_ends_of_the_amplitude(dev, amplitude, dtype):
+    """Groups of zeros alone, of the type's smallest and of its largest values, whose scales are at their ends."""
+    rope = hs.hs_rope_plan(64, 0, 10000.0, hs.HS_ROPE_PLAIN, 1.0, 1, 1.0, 2.0, amplitude)
+    y, n, info = Layer(dev, 1, 64, 16, dtype, 4), 64, torch.finfo(DT[dtype])
+    x = rows_of(11, n, 128, 0, DT[dtype], dev)[:n]
+    x[:16, :64] = 0.0
+    x[16:32, :64] = info.smallest_normal * info.eps * torch.randint(0, 3, (16, 64), generator=torch.Generator().manual_seed(0))
+    x[32:48, :64] = (x[32:48, :64].sign().double() * info.max * min(1.0, 1.0 / amplitude) / 2).to(DT[dtype])
+    slots, pos = list(range(n)), [0] * 8 + list(range(1, n - 7))
+    append_keys(dev, y, rope, x, slots, pos)
+    z = x.double().reshape(n, 2, 1, 64)
+    z[:, 0] = turned(rope, z[:, 0], pos)[0]
+    y.ref.append(z, slots)
+    # a zero's sign is not compared
+    got = y.cache.cpu()
+    m = y.ref.bytes[0].numel()
+    got[:, :m] = torch.where(got[:, :m] == 128, torch.zeros_like(got[:, :m]), got[:, :m])
+    y.ref.bytes = torch.where(y.ref.bytes == 128, torch.zeros_like(y.ref.bytes), y.ref.bytes)
     y.cache = got
     y.check()
 

@@ -267,13 +267,13 @@ def test_the_tests_own_rounding():
             assert to_e4m3(VALUES.new_tensor([x])).item() == want, (b, x)
 
 
-@pytest.mark.parametrize("amplitude", [2.0 ** -65, 2.0 ** 65, 1e-300, 1e300, math.inf])
+@pytest.mark.parametrize("amplitude", [2.0 ** -21, 2.0 ** 21, 1e-300, 1e300, math.inf])
 @pytest.mark.parametrize("call", [apply, append_rope])
-def test_amplitudes_that_float32_does_not_hold(call, amplitude):
+def test_amplitudes_out_of_range(call, amplitude):
     with pytest.raises(hs.HsError) as e:
         plan(amplitude=amplitude)
     assert e.value.status == INV
     with pytest.raises(hs.HsError) as e:
         call(rope=bent(amplitude=amplitude))
     assert e.value.status == INV
-    assert plan(amplitude=2.0 ** -64).amplitude == 2.0 ** -64 and plan(amplitude=2.0 ** 64).amplitude == 2.0 ** 64
+    assert plan(amplitude=2.0 ** -20).amplitude == 2.0 ** -20 and plan(amplitude=2.0 ** 20).amplitude == 2.0 ** 20
