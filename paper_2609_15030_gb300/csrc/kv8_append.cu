@@ -11,8 +11,8 @@
 // 16 rows in registers, so that M and the bytes come from one read.  Keys that are turned are taken by teams of D threads, a
 // lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
 //
-// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 31.3 us, 5.7 TB/s; with
-// positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.9 us, 5.3.  A step of 64 rows
+// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 29.7 us, 6.0 TB/s; with
+// positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.4 us, 5.4.  A step of 64 rows
 // with positions takes 4.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
 //
 // Turned values are good to 2^-21 of |x| + |y|: the angle is good to 2^-25 half turns, sines and cosines to 2^-24, and four
@@ -237,13 +237,18 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
 }
 
 // The groups that begin in a window of 16 rows: lane l of each warp has the slot of row `first` + l, -1 if it is left out.
+// `meanwhile` is done while the slots are on their way, given the row behind `first`.
 struct Window {
     int64_t first, slot;
     unsigned begins;              // lanes whose row begins a group
-    __device__ __forceinline__ Window(const Kv8Append &p, int64_t row, bool complain, int lane) : first(row - 1)
+    template <typename F>
+    __device__ __forceinline__ Window(const Kv8Append &p, int64_t row, bool complain, int lane, F meanwhile) : first(row - 1)
     {
         const int64_t mine = first + lane;
-        slot = mine >= 0 && mine < p.n_rows ? __ldg(p.slots + mine) : -1;
+        slot = -1;
+        if (mine >= 0 && mine < p.n_rows)
+            asm volatile("ld.global.nc.b64 %0, [%1];" : "=l"(slot) : "l"(p.slots + mine));
+        meanwhile(row);
         if (slot >= p.cache.num_blocks << p.cache.page_shift) {
             if (complain && lane > 0 && lane <= kGroup)
                 report(p.d_err, HS_DEVERR_BLOCK_OOB);
@@ -262,6 +267,18 @@ struct Window {
         return n < 0 || n > kGroup ? kGroup : n;
     }
 };
+
+// Brings a head's 16 rows from row `first` on to L2 while the slots that say whose they are come: 28,913 rows of 8 x 128 29.7
+// us, 31.3 without; 4,000 of 32 + 8 x 128 with positions 18.7, 19.8.
+template <int D>
+__device__ __forceinline__ void ahead(const Kv8Append &p, const uint4 *head, int64_t first, int lane)
+{
+    constexpr int kLines = D / 64;                     // of 128 bytes to a row
+#pragma unroll
+    for (int i = lane / kLines; i < kGroup; i += 32 / kLines)
+        if (first + i < p.n_rows)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(head + (first + i) * p.kv_stride + lane % kLines * 8));
+}
 
 // Who shares a window takes a run of its (group, plane) pairs, the planes of a group one after the other: of a prompt's window
 // one group's, of a step's up to 16 groups'.  f(lane whose row begins the group, its planes `from` up to `to`).  Windows of
@@ -519,7 +536,12 @@ kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ R
             const int unit = blockIdx.x * Keys::kCount + team, slice = unit / p.windows;
             if (slice >> p.slices_log)
                 return;
-            const Window w(p, (int64_t)(unit - slice * p.windows) * kGroup, false, lane);
+            const Window w(p, (int64_t)(unit - slice * p.windows) * kGroup, false, lane, [&](int64_t first) {
+                // the first two heads that fall to this team where the window begins one group
+                const int head = (slice * p.cache.n_kv >> p.slices_log) + in_team / 32;
+                if (in_team < 64 && head < (slice + 1) * p.cache.n_kv >> p.slices_log)
+                    ahead<D>(p, p.k + head * (D / 8), first, lane);
+            });
             Keys keys{p, rope, tops[team], team, lane, in_team / 32, in_team / Keys::kLanes, in_team % Keys::kLanes};
             share(w.begins, p.cache.n_kv, slice, p.slices_log, [&](int l, int from, int to) { keys.group(w, l, from, to); });
             return;
@@ -530,7 +552,12 @@ kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ R
         const int planes = (kRope ? 1 : 2) * p.cache.n_kv;            // values alone, or both planes of each head
         if (part >> p.parts_log)
             return;
-        const Window w(p, (int64_t)(unit - part * p.windows) * kGroup, part == 0, lane);
+        const Window w(p, (int64_t)(unit - part * p.windows) * kGroup, part == 0, lane, [&](int64_t first) {
+            // the plane that falls to this warp where the window begins one group
+            const int plane = part * planes >> p.parts_log;
+            if (plane < (part + 1) * planes >> p.parts_log)
+                ahead<D>(p, (kRope || (plane & 1) ? p.v : p.k) + (kRope ? plane : plane >> 1) * (D / 8), first, lane);
+        });
         const int shift = p.cache.page_shift - 4;
         share(w.begins, planes, part, p.parts_log, [&](int l, int from, int to) {
             const int64_t id = __shfl_sync(0xffffffffu, w.slot, l) >> 4;
