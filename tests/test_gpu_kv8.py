@@ -391,6 +391,23 @@ def test_steps_beside_prompts(dev, kv_heads, d, dtype, dims, times):
     y.check()
 
 
+@pytest.mark.parametrize("kv_heads,d", [(1024, 64), (511, 128)])
+def test_append_of_the_most_heads(dev, kv_heads, d):
+    slots = [3, 16, 40, 41, 42] + list(range(50, 75)) + [96]
+    n, w = len(slots), kv_heads * d
+    y = Layer(dev, kv_heads, d, 16, "bf16", 7)
+    y.append(11, list(range(7 * 16)), loud=0.5)       # a group that goes on has begun
+    y.append(12, slots)
+    y.append(13, [4, 17, 97], loud=4.0)
+    rope = hs.hs_rope_plan(d, 1, 10000.0)
+    x, pos = rows_of(14, n, 2 * w, 0, torch.bfloat16, dev, loud=9.0)[:n], list(range(500, 500 + n))
+    append_keys(dev, y, rope, x, slots, pos)
+    z = x.double().reshape(n, 2, kv_heads, d)
+    z[:, 0] = turned(rope, z[:, 0], pos)[0]
+    y.ref.append(z, slots)
+    y.check()
+
+
 # ---- reading back ------------------------------------------------------------------------
 
 READ = [(4, 128, 16, "bf16", [300, 0, 1, 16, 17, 999]), (2, 64, 32, "fp16", [31, 33]), (8, 128, 32, "fp16", [2000]),
