@@ -700,7 +700,8 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
                     lost = !ptx::mbar_wait_bounded(p.stall_for_test ? loader.bars + 8 * S::kStages : loader.bars + 8 * stage,
                                                    parity, p.limit_ns);
                     arrived<S::kStages - 2>();
-                    lost = __any_sync(0xffffffffu, lost);    // the scales are there too, and the stage before is free
+                    lost = __any_sync(0xffffffffu, lost);
+                    __syncwarp();                            // all lanes see the scales, and have read the stage before
                     if (lost)
                         break;
                 }
