@@ -7,7 +7,7 @@
 // Bytes to numbers.  E4M3 lies within binary16, so keys and values become binary16 without loss on their way
 // from the load to the tensor core.  A key's scale is a factor of its scores; a value's one goes into its
 // weight, w_j = 2^(s_j - m) 2^(7 - E) scale_j with 2^E the largest scale so far, so that weights are at most 2^15 and one is
-// rounded to nothing only below 2^-32 of the largest (for fp16 outputs a weight is two numbers).  A bf16 q is scaled to binary16 by a power of two
+// rounded to nothing only below 2^-32 of the largest (a weight is the sum of two such numbers).  A bf16 q is scaled to binary16 by a power of two
 // for each row.
 //
 // Shares.  A tile is a group of 16 tokens.  Every warp has a contiguous run of tiles of its own, shared out
@@ -134,8 +134,9 @@ template <typename T, int D, int NT>
 struct Warp {
     static constexpr int R = 8 * NT, C = D / 64;
     // Numbers to a weight.  One binary16 would cost an fp16 output as much as its own rounding (3.1e-4 of it, 2-norm, instead
-    // of 2.1e-4, which the output's alone makes); the second product takes 2 to 3 % of the time, 10 % with 16 rows.
-    static constexpr int H = std::is_same<T, __half>::value ? 2 : 1;
+    // of 2.1e-4, which the output's alone makes), and a bf16 output whose keys' shares cancel several steps.  The second
+    // product takes 2 to 3 % of the time, 4 with heads of 64, 8 with more than 8 rows.
+    static constexpr int H = 2;
     uint32_t q[C * 4][NT][2];
     float factor[NT][2];          // of scores, beside the keys' scale
     float m[NT][2], l[NT][2];
@@ -311,11 +312,9 @@ struct Warp {
                 for (int i = 0; i < 2; ++i) {
                     const float y0 = y[2 * i] * by, y1 = y[2 * i + 1] * by;
                     const uint32_t z = narrow<__half>(y0, y1);
+                    const float2 f = widen<__half>(z);
                     w[a][n][0][i] = transposed(z);
-                    if constexpr (H == 2) {
-                        const float2 f = widen<__half>(z);
-                        w[a][n][1][i] = transposed(narrow<__half>(y0 - f.x, y1 - f.y));
-                    }
+                    w[a][n][1][i] = transposed(narrow<__half>(y0 - f.x, y1 - f.y));
                 }
             }
         }

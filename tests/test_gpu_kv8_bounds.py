@@ -1,0 +1,53 @@
+"""The decode step over the 8-bit cache within bounds that follow its documented roundings one by one
+(tests/kv8_tight.py)."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_15030_gb300 as hs
+from tests.gpu_helpers import device
+from tests.kv8_helpers import DT, filled, keys_of
+from tests.kv8_tight import bounded, one_element_rows
+from tests.test_gpu_kv8 import decoded
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return device()
+
+
+def scale_of(c, table, b, n):
+    """The largest scale of a request's values, by KV head."""
+    pages = table[b, :-(-n // c.page)].long()
+    x = c.scales[pages, :, 1].permute(1, 0, 2).flatten(1)[:, :-(-n // 16)]
+    return x.amax(dim=1)
+
+
+def excess(c, table, q, heads, dtype, b, n, o, z, scale):
+    """How far one request's outputs are beyond their bounds: the largest quotient, of o and of lse."""
+    k, v = keys_of(c, table, b, n)
+    x = q[b, :heads * c.d].double().reshape(c.kv_heads, heads // c.kv_heads, c.d)
+    want, want_z, bound, bound_z = bounded(x, k, v, scale_of(c, table, b, n), scale, dtype)
+    return (((o[b].double().reshape(want.shape) - want).abs() / bound).max().item(),
+            ((z[b].double().reshape(want_z.shape) - want_z).abs() / bound_z).max().item())
+
+
+SHAPES = [(8, 2, 128, 16, "bf16"), (16, 1, 128, 32, "bf16"), (12, 2, 64, 16, "bf16"), (32, 1, 64, 16, "bf16"),
+          (8, 2, 128, 16, "fp16"), (16, 1, 64, 32, "fp16")]
+
+
+@pytest.mark.parametrize("unsplit", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,d,page,dtype", SHAPES)
+def test_weights_keep_more_bits_than_the_outputs(dev, heads, kv_heads, d, page, dtype, unsplit):
+    """Outputs whose keys' shares cancel show what the weights lost."""
+    lens = [2, 3, 5, 9, 17, 40, 100, 333, 1000, 1]
+    c, table = filled(60, lens, kv_heads, page, d)
+    q = one_element_rows(61, len(lens), heads, d, DT[dtype])
+    o, z, err = decoded(dev, c, table, q, heads, dtype, lens, max(lens), scale=0.25, unsplit=unsplit)
+    assert err == 0
+    for b, n in enumerate(lens):
+        over, over_z = excess(c, table, q, heads, dtype, b, n, o, z, 0.25)
+        assert over <= 1 and over_z <= 1, (b, n, over, over_z)
