@@ -126,12 +126,6 @@ __device__ __forceinline__ void bytes_of(const Pairs &p, uint32_t (&w)[4])
     }
 }
 
-// 2^-e of 2^e, -126 <= e <= 126
-__device__ __forceinline__ float inverse(float power)
-{
-    return __uint_as_float(0x7f000000u - __float_as_uint(power));
-}
-
 // what a warp needs of the group whose rows it quantises
 struct Group {
     uint8_t *at;                  // its first token's bytes of the KV head's plane

@@ -39,9 +39,10 @@ namespace hs {
 namespace kv8 {
 namespace {
 
-// floats of a part: per row m and l, then its sums, rows padded against bank conflicts
+// Floats of a part: per row its D sums, then m, l and 2^E, in units of 2^(E - 7) of which the sums are (their own size may
+// be beyond float32 where the average of the values is not), and one that keeps rows apart in the banks.
 template <int D, int R>
-constexpr int kPartFloats = 2 * R + R * (D + 4);
+constexpr int kPartFloats = R * (D + 4);
 
 // The kernel's sizes.  A warp takes a step of kTiles tiles at a time; its steps arrive in a ring of its own in shared
 // memory, kStages - 1 ahead.
@@ -372,11 +373,11 @@ struct Warp {
                 const int r = n * 8 + 2 * t + i;
                 if (r >= rows.n)
                     continue;
-                const float by = l[n][i] == 0.f ? 0.f : top * 0x1p-7f / l[n][i];
+                const float by = l[n][i] == 0.f ? 0.f : 0x1p-7f / l[n][i];
                 uint32_t x[D / 16];
 #pragma unroll
                 for (int j = 0; j < D / 16; ++j)
-                    x[j] = narrow_finite<T>(sum(n, i, 2 * j) * by, sum(n, i, 2 * j + 1) * by);
+                    x[j] = narrow_finite<T>(sum(n, i, 2 * j) * by * top, sum(n, i, 2 * j + 1) * by * top);
                 uint4 *const to = reinterpret_cast<uint4 *>(static_cast<T *>(p.o) + rows.b * p.o_stride +
                                                             (int64_t)(rows.head + r) * D + g * (D / 8));
 #pragma unroll
@@ -391,21 +392,17 @@ struct Warp {
     __device__ __forceinline__ void leave(float *part, int lane) const
     {
         const int g = lane >> 2, t = lane & 3;
-        const float by = top * 0x1p-7f;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int r = n * 8 + 2 * t + i;
-                if (g == 0) {
-                    part[2 * r] = m[n][i];
-                    part[2 * r + 1] = l[n][i];
-                }
-                float4 *const to = reinterpret_cast<float4 *>(part + 2 * R + r * (D + 4) + g * (D / 8));
+                float *const row = part + (n * 8 + 2 * t + i) * (D + 4);
+                if (g == 0)
+                    *reinterpret_cast<float4 *>(row + D) = make_float4(m[n][i], l[n][i], top, 0.f);
+                float4 *const to = reinterpret_cast<float4 *>(row + g * (D / 8));
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j)
-                    to[j] = make_float4(sum(n, i, 4 * j) * by, sum(n, i, 4 * j + 1) * by,
-                                        sum(n, i, 4 * j + 2) * by, sum(n, i, 4 * j + 3) * by);
+                    to[j] = make_float4(sum(n, i, 4 * j), sum(n, i, 4 * j + 1), sum(n, i, 4 * j + 2), sum(n, i, 4 * j + 3));
             }
     }
 };
@@ -575,32 +572,45 @@ __host__ __device__ __forceinline__ int64_t parts_at(int ctas)
     return (int64_t)(ctas + 1) / 2 * 4;            // parts stay 16-byte aligned
 }
 
+// a row's state beside its sums, which are in units of 2^-7 unit
+struct State {
+    float m, l, unit;
+    __device__ __forceinline__ State() : m(-INFINITY), l(0.f), unit(0x1p-126f) {}     // of no tiles
+    __device__ __forceinline__ explicit State(float4 x) : m(x.x), l(x.y), unit(x.z) {}
+    __device__ __forceinline__ operator float4() const { return make_float4(m, l, unit, 0.f); }
+    __device__ __forceinline__ bool none() const { return m == -INFINITY && l == 0.f; }
+};
+
 // one row's result, a lane's columns c to c + 3
 template <typename T, int D>
-__device__ __forceinline__ void write_row(const AttnParams &p, int b, int head, int c, float4 o, float m, float l)
+__device__ __forceinline__ void write_row(const AttnParams &p, int b, int head, int c, float4 o, const State &x)
 {
-    const float by = l == 0.f ? 0.f : 1.f / l;
+    const float by = x.l == 0.f ? 0.f : 0x1p-7f / x.l;
     *reinterpret_cast<uint2 *>(static_cast<T *>(p.o) + b * p.o_stride + (int64_t)head * D + c) =
-        make_uint2(narrow_finite<T>(o.x * by, o.y * by), narrow_finite<T>(o.z * by, o.w * by));
+        make_uint2(narrow_finite<T>(o.x * by * x.unit, o.y * by * x.unit),
+                   narrow_finite<T>(o.z * by * x.unit, o.w * by * x.unit));
     if (c == 0 && p.lse != nullptr)
-        p.lse[(int64_t)b * p.n_heads + head] = 0.6931471805599453f * (m + log2f(l));
+        p.lse[(int64_t)b * p.n_heads + head] = 0.6931471805599453f * (x.m + log2f(x.l));
 }
 
-// Parts of a row joined by a warp: lane i has part i's m and l (-infinity and 0: none), row_of(i, i % kAhead) a lane's four
-// columns of its sums, loaded kAhead at a time.
+// Parts of a row joined by a warp: lane i has part i's state, row_of(i, i % kAhead) a lane's four columns of its sums,
+// loaded kAhead at a time.
 template <int kAhead, typename RowOf>
-__device__ __forceinline__ float4 join(float &m, float &l, int count, RowOf row_of)
+__device__ __forceinline__ float4 join(State &s, int count, RowOf row_of)
 {
-    float top = m;
+    float top = s.m;
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1)
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-    const float h = m == -INFINITY && l == 0.f ? 0.f : ex2(m - top);
-    m = top;
-    l *= h;
+    float h = s.none() ? 0.f : ex2(s.m - top);
+    s.m = top;
+    s.l *= h;
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1)
-        l += __shfl_xor_sync(0xffffffffu, l, x);
+        s.l += __shfl_xor_sync(0xffffffffu, s.l, x);
+    const float unit = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(s.unit)));
+    h *= s.unit * inverse(unit);
+    s.unit = unit;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
     for (int i0 = 0; i0 < count; i0 += kAhead) {
@@ -793,29 +803,25 @@ kv8_decode_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ 
             const Rows<R> rows(p, plan, bb, it - bb * plan.items);
             if (r >= rows.n || (!(starts && ends) && !p.joined))       // the latter: a wait has run out
                 continue;
-            float m = -INFINITY, l = 0.f;
-            if (lane < n) {
-                m = at[2 * r];
-                l = at[2 * r + 1];
-            }
+            at += r * (D + 4);
+            State s;
+            if (lane < n)
+                s = State(*reinterpret_cast<const float4 *>(at + D));
             const int col = lane * 4 % D;                   // 64 columns: the second half of the lanes repeats the first
-            at += 2 * R + r * (D + 4);
-            const float4 o = join<4>(m, l, n, [&](int i, int) {
+            const float4 o = join<4>(s, n, [&](int i, int) {
                 const int from = __shfl_sync(0xffffffffu, (int)(at - heads), i);
                 return *reinterpret_cast<const float4 *>(heads + from + col);
             });
             if (lane * 4 >= D)
                 continue;
             if (starts && ends) {
-                write_row<T, D>(p, bb, rows.head + r, col, o, m, l);
+                write_row<T, D>(p, bb, rows.head + r, col, o, s);
                 continue;
             }
-            float *const to = p.part + parts_at(gridDim.x) + (int64_t)(2 * blockIdx.x + starts) * kPart;
-            *reinterpret_cast<float4 *>(to + 2 * R + r * (D + 4) + col) = o;
-            if (lane == 0) {
-                to[2 * r] = m;
-                to[2 * r + 1] = l;
-            }
+            float *const to = p.part + parts_at(gridDim.x) + (int64_t)(2 * blockIdx.x + starts) * kPart + r * (D + 4);
+            *reinterpret_cast<float4 *>(to + col) = o;
+            if (lane == 0)
+                *reinterpret_cast<float4 *>(to + D) = s;
         }
         if (!p.unsplit) {
             if (threadIdx.x == 0) {
@@ -848,7 +854,7 @@ kv8_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Kv
 {
     constexpr int R = 8 * NT, kPart = kPartFloats<D, R>, kAhead = 4;
     __shared__ float4 sums[kJoinWarps][32];
-    __shared__ float2 pairs[kJoinWarps];
+    __shared__ float4 states[kJoinWarps];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_row = plan.per_row;
     const int r = blockIdx.y * (kJoinWarps / per_row) + warp / per_row, first = warp % per_row;
     const int col = lane * 4 % D;
@@ -858,46 +864,45 @@ kv8_join_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ Kv
         return;
     const int b = plan.by_items.div(x.item);
     const Rows<R> rows(p, plan, b, x.item - b * plan.items);
-    float m = -INFINITY, l = 0.f;
+    State s;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    // up to 32 parts at a time, the sums of the first ones on their way with the pairs
+    // up to 32 parts at a time, the sums of the first ones on their way with the states
     for (int c0 = blockIdx.x + first; r < rows.n && c0 <= x.last; c0 += 32 * per_row) {
         auto at = [&](int i) {
             const int c = c0 + i * per_row;
-            return p.part + parts_at(plan.ctas) + (int64_t)(c == (int)blockIdx.x ? 2 * c + 1 : 2 * c) * kPart;
+            return p.part + parts_at(plan.ctas) + (int64_t)(c == (int)blockIdx.x ? 2 * c + 1 : 2 * c) * kPart + r * (D + 4);
         };
-        auto row = [&](int i) { return *reinterpret_cast<const float4 *>(at(i) + 2 * R + r * (D + 4) + col); };
+        auto row = [&](int i) { return *reinterpret_cast<const float4 *>(at(i) + col); };
         const int count = min(32, (x.last - c0) / per_row + 1);
         float4 ahead[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i)
             ahead[i] = row(min(i, count - 1));
-        float pm = -INFINITY, pl = 0.f;
-        if (lane < count) {
-            pm = at(lane)[2 * r];
-            pl = at(lane)[2 * r + 1];
-        }
-        const float4 y = join<kAhead>(pm, pl, count, [&](int i, int k) { return i < kAhead ? ahead[k] : row(i); });
-        const float top = fmaxf(m, pm), h = m == -INFINITY ? 0.f : ex2(m - top),
-                    hy = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - top);
+        State part;
+        if (lane < count)
+            part = State(*reinterpret_cast<const float4 *>(at(lane) + D));
+        const float4 y = join<kAhead>(part, count, [&](int i, int k) { return i < kAhead ? ahead[k] : row(i); });
+        const float top = fmaxf(s.m, part.m), unit = fmaxf(s.unit, part.unit);
+        float h = s.none() ? 0.f : ex2(s.m - top), hy = part.none() ? 0.f : ex2(part.m - top);
+        s.l = s.l * h + part.l * hy;
+        h *= s.unit * inverse(unit);
+        hy *= part.unit * inverse(unit);
         o.x = o.x * h + y.x * hy, o.y = o.y * h + y.y * hy, o.z = o.z * h + y.z * hy, o.w = o.w * h + y.w * hy;
-        l = l * h + pl * hy;
-        m = top;
+        s.m = top;
+        s.unit = unit;
     }
     if (per_row > 1) {
         sums[warp][lane] = o;
         if (lane == 0)
-            pairs[warp] = make_float2(m, l);
+            states[warp] = s;
         __syncthreads();
         if (first != 0)
             return;
-        const float2 z = lane < per_row ? pairs[warp + lane] : make_float2(-INFINITY, 0.f);
-        m = z.x;
-        l = z.y;
-        o = join<2>(m, l, per_row, [&](int i, int) { return sums[warp + i][lane]; });
+        s = lane < per_row ? State(states[warp + lane]) : State();
+        o = join<2>(s, per_row, [&](int i, int) { return sums[warp + i][lane]; });
     }
     if (r < rows.n && lane * 4 < D)
-        write_row<T, D>(p, b, rows.head + r, col, o, m, l);
+        write_row<T, D>(p, b, rows.head + r, col, o, s);
 }
 
 // The cache as rows of 128 bytes: a copy takes a group of one head's plane, which lands in swizzled rows (16-byte chunk c

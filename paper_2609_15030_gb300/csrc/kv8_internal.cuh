@@ -165,6 +165,12 @@ __device__ __forceinline__ float power_of_two(int e)     // -126 <= e <= 127
     return __int_as_float((e + 127) << 23);
 }
 
+// 2^-e of 2^e, -126 <= e <= 126
+__device__ __forceinline__ float inverse(float power)
+{
+    return __uint_as_float(0x7f000000u - __float_as_uint(power));
+}
+
 // ---- addresses -----------------------------------------------------------------------------
 
 // bytes of one (KV head, plane) of a block

@@ -51,3 +51,21 @@ def test_weights_keep_more_bits_than_the_outputs(dev, heads, kv_heads, d, page, 
     for b, n in enumerate(lens):
         over, over_z = excess(c, table, q, heads, dtype, b, n, o, z, 0.25)
         assert over <= 1 and over_z <= 1, (b, n, over, over_z)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,page", [(4, 2, 128, 16), (12, 1, 128, 32), (3, 1, 64, 16), (20, 2, 64, 16)])
+@pytest.mark.parametrize("e", [119, 112, 96])
+def test_sums_of_large_values_stay_in_range(dev, heads, kv_heads, d, page, e):
+    """Averages far below bf16's largest number whose sums are beyond float32, of either sign, however a row's keys
+    are shared out."""
+    lens = [3000, 1, 17, 250, 40]
+    c, table = filled(62, lens, kv_heads, page, d, spread=0)
+    c.bytes[:, :, 1] = torch.where(c.bytes[:, :, 1] % 128 > 56, c.bytes[:, :, 1] - 16, c.bytes[:, :, 1])   # 448 to 60
+    c.scales[:, :, 1] *= 2.0 ** (e + 8)
+    q = one_element_rows(63, len(lens), heads, d, torch.bfloat16, loud=4.0)
+    for unsplit in (False, True):
+        o, z, err = decoded(dev, c, table, q, heads, "bf16", lens, max(lens), scale=0.25, unsplit=unsplit)
+        assert err == 0
+        for b, n in enumerate(lens):
+            over, over_z = excess(c, table, q, heads, "bf16", b, n, o, z, 0.25)
+            assert over <= 1 and over_z <= 1, (unsplit, b, n, over, over_z)
