@@ -142,7 +142,7 @@ struct Warp {
     float factor[NT][2];          // of scores, beside the keys' scale
     float m[NT][2], l[NT][2];
     float o[D / 16][NT][4];
-    float top;                    // 2^E
+    float top;                    // 2^E, 2^-126 at least
 
     // the queries as they are
     __device__ __forceinline__ static void load(uint32_t (&x)[NT][C][8], const AttnParams &p, const Rows<R> &rows, int lane)
@@ -166,7 +166,7 @@ struct Warp {
     __device__ __forceinline__ void begin(uint32_t (&raw)[NT][C][8], const AttnParams &p, int lane)
     {
         const int t = lane & 3;
-        top = 0x1p-100f;
+        top = 0x1p-126f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             uint32_t (&x)[C][8] = raw[n];
@@ -272,7 +272,7 @@ struct Warp {
             if (most > top) {
                 // a power of two even where the cache's scale is none
                 const float up = __uint_as_float(__float_as_uint(most) & 0x7f800000u);
-                h0 = top / up;
+                h0 = top * inverse(up);
                 top = up;
             }
 #pragma unroll
@@ -297,10 +297,10 @@ struct Warp {
                     }
                 }
         }
-        const float down = 128.f / top;
+        const float down = inverse(top);                   // 128 times it may be beyond float32
 #pragma unroll
         for (int a = 0; a < N; ++a) {
-            const float by = scale[a] * down;
+            const float by = scale[a] * down * 128.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 float y[4];

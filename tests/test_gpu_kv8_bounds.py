@@ -69,3 +69,24 @@ def test_sums_of_large_values_stay_in_range(dev, heads, kv_heads, d, page, e):
         for b, n in enumerate(lens):
             over, over_z = excess(c, table, q, heads, "bf16", b, n, o, z, 0.25)
             assert over <= 1 and over_z <= 1, (unsplit, b, n, over, over_z)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,page", [(8, 2, 128, 16), (16, 1, 128, 16), (6, 2, 64, 32), (12, 1, 64, 16)])
+@pytest.mark.parametrize("e", [-126, -118, -101, -100, -90])
+def test_smallest_scales_keep_the_weights_bits(dev, heads, kv_heads, d, page, e):
+    """Values whose scales are all near the smallest one, alone and in front of larger ones."""
+    lens = [600, 2, 40, 2000, 9]
+    c, table = filled(64, lens, kv_heads, page, d, spread=0)
+    c.scales[:, :, 1] *= 2.0 ** (e + 8)
+    q = one_element_rows(65, len(lens), heads, d, torch.bfloat16)
+    for late in (0, 30):
+        if late:                     # the second half of each request's pages has larger scales
+            for b, n in enumerate(lens):
+                pages = table[b, :-(-n // page)].long()
+                c.scales[pages[len(pages) // 2:], :, 1] *= 2.0 ** late
+        for unsplit in (False, True):
+            o, z, err = decoded(dev, c, table, q, heads, "bf16", lens, max(lens), scale=0.25, unsplit=unsplit)
+            assert err == 0
+            for b, n in enumerate(lens):
+                over, over_z = excess(c, table, q, heads, "bf16", b, n, o, z, 0.25)
+                assert over <= 1 and over_z <= 1, (late, unsplit, b, n, over, over_z)
