@@ -284,7 +284,8 @@ struct Warp {
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
                     float h = 1.f;
-                    if (y > m[n][i]) {
+                    // by the row's own scores, whichever row brought the warp here
+                    if (y > m[n][i] + 8.f) {
                         h = ex2(m[n][i] - y);
                         m[n][i] = y;
                         l[n][i] *= h;

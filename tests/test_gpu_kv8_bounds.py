@@ -90,3 +90,21 @@ def test_smallest_scales_keep_the_weights_bits(dev, heads, kv_heads, d, page, e)
             for b, n in enumerate(lens):
                 over, over_z = excess(c, table, q, heads, "bf16", b, n, o, z, 0.25)
                 assert over <= 1 and over_z <= 1, (late, unsplit, b, n, over, over_z)
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,dtype", [(8, 2, 128, "bf16"), (16, 1, 128, "fp16"), (12, 2, 64, "bf16"),
+                                                    (4, 1, 64, "fp16")])
+def test_unsplit_rows_know_nothing_of_their_groups_other_heads(dev, heads, kv_heads, d, dtype):
+    """A row depends on its own query and its keys: not on what the other heads of its KV head ask."""
+    lens = [900, 64, 2500]
+    c, table = filled(66, lens, kv_heads, 16, d)
+    q = one_element_rows(67, len(lens), heads, d, DT[dtype], loud=2.0)
+    others = one_element_rows(68, len(lens), heads, d, DT[dtype], loud=40.0)
+    group = heads // kv_heads
+    kept = torch.arange(heads) % group == 1
+    mixed = torch.where(kept.repeat_interleave(d), q, others)
+    o, z, _ = decoded(dev, c, table, q, heads, dtype, lens, 2500, scale=0.25, unsplit=True)
+    o1, z1, _ = decoded(dev, c, table, mixed, heads, dtype, lens, 2500, scale=0.25, unsplit=True)
+    assert not torch.equal(o1, o)
+    assert torch.equal(o1.unflatten(1, (heads, d))[:, kept], o.unflatten(1, (heads, d))[:, kept])
+    assert torch.equal(z1[:, kept], z[:, kept])
