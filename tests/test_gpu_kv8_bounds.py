@@ -5,11 +5,10 @@ import math
 import pytest
 import torch
 
-import paper_2609_15030_gb300 as hs
 from tests.gpu_helpers import device
 from tests.kv8_helpers import DT, filled, keys_of
 from tests.kv8_tight import bounded, one_element_rows
-from tests.test_gpu_kv8 import decoded
+from tests.test_gpu_kv8 import DECODE, decoded, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -108,3 +107,81 @@ def test_unsplit_rows_know_nothing_of_their_groups_other_heads(dev, heads, kv_he
     assert not torch.equal(o1, o)
     assert torch.equal(o1.unflatten(1, (heads, d))[:, kept], o.unflatten(1, (heads, d))[:, kept])
     assert torch.equal(z1[:, kept], z[:, kept])
+
+
+# ---- keys that are lost do not meet the bounds ---------------------------------------------
+
+
+def without(c, table, q, heads, dtype, b, n, scale, first, last):
+    """The quotients of the exact outputs of a request without its keys [first, last)."""
+    k, v = keys_of(c, table, b, n)
+    x = q[b, :heads * c.d].double().reshape(c.kv_heads, heads // c.kv_heads, c.d)
+    want, want_z, bound, bound_z = bounded(x, k, v, scale_of(c, table, b, n), scale, dtype)
+    keep = (torch.arange(n) < first) | (torch.arange(n) >= last)
+    s = (torch.einsum("agd,and->agn", x, k) * scale)[:, :, keep]
+    z = torch.logsumexp(s, dim=2)
+    o = torch.einsum("agn,and->agd", (s - z[..., None]).exp(), v[:, keep]).to(DT[dtype]).double()
+    return ((o - want).abs() / bound).max().item(), ((z - want_z).abs() / bound_z).max().item()
+
+
+def mark_tiles(seed, c, table, lens):
+    """Values of 1 or -1 in one column of each tile of 16 keys, 0 elsewhere, and flat scales: a lost tile, or what is left of
+    the last, changes a column by several of its bounds."""
+    g = torch.Generator().manual_seed(seed)
+    c.scales[:, :, 1] = 2.0 ** -3
+    c.bytes[:, :, 1] = 0
+    for b, n in enumerate(lens):
+        t = torch.arange(-(-n // 16))
+        column = (t * 7 + 3) % c.d
+        sign = torch.randint(0, 2, t.shape, generator=g)
+        at = t[:, None] * 16 + torch.arange(16)
+        c.bytes[table[b].long()[at // c.page], :, 1, at % c.page, column[:, None]] = (56 + 128 * sign)[:, None, None]
+
+
+LONG = [(2, 1, 64, 256, "bf16"), (1, 1, 128, 256, "fp16"), (16, 1, 128, 256, "bf16"), (12, 1, 64, 256, "fp16"),
+        (4, 1, 128, 16, "bf16")]
+LONG_LENS = [200_003, 30_000, 4_608, 1_000, 33]
+
+
+def long_case(heads, kv_heads, d, page, dtype):
+    c, table = filled(69, LONG_LENS, kv_heads, page, d)
+    mark_tiles(71, c, table, LONG_LENS)
+    return c, table, one_element_rows(70, len(LONG_LENS), heads, d, DT[dtype])
+
+
+def lost(n):
+    """First and last tiles, one inside, and a block's share of the keys, were the request a call's only one."""
+    inside = n // 2 // 16 * 16
+    return (0, 16), (inside, inside + 16), ((n - 1) // 16 * 16, n), (n // 3, n // 3 + max(-(-n // 152), 16))
+
+
+@pytest.mark.parametrize("heads,kv_heads,d,page,dtype", LONG)
+def test_every_tile_of_a_context_counts(dev, heads, kv_heads, d, page, dtype):
+    """At every length the outputs meet bounds that those without one tile of 16 keys, or one block's share of them, do
+    not meet."""
+    c, table, q = long_case(heads, kv_heads, d, page, dtype)
+    scale = 2.0 ** -6
+    both = [decoded(dev, c, table, q, heads, dtype, LONG_LENS, max(LONG_LENS), scale=scale, unsplit=u) for u in (False, True)]
+    for b, n in enumerate(LONG_LENS):
+        for o, z, err in both:
+            over, over_z = excess(c, table, q, heads, dtype, b, n, o, z, scale)
+            assert err == 0 and over <= 1 and over_z <= 1, (b, n, over, over_z)
+        for first, last in lost(n):
+            over, _ = without(c, table, q, heads, dtype, b, n, scale, first, last)
+            assert over > 1, (n, first, last, over)
+
+
+@pytest.mark.parametrize("unsplit", [False, True])
+@pytest.mark.parametrize("heads,kv_heads,d,page,dtype,lens", DECODE)
+def test_decode_of_dense_queries(dev, heads, kv_heads, d, page, dtype, lens, unsplit):
+    """Every head, page size and length of tests/test_gpu_kv8.py, within the bounds of single roundings."""
+    c, table = filled(72, lens, kv_heads, page, d)
+    q = rows_of(73, len(lens), heads * d, 8, DT[dtype], dev, loud=0.5)
+    o, z, err = decoded(dev, c, table, q, heads, dtype, lens, max(lens), unsplit=unsplit)
+    assert err == 0
+    for b, n in list(enumerate(lens))[:40]:
+        if n == 0:
+            assert (o[b] == 0).all() and (z[b] == -math.inf).all()
+            continue
+        over, over_z = excess(c, table, q, heads, dtype, b, n, o, z, d ** -0.5)
+        assert over <= 1 and over_z <= 1, (b, n, over, over_z)
