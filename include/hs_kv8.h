@@ -44,7 +44,7 @@ typedef struct hs_rope {
     int32_t dims;       /* the first dims elements of a head are turned; a multiple of 16, at most head_dim */
     int32_t layout;     /* hs_rope_layout */
     double amplitude;   /* factor of the turned elements, 2^-20 to 2^20 (1: lengths are kept) */
-    double theta[HS_ROPE_MAX_PAIRS]; /* angle of pair i for each position, in radians; finite */
+    double theta[HS_ROPE_MAX_PAIRS]; /* angle of pair i for each position, in radians; below 2^64 in magnitude */
 } hs_rope;
 
 /*
@@ -87,8 +87,9 @@ hs_status hs_rope_plan(int32_t dims, int32_t layout, double base, int32_t scalin
  *              a fused projection's output are fine.  Either may be NULL: its rows are left out
  *   in_stride  elements between rows of both, a multiple of 8; 0: q's n_heads * head_dim, k's
  *              n_kv_heads * head_dim
- *   pos        device int64 [n_rows]; negative positions turn backwards.  The angle is reduced exactly (in units of
- *              2^-64 turns), so it is as good as theta's 53 bits at any position
+ *   pos        device int64 [n_rows]; negative positions turn backwards.  theta is rounded to a multiple of 2^-64
+ *              turns and the angle reduced exactly, so that it is off by |pos| 2^-65 turns at most (1.5e-9 radians at
+ *              2^33) beside float32's roundings
  *   q_out, q_out_stride, k_out, k_out_stride  device, the results, laid out alike (a stride of 0: the rows touch).
  *              In place is fine: q_out == q with the same stride, k_out == k with the same stride.  They must
  *              not overlap otherwise
@@ -144,8 +145,8 @@ hs_status hs_kv8_append(const hs_attn_shape *shp, const void *k, const void *v, 
  * hs_kv8_append_rope -- hs_rope_apply of q into q_out and hs_kv8_append of the turned k, and of v, in one
  * launch.
  *
- * k's turned values are not rounded to the element type in between: scales and bytes are those of the exactly turned
- * keys (what float32 leaves open is decided with twice its bits).  Rows with a negative slot
+ * k's turned values are not rounded to the element type in between: at positions below 2^39 in magnitude scales and bytes
+ * are those of the exactly turned keys (what float32 leaves open is decided with twice its bits).  Rows with a negative slot
  * are skipped altogether: their row of q_out is not written.  A row whose slot is out of range is turned into q_out.
  *   in_stride  elements between rows of q, k and v, a multiple of 8; 0: each one's own heads * head_dim
  *   q_out      as hs_rope_apply (in place is fine); q and q_out may both be NULL

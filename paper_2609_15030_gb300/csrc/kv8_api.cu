@@ -32,6 +32,42 @@ inline bool usable_amplitude(double x)
     return x >= 0x1p-20 && x <= 0x1p20;
 }
 
+// 1 / (2 pi), in units of 2^-192, the lowest word first
+constexpr uint64_t kTurnsPerRadian[3] = {0x36d8a5664f10e410ull, 0x7f09d5f47d4d3770ull, 0x28be60db9391054aull};
+
+// theta / (2 pi) modulo 1, in units of 2^-96 and to half of one, for |theta| < 2^64: theta is m 2^(e - 53) with integers m and
+// e, so that its product with the constant is one of integers.
+void turns_of(double theta, uint64_t &turns, int32_t &rest)
+{
+    using uint128 = unsigned __int128;
+    int e;
+    const uint64_t m = (uint64_t)std::ldexp(std::frexp(std::fabs(theta), &e), 53);
+    uint64_t product[6] = {};
+    uint128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += (uint128)m * kTurnsPerRadian[i];
+        product[i] = (uint64_t)carry;
+        carry >>= 64;
+    }
+    product[3] = (uint64_t)carry;
+    // from units of 2^(e - 53 - 192) to 2^-96
+    const int down = 149 - e;
+    uint128 x = 0;
+    if (down < 256) {
+        auto bits = [&](int at) {                    // 64 of the product's
+            const int word = at / 64, shift = at % 64;
+            return shift == 0 ? product[word] : product[word] >> shift | product[word + 1] << (64 - shift);
+        };
+        x = (uint128)(down < 192 ? bits(down + 64) : 0) << 64 | bits(down);
+        x += bits(down - 1) & 1;
+    }
+    if (theta < 0.0)
+        x = -x;
+    x += (uint128)1 << 31;
+    turns = (uint64_t)(x >> 32);
+    rest = (int32_t)((uint32_t)x - (1u << 31));
+}
+
 hs_status check_rope(const hs_rope *rope, int32_t head_dim, hs::RopeParams &p)
 {
     if (rope == nullptr || (rope->layout != HS_ROPE_HALF && rope->layout != HS_ROPE_INTERLEAVED) ||
@@ -45,12 +81,9 @@ hs_status check_rope(const hs_rope *rope, int32_t head_dim, hs::RopeParams &p)
     p.pairs = rope->dims / 2;
     p.layout = rope->layout;
     for (int i = 0; i < p.pairs; ++i) {
-        if (!std::isfinite(rope->theta[i]))
+        if (!(std::fabs(rope->theta[i]) < 0x1p64))
             return HS_ERR_INVALID_ARG;
-        double turns = rope->theta[i] / kTurn;
-        turns -= std::floor(turns);
-        turns = turns < 1.0 ? std::ldexp(turns, 64) : 0.0;
-        p.turns[i] = (uint64_t)turns;
+        turns_of(rope->theta[i], p.turns[i], p.rest[i]);
     }
     return HS_OK;
 }

@@ -16,8 +16,9 @@
 // with positions takes 4.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
 //
 // Turned values are good to 2^-21 of |x| + |y|: the angle is good to 2^-25 half turns, sines and cosines to 2^-24, and four
-// more roundings follow (sum 2^-21.3).  What lies nearer than that to a border, of two scales or of two E4M3 numbers, is
-// decided by its value in twice as many bits, so that the bytes are those of the exactly turned keys.
+// more roundings follow (sum 2^-21.3), which leaves room for 2^-23.3 radians that the 64 bits of an angle lack at
+// positions up to 2^39.  What lies nearer than that to a border, of two scales or of two E4M3 numbers, is
+// decided by its value in twice as many bits (of an angle: 96), so that the bytes are those of the exactly turned keys.
 #include "attn_ptx.cuh"
 #include "kv8_internal.cuh"
 
@@ -391,7 +392,7 @@ struct Team {
                     const float low = j & 2 ? one[1] : one[0], high = j & 2 ? one[3] : one[2];
                     return j & 4 ? high : low;
                 };
-                return turned_closely(angle_of(rope.turns[8 * v + j], pos), Two{rope.gain, rope.gain_low}, of(in.x),
+                return turned_closely(angle_of(rope.turns[8 * v + j], rope.rest[8 * v + j], pos), Two{rope.gain, rope.gain_low}, of(in.x),
                                       of(in.y), f, second);
             };
             float top = 0.f;

@@ -10,10 +10,12 @@
 
 namespace hs {
 
-// A model's positions as the kernels take them: pair i turns by turns[i] 2^-64 of a full turn for each
-// position, so that a position's angle is an integer product modulo 2^64, without loss at any position.
+// A model's positions as the kernels take them: pair i turns by turns[i] 2^-64 + rest[i] 2^-96 of a full turn for each
+// position, to half a unit.  So a position's angle is an integer product modulo 2^64, off by |pos| 2^-65 turns at most
+// without the rest and by |pos| 2^-97 + 2^-64 with it.
 struct RopeParams {
     uint64_t turns[HS_ROPE_MAX_PAIRS];
+    int32_t rest[HS_ROPE_MAX_PAIRS];
     float gain, gain_low;         // the amplitude as a sum of two numbers
     int32_t pairs;                // dims / 2
     int32_t layout;
@@ -197,6 +199,12 @@ __device__ __forceinline__ uint8_t *group_at(const Kv8Cache &c, int64_t blk, int
 __device__ __forceinline__ int64_t angle_of(uint64_t turns, int64_t pos)
 {
     return (int64_t)(turns * (uint64_t)pos);
+}
+
+// the same with the rest
+__device__ __forceinline__ int64_t angle_of(uint64_t turns, int32_t rest, int64_t pos)
+{
+    return angle_of(turns, pos) + __mul64hi(pos, (int64_t)rest * (1ll << 32));
 }
 
 // amplitude times (cos, sin) of an angle; its upper 32 bits are kept: 2^-32 of a turn

@@ -2,8 +2,8 @@
 // absolute positions, Section 2.2 of the paper).
 //
 // Pair (x, y) of a head becomes (x c - y s, y c + x s) with c, s = cos, sin of pos theta_i.  An angle is one
-// 64-bit integer product modulo a full turn (RopeParams), so nothing is lost at far positions, where
-// pos theta_i in float32 is off by whole radians; its upper 32 bits go through one sine and cosine.
+// 64-bit integer product modulo a full turn (RopeParams), off by |pos| 2^-65 turns at most, where pos theta_i in
+// float32 is off by whole radians from some 10^7 on; its upper 32 bits go through one sine and cosine.
 //
 // A lane holds 8 pairs of a head: two 16-byte vectors, a head's halves or neighbours by the layout.  It computes
 // their 8 sines and cosines once and takes them through several heads of the row.
