@@ -146,7 +146,9 @@ hs_status hs_kv8_append(const hs_attn_shape *shp, const void *k, const void *v, 
  * launch.
  *
  * k's turned values are not rounded to the element type in between: at positions below 2^39 in magnitude scales and bytes
- * are those of the exactly turned keys (what float32 leaves open is decided with twice its bits).  Rows with a negative slot
+ * are those of the exactly turned keys (what float32 leaves open is decided with twice its bits).  Where a
+ * turned value is beyond float32's range, both of its pair count as not finite; where amplitude times an element is, they
+ * may.  Rows with a negative slot
  * are skipped altogether: their row of q_out is not written.  A row whose slot is out of range is turned into q_out.
  *   in_stride  elements between rows of q, k and v, a multiple of 8; 0: each one's own heads * head_dim
  *   q_out      as hs_rope_apply (in place is fine); q and q_out may both be NULL

@@ -407,8 +407,11 @@ struct Team {
                 top = 0.f;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    // turned, both of a pair: beside one that is too large for float32 the other may be rounding alone
+                    if (turned)
+                        x.x[k] = ptx::fma2(x.y[k], 0, x.x[k]);
+                    x.y[k] = ptx::fma2(turned ? x.x[k] : x.y[k], 0, x.y[k]);
                     x.x[k] = ptx::fma2(x.x[k], 0, x.x[k]);
-                    x.y[k] = ptx::fma2(x.y[k], 0, x.y[k]);
                     const float2 f = ptx::unpair(x.x[k]), g = ptx::unpair(x.y[k]);
                     top = fmaxf(fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y))), fmaxf(fabsf(g.x), fabsf(g.y)));
                 }

@@ -127,3 +127,26 @@ def test_angles_backwards_are_those_of_positions_backwards(dev):
     for r, p, o in ((rope, -pos, out[0]), (back, pos, out[1])):
         hs.hs_rope_apply(shape, r, x, None, 0, p, 300, o, 0, None, 0)
     assert torch.equal(out[0], out[1])
+
+
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("amplitude,size", [(1.0, 3e38), (2.0 ** 20, 2.0 ** 107 * 1.5)])
+def test_turned_keys_beyond_float32_count_as_not_finite(dev, layout, amplitude, size):
+    """One pair of equal elements at an eighth of a turn: one turned value is sqrt 2 of its size, and the other, which is near 0,
+    rounding alone."""
+    rope = hs.hs_rope_plan(64, layout, 10000.0, amplitude=amplitude)
+    n, pair = 40, 5
+    rope.theta[pair] = math.pi / 4
+    at = [(pair, pair + 32), (2 * pair, 2 * pair + 1)][layout]
+    y = Layer(dev, 1, 64, 16, "bf16", 3)
+    x = rows_of(85, n, 128, 0, torch.bfloat16, dev)[:n]
+    x[3, list(at)] = x[20, list(at)] = size
+    pos = [0] * n
+    pos[3] = pos[20] = 1
+    append_keys(dev, y, rope, x, list(range(n)), pos)
+    z = x.double().reshape(n, 2, 1, 64)
+    z[:, 0] = exactly(rope, z[:, 0], pos)[0]
+    assert size * amplitude < torch.finfo(torch.float32).max < z[3, 0, 0, at[1]] == z[20, 0, 0, at[1]]
+    z[3, 0, 0, list(at)] = z[20, 0, 0, list(at)] = math.nan
+    y.ref.append(z, list(range(n)))
+    y.check()
