@@ -131,8 +131,8 @@ hs_status hs_kv8_block_bytes(const hs_attn_shape *shp, int64_t *bytes_out);
  * New values are divided by the scale and rounded to the nearest E4M3 number (ties to even).  So a value is
  * off by at most 2^-4 of itself, or by 2^-10 of the scale where that is more, and once more for each time that its
  * group's scale grew: at most 16 times in all, since a group has 16 tokens.
- * The rows of a group must stand one behind the other (in any order), as the new tokens of a request do, and
- * slots >= 0 must be distinct: else the group's values mean nothing.  A value that is not finite becomes
+ * The rows of a group must stand within 16 rows (in any order), with none but skipped rows among them, as the new tokens of
+ * a request do, and slots >= 0 must be distinct: else the group's values mean nothing.  A value that is not finite becomes
  * NaN and takes no part in M.
  * k, v and the cache must be 16-byte aligned and must not overlap.
  * Errors: as hs_kv_append.

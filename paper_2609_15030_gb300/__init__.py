@@ -543,7 +543,8 @@ def hs_kv8_block_bytes(shape: hs_attn_shape) -> int:
 
 def hs_kv8_append(shape: hs_attn_shape, k, v, kv_stride: int, slots, n_rows: int, cache, d_err=None,
                   stream=None):
-    """slots as in hs_kv_append; the rows of a group of 16 tokens stand one behind the other."""
+    """slots as in hs_kv_append; the rows of a group of 16 tokens stand within 16 rows, none but skipped
+    ones among them."""
     rc = (_lib or load()).hs_kv8_append(
         C.byref(shape), _ptr(k), _ptr(v), int(kv_stride), _ptr(slots), int(n_rows), _ptr(cache),
         _ptr(d_err), _stream(stream))

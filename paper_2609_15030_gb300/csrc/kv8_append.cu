@@ -6,8 +6,8 @@
 // bytes that the group holds are rounded to the new scale), bytes = E4M3(x / scale).  With powers of two
 // both divisions are exact, so each value is rounded once for each scale that it lives under.
 //
-// The rows of a group stand one behind the other: its first row's place (the row in front has another group)
-// says who owns it.  Values and keys that are not turned are taken by warps, a (KV head, plane) of a group at a time with its
+// The rows of a group stand one behind the other, but for skipped ones: its first row's place (the last row in front that is
+// not skipped has another group) says who owns it.  Values and keys that are not turned are taken by warps, a (KV head, plane) of a group at a time with its
 // 16 rows in registers, so that M and the bytes come from one read.  Keys that are turned are taken by teams of D threads, a
 // lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
 //
@@ -133,7 +133,8 @@ struct Group {
     float *scale_at;
     float old;
     unsigned tokens;              // that get rows
-    int n, spot;                  // rows; lane i: the token of row i
+    unsigned rows;                // of the 16 from the first one on
+    int spot;                     // lane i: the token of row i
 };
 
 // Settles the group's scale, rounds what it holds to it where it grows, and gives the scale.
@@ -172,12 +173,13 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
     constexpr int kLanes = D / 16, kAtOnce = 32 / kLanes, kSteps = kGroup / kAtOnce;
     constexpr uint32_t kInf = std::is_same<T, __half>::value ? 0x7c00 : 0x7f80;
     const int v = lane % kLanes, sub = lane / kLanes;
+    const unsigned on = g.rows >> sub;
     uint4 in[kSteps][2];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         const int i = s * kAtOnce + sub;
         in[s][0] = in[s][1] = make_uint4(0, 0, 0, 0);
-        if (i < g.n) {
+        if (on & (1u << s * kAtOnce)) {
             in[s][0] = __ldcs(from + i * stride + v);
             in[s][1] = __ldcs(from + i * stride + v + kLanes);
         }
@@ -211,7 +213,7 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         const int i = s * kAtOnce + sub, token = __shfl_sync(0xffffffffu, g.spot, i);
-        if (i >= g.n)
+        if (!(on & (1u << s * kAtOnce)))
             continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -231,7 +233,8 @@ __device__ __forceinline__ void quantise(const Group &g, const uint4 *from, int6
     }
 }
 
-// The groups that begin in a window of 16 rows: lane l of each warp has the slot of row `first` + l, -1 if it is left out.
+// The groups that begin in a window of 16 rows: lane l of each warp has the slot of row `first` + l, -1 if it is skipped.
+// A group's rows lie within 16, with none but skipped ones among them, so that 32 rows in front say whether one begins it.
 // `meanwhile` is done while the slots are on their way, given the row behind `first`.
 struct Window {
     int64_t first, slot;
@@ -250,16 +253,26 @@ struct Window {
             slot = -1;
         }
         slot = slot < 0 ? -1 : slot;
-        const int64_t before = __shfl_up_sync(0xffffffffu, group(), 1);
+        // the group of the last row in front that is not skipped
+        const unsigned taken = __ballot_sync(0xffffffffu, slot >= 0), front = taken & ((1u << lane) - 1);
+        int64_t before = __shfl_sync(0xffffffffu, group(), front != 0 ? 31 - __clz(front) : 0);
+        if (!(taken & 1) && first > 0) {
+            int64_t older = -1;
+            if (mine >= 32)
+                older = __ldg(p.slots + (mine - 32));
+            older = older >= p.cache.num_blocks << p.cache.page_shift ? -1 : older;
+            const unsigned some = __ballot_sync(0xffffffffu, older >= 0);
+            older = __shfl_sync(0xffffffffu, older, some != 0 ? 31 - __clz(some) : 0);
+            if (front == 0)
+                before = some != 0 ? older >> 4 : -1;
+        }
         begins = __ballot_sync(0xffffffffu, lane >= 1 && lane <= kGroup && slot >= 0 && group() != before);
     }
     __device__ __forceinline__ int64_t group() const { return slot >> 4; }
-    // rows of the group that begins with lane l's
-    __device__ __forceinline__ int rows(int l) const
+    // which of the 16 rows from lane l's on are of its group
+    __device__ __forceinline__ unsigned rows(int l) const
     {
-        const unsigned other = ~(__ballot_sync(0xffffffffu, group() == __shfl_sync(0xffffffffu, group(), l)) >> l);
-        const int n = __ffs(other) - 1;
-        return n < 0 || n > kGroup ? kGroup : n;
+        return __ballot_sync(0xffffffffu, group() == __shfl_sync(0xffffffffu, group(), l)) >> l & 0xffffu;
     }
 };
 
@@ -329,12 +342,12 @@ struct Team {
     // one group's rows of the heads first to end - 1
     __device__ __forceinline__ void group(const Window &w, int l, int first, int end)
     {
-        const int n = w.rows(l);
+        const unsigned rows = w.rows(l);
         const int64_t id = __shfl_sync(0xffffffffu, w.slot, l) >> 4, row = w.first + l + i;
         const int spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
-        const unsigned tokens = __reduce_or_sync(0xffffffffu, lane < n ? 1u << spot : 0u);
+        const unsigned tokens = __reduce_or_sync(0xffffffffu, (rows >> lane) & 1 ? 1u << spot : 0u);
         const int token = (int)(__shfl_sync(0xffffffffu, w.slot, (l + i) & 31) & (kGroup - 1));
-        const bool on = i < n, anew = tokens & 1, turned = v < rope.pairs / 8;
+        const bool on = (rows >> i) & 1, anew = tokens & 1, turned = v < rope.pairs / 8;
         int a, b;
         lane_vectors(v, rope.pairs, kHalf, a, b);
         Spins spins;
@@ -560,9 +573,9 @@ kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ R
         share(w.begins, planes, part, p.parts_log, [&](int l, int from, int to) {
             const int64_t id = __shfl_sync(0xffffffffu, w.slot, l) >> 4;
             Group g;
-            g.n = w.rows(l);
+            g.rows = w.rows(l);
             g.spot = (int)(__shfl_sync(0xffffffffu, w.slot, (l + lane) & 31) & (kGroup - 1));
-            g.tokens = __reduce_or_sync(0xffffffffu, lane < g.n ? 1u << g.spot : 0u);
+            g.tokens = __reduce_or_sync(0xffffffffu, (g.rows >> lane) & 1 ? 1u << g.spot : 0u);
 #pragma unroll 1
             for (int x = from; x < to; ++x) {
                 const int head_plane = kRope ? 2 * x + 1 : x;
