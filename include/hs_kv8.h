@@ -110,6 +110,11 @@ hs_status hs_rope_apply(const hs_attn_shape *shp, const hs_rope *rope, const voi
  * two from 2^-126 to 2^120.  A block is a page that hs_restore_kv_pages, hs_restore_request and
  * hs_save_kv_pages move (page_bytes = the block's bytes): its scales travel with it.  Key j of a request lies
  * in block block_table[request][j / page_size] as token j % page_size.
+ * KV heads h to h + n - 1 of a block are two ranges, the values and behind all values the scales.
+ * hs_restore_kv_page_slices and hs_save_kv_page_slices move each with rows = 1:
+ *     values  col_off = h * B,                   col_bytes = n * B,  B = 2 * page_size * head_dim
+ *     scales  col_off = n_kv_heads * B + h * S,  col_bytes = n * S,  S = page_size / 2
+ * which have to be multiples of 16: with pages of 16 tokens h and n are even.
  *
  * shp->dtype is the type of q, k, v, o and of the 16-bit cache, not of this one's.
  */
