@@ -173,8 +173,8 @@ hs_status hs_kv8_append_rope(const hs_attn_shape *shp, const hs_rope *rope, cons
  * Arithmetic: q . k as products of binary16 numbers with float32 sums (E4M3 fits it; a bf16 q is scaled by a
  * power of two for each row, elements below 2^-24 of its largest lose bits and those below 2^-39 count as zero);
  * maxima, sums and lse in float32; the weights times the values' scales as the sum of two binary16 numbers before the
- * product with v (2^-22 relative, or half a step of 2^-32 of the row's largest weight times the largest scale where that is
- * more); the outputs once at the end, kept within the element type's finite values.
+ * product with v (2^-22 relative, or 2^-32 of the row's largest weight times the largest scale where that is more); the
+ * outputs once at the end, kept within the element type's finite values.
  * Scores must lie within float32's range; a weight below 2^-126 of the row's largest counts as zero.
  * With shp->unsplit a row's result depends on nothing but its query and its keys; without it, the keys of one
  * row may be shared out by the sizes of the call, and equal calls give equal bits.

@@ -39,8 +39,9 @@ def bounded(q, k, v, v_scale, scale, dtype):
     lost = q.abs().amax(dim=2)[..., None] * k.abs().sum(dim=2)[:, None] * scale * 2.0 ** -39 * (some > 1)
     off = (some + 8) * 2.0 ** -23 * size + lost + 2.0 ** -20 + 2.0 ** -23 * (s.amax(dim=2, keepdim=True) - s)
     do = torch.einsum("agn,and->agd", w * off, v.abs()) + o.abs() * (w * off).sum(dim=2, keepdim=True)
-    # the weight in front of the product: two binary16 numbers, and half a step of 2^-32 of the largest weight and scale
-    floor = 2.0 ** -33 * w.amax(dim=2) * v_scale[:, None] * 448.0 * n
+    # The weight in front of the product: two binary16 numbers, the second to half a step of 2^-24 where the row's largest
+    # weight, at the largest scale, is 2^7 or more: 2^-32 of it.
+    floor = 2.0 ** -32 * w.amax(dim=2) * v_scale[:, None] * 448.0 * n
     do = do + 2.0 ** -22 * mag + floor[..., None]
     # Sums of a tile's products are cut to float32 behind at most four passes, 2^-24 each of the running sum and of the
     # tile's magnitudes; a running sum is the difference of two of the sums from the first key on.  200 more for joins.
