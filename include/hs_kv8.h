@@ -140,7 +140,7 @@ hs_status hs_kv8_block_bytes(const hs_attn_shape *shp, int64_t *bytes_out);
  * a request do, and slots >= 0 must be distinct: else the group's values mean nothing.  A value that is not finite becomes
  * NaN and takes no part in M.
  * k, v and the cache must be 16-byte aligned and must not overlap.
- * Errors: as hs_kv_append.
+ * Errors: as hs_kv_append (HS_ERR_UNSUPPORTED also for 2^31 rows).
  */
 hs_status hs_kv8_append(const hs_attn_shape *shp, const void *k, const void *v, int64_t kv_stride,
                         const int64_t *slots, int64_t n_rows, void *cache, int32_t *d_err,

@@ -11,9 +11,9 @@
 // 16 rows in registers, so that M and the bytes come from one read.  Keys that are turned are taken by teams of D threads, a
 // lane 16 values of one row, and q by blocks of their own, as hs_rope_apply does.
 //
-// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 29.7 us, 6.0 TB/s; with
-// positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.4 us, 5.4.  A step of 64 rows
-// with positions takes 4.1 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
+// Bound by HBM where there are many rows: 28,913 rows of 8 x 128 keys and values (178 MB) take 29.5 us, 6.0 TB/s; with
+// positions and 32 heads of q, 28,000 rows 107 us, 6.0 TB/s; 14,494 rows of 16 + 4 heads 30.6 us, 5.3.  A step of 64 rows
+// with positions takes 4.2 us: four loads that wait for one another, sines and cosines, a meeting of four warps a head.
 //
 // Turned values are good to 2^-21 of |x| + |y|: the angle is good to 2^-25 half turns, sines and cosines to 2^-24, and four
 // more roundings follow (sum 2^-21.3), which leaves room for 2^-23.3 radians that the 64 bits of an angle lack at
@@ -52,7 +52,7 @@ __device__ __forceinline__ Two two_of(uint64_t magnitude, bool negative)
 
 // Element `second` of the pair (x, y) times `by` turned, to 2^-45 of |x| + |y|: what lies next to a border of rounding is
 // decided by it.  The angle's sine and cosine are Taylor's series of at most an eighth of a turn in integers of 64 bits
-// (to 2^-54), which need neither tables nor the float64 units: with those a step of 64 rows took 5.1 us, not 4.1.
+// (to 2^-54), which need neither tables nor the float64 units: with those a step of 64 rows took 1 us more.
 __device__ __noinline__ Two turned_closely(int64_t angle, Two gain, float x, float y, float by, bool second)
 {
     // angle = quarter 2^62 + r, -2^61 <= r <= 2^61
@@ -276,8 +276,8 @@ struct Window {
     }
 };
 
-// Brings a head's 16 rows from row `first` on to L2 while the slots that say whose they are come: 28,913 rows of 8 x 128 29.7
-// us, 31.3 without; 4,000 of 32 + 8 x 128 with positions 18.7, 19.8.
+// Brings a head's 16 rows from row `first` on to L2 while the slots that say whose they are come: 28,913 rows of 8 x 128 29.5
+// us, 31.4 without; 4,000 of 32 + 8 x 128 with positions 18.7, 19.9.
 template <int D>
 __device__ __forceinline__ void ahead(const Kv8Append &p, const uint4 *head, int64_t first, int lane)
 {
@@ -290,7 +290,7 @@ __device__ __forceinline__ void ahead(const Kv8Append &p, const uint4 *head, int
 
 // Who shares a window takes a run of its (group, plane) pairs, the planes of a group one after the other: of a prompt's window
 // one group's, of a step's up to 16 groups'.  f(lane whose row begins the group, its planes `from` up to `to`).  Windows of
-// fewer rows, of which most begin nothing in a prompt, took 4.5 us for 1,000 rows of 8 x 128, not 3.9.
+// fewer rows, of which most begin nothing in a prompt, took 15 % longer for 1,000 rows of 8 x 128.
 template <typename F>
 __device__ __forceinline__ void share(unsigned begins, int planes, int part, int parts_log, F f)
 {
@@ -531,8 +531,8 @@ struct Team {
 };
 
 // Blocks: the turned keys' teams, which take longest; warps for the other planes' heads; q.  With positions 24 warps share an
-// SM (80 registers, a few of them spilled) where four meet for a head, 14,494 rows of 4 x 128 32.7 us, 36.4 with 16 warps;
-// 16 where two do, 12,000 rows of 16 x 64 35.3 us, 40.4 with 24.
+// SM (80 registers, a few of them spilled) where four meet for a head, 14,494 rows of 4 x 128 30.6 us, 33.9 with 16 warps;
+// 16 where two do, 12,000 rows of 16 x 64 34.8 us, 41.0 with 24.
 template <typename T, int D, bool kRope, bool kHalf>
 __global__ void __launch_bounds__(kThreads, kRope ? (D == 64 ? 4 : 6) : 8)
 kv8_append_kernel(const __grid_constant__ Kv8Append p, const __grid_constant__ RopeParams rope)
@@ -609,10 +609,10 @@ cudaError_t launch(Kv8Append p, const RopeParams *rope, int sm_count, cudaStream
     constexpr int kTeams = kThreads / D, kJobs = kThreads / (D / 16);
     constexpr int64_t most = INT32_MAX / 4;
     p.windows = (int)((p.n_rows + kGroup - 1) / kGroup);
-    // 24 warps for each SM (256 rows of 8 x 128, each a group, 4.1 us), or more: one for each plane of a prompt's group
-    // (28,913 rows 31.3 us; 34.8 with fewer, which wait for one group's rows after another).  Beside turned keys, whose teams
-    // are the longer part and share the SM, four (256 rows 6.9 us, 7.3 with eight), or one for each two heads
-    // (12,000 rows of 16 + 16 x 128 52 us, 63 with eight).
+    // 24 warps for each SM (256 rows of 8 x 128, each a group, 4.3 us), or more: one for each plane of a prompt's group
+    // (28,913 rows 29.5 us; 34.2 with fewer, which wait for one group's rows after another).  Beside turned keys, whose teams
+    // are the longer part and share the SM, four (256 rows 7.0 us, 7.4 with eight), or one for each two heads
+    // (12,000 rows of 16 + 16 x 128 51.6 us, 63.8 with eight).
     const int planes = (rope != nullptr ? 1 : 2) * p.cache.n_kv;
     int64_t warps = (int64_t)sm_count * (rope != nullptr ? 4 : 24);
     const int64_t prompt = (int64_t)p.windows * (rope != nullptr ? (planes + 1) / 2 : planes);
@@ -621,9 +621,9 @@ cudaError_t launch(Kv8Append p, const RopeParams *rope, int sm_count, cudaStream
     p.warp_blocks = ((p.windows << p.parts_log) + kThreads / 32 - 1) / (kThreads / 32);
     int64_t blocks = p.warp_blocks;
     if (rope != nullptr) {
-        // Teams of up to 8 heads, so that sines and cosines are worth it (14,494 rows of 4 heads 30.9 us, 32.7 with 2 to
-        // a team) and the last wave stays short (12,000 rows of 16 heads 51.7 us, 59.4 with all in a team); of
-        // fewer where there are not two to an SM (2,000 rows of 8 heads 10.6 us so, 12.0 with four, 12.3 with one).
+        // Teams of up to 8 heads, so that sines and cosines are worth it (14,494 rows of 4 heads 30.6 us, 32.4 with 2 to
+        // a team) and the last wave stays short (12,000 rows of 16 heads 51.6 us, 59.2 with all in a team); of
+        // fewer where there are not two to an SM (2,000 rows of 8 heads 10.7 us so, 12.0 with four, 12.1 with one).
         const int64_t eights = (int64_t)p.windows * ((p.cache.n_kv + 7) / 8);
         int64_t teams = (int64_t)sm_count * 2 * kTeams;
         teams = eights > teams ? eights : teams;

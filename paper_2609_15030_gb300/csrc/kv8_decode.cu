@@ -21,16 +21,17 @@
 //
 // Few rows share a tile's bytes (the heads of one KV head), so the step is bound by HBM; products of M = 128 rows as in
 // the 16-bit attention would leave most of the tensor core's rows empty, and the bytes would have to
-// become numbers on a way through shared memory.  Four requests of 98k to 131k keys (943 MB) take 146 us, 6.5 TB/s, where
-// the 16-bit step takes 269 to 279; 64 of 4,096 keys of 8 heads 91 us, 5.9 TB/s; 32 ragged ones 33 us, of which HBM
+// become numbers on a way through shared memory.  Four requests of 98k to 131k keys (943 MB) take 145 us, 6.5 TB/s, where
+// the 16-bit step takes 269 to 279; 64 of 4,096 keys of 8 heads 90 us, 5.9 TB/s; 32 ragged ones 34 us, of which HBM
 // accounts for 22 (3.5 us until the first tiles are there, 2 to 5 for the ends and the join's launch, 2 for the join); one
-// of 4,600 keys 9.0 us, latency.  16 rows to a KV head (155 us for 799 MB, 5.1 TB/s) and heads of 64 (58 us for 268 MB) are bound by
-// instructions: 650 a tile and warp, 100 of them conversions, with 2 to 4 warps to a scheduler.
+// of 4,600 keys 8.9 us, latency.  16 rows to a KV head (169 us for 799 MB, 4.7 TB/s) and heads of 64 (59 us for 268 MB) are
+// bound by instructions: 475 and 320 a tile and warp (395 for 8 rows of 128), 64 and 32 of them conversions of keys
+// and values, with 2 to 4 warps to a scheduler.
 //
-// What was tried: loads into registers (two blocks of 8 warps to an SM: 154 us for the long ones, 67 for heads of 64, 82 for 16
-// rows where the ring takes 63; no room for more than one tile ahead); the ring by asynchronous copies of 16 bytes (205 us: they and
-// the reads share one queue); prefetches into L2 (1 to 4 tiles ahead: no gain); two tiles to a step (148 us, but 11.3 us
-// for one request: code that runs once waits for its instructions).
+// What was tried, against the ring when it was new: loads into registers (two blocks of 8 warps to an SM: 5 % more for the long
+// ones, 15 for heads of 64, 30 for 16 rows; no room for more than one tile ahead); the ring by asynchronous copies of 16
+// bytes (40 %: they and the reads share one queue); prefetches into L2 (1 to 4 tiles ahead: no gain); two tiles to a step
+// (1 %, but 25 for one request: code that runs once waits for its instructions).
 #include "attn_ptx.cuh"
 #include "kv8_walk.cuh"
 #include "tensor_map.cuh"
@@ -960,9 +961,9 @@ int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
         return -1;
     // Whole items: as many warps to each as the SMs have for it, and as it has steps.  They save the join and the walk over
     // lengths, 2 to 5 us, and cost what the longest item takes its warps above an even share.  128 short requests of 2 heads
-    // 7.0 us instead of 12.8 split, 300 of 8 heads of up to 150 keys 22.2 instead of 27.4, 32 of 4 heads of up to 2,000 keys
-    // 16.7 instead of 19.1; but with one warp to an item 128 of 8 heads of up to 400 keys (25 tiles) 27.7 instead of 23.9, and
-    // where half of the SMs would have none, one request of 4 heads of 1,500 keys (8 tiles to a warp) 12.0 instead of 9.4.
+    // 7.1 us instead of 12.9 split, 300 of 8 heads of up to 150 keys 23.9 instead of 29.7, 32 of 4 heads of up to 2,000 keys
+    // as fast either way (16.5); but with one warp to an item 128 of 8 heads of up to 400 keys (25 tiles) 29.4 instead of 24.3,
+    // and where half of the SMs would have none, one request of 4 heads of 1,500 keys (8 tiles to a warp) 12.3 instead of 8.8.
     const int64_t rounds = (items + sm_count - 1) / sm_count, steps = (longest + S::kTiles - 1) / S::kTiles;
     int64_t warps = rounds < S::kWarps ? S::kWarps / rounds : 1;
     if (warps > steps)
@@ -977,7 +978,7 @@ int64_t make_plan(AttnParams &p, Kv8Plan &plan, int sm_count)
         plan.ctas = (int)(items < most ? items : most);
     } else {
         // A block to each SM, fewer where they would not be full: a step to a warp.  One request of one KV head and 8,000 keys
-        // 9.3 us in 16 blocks of 16 warps, 12.4 in 152 of two, whose many parts are joined.
+        // of 64 9.1 us in 16 blocks of 16 warps, 10.2 in 152 of two, whose many parts are joined.
         const int64_t all = (items * steps + S::kWarps - 1) / S::kWarps;
         plan.ctas = (int)(all < sm_count ? all : sm_count);
         warps = S::kWarps;

@@ -3,8 +3,8 @@
 //
 // Bytes in, twice as many out: bound by HBM.  Units of 16 tokens (a group, all heads, both planes) are shared
 // out evenly over the blocks, whatever the requests' lengths.  A thread takes 16 bytes of a token to 32, of up to
-// eight (KV head, plane) at a time.  459,413 tokens of 8 heads of 128 (2.82 GB) take 434 us, 6.5 TB/s; with 8 bytes to
-// 16 and as many loads in flight 461.  Groups of fewer heads have fewer loads for a thread (16 requests of 3,000 tokens of 4
+// eight (KV head, plane) at a time.  459,413 tokens of 8 heads of 128 (2.82 GB) take 435 us, 6.5 TB/s; with 8 bytes to
+// 16 and as many loads in flight 6 % more.  Groups of fewer heads have fewer loads for a thread (16 requests of 3,000 tokens of 4
 // heads: 26 us, 5.5 TB/s); taking several groups at a time, each vector with its own table entries, cost more than it
 // brought (35 us).
 #include "kv8_walk.cuh"
